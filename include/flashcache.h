@@ -279,6 +279,124 @@ fc_status flashcache_decode_attention_paged(const void* Q, const void* K_pages, 
                                             float scale, float* out, void* workspace,
                                             size_t workspace_bytes, void* hip_stream);
 
+/* ---- the decode loop around a compacted cache: positions, pages, a cache in four bits ---------------------------- */
+
+/* Rotary positions of queries and keys.  Pair i < rotary_dim / 2 of every head, columns (i, i + rotary_dim / 2) or, interleaved,
+ * (2i, 2i + 1), is turned by the angle position * f_i:  y0 = m (x0 cos - x1 sin), y1 = m (x1 cos + x0 sin).  Columns from rotary_dim on are
+ * copied.  f_i = theta^(-2i / rotary_dim), rescaled by `factor` s for contexts longer than the model was trained on:
+ *   FC_ROTARY_LINEAR  f_i / s
+ *   FC_ROTARY_BASE    theta * s^(rotary_dim / (rotary_dim - 2)) in place of theta
+ *   FC_ROTARY_PARTS   by the turns n_i = original_tokens * f_i / (2 pi) that a pair makes over the original context: f_i from beta_fast turns
+ *                     on, f_i / s up to beta_slow, and between them f_i g + (f_i / s) (1 - g) with g = (n_i - beta_slow) / (beta_fast -
+ *                     beta_slow); m = 0.1 ln s + 1
+ * `streams` (1 to 4) sequences of positions share out the pairs: the first stream_pairs[0] pairs turn by the first one, the next
+ * stream_pairs[1] by the second (time, height and width of images, for instance); with one stream stream_pairs is not read.
+ * `magnitude` m, 0: as above, 1 without FC_ROTARY_PARTS. */
+typedef enum { FC_ROTARY_PLAIN = 0, FC_ROTARY_LINEAR = 1, FC_ROTARY_BASE = 2, FC_ROTARY_PARTS = 3 } fc_rotary_scaling;
+#define FC_ROTARY_MAX_PAIRS 128
+typedef struct {
+  int32_t rotary_dim, interleaved, scaling, original_tokens, streams, stream_pairs[4], reserved;
+  double theta, factor, beta_fast, beta_slow, magnitude;
+} fc_rotary_spec;
+
+/* What flashcache_rotary needs to know, in host memory: filled by flashcache_rotary_prepare, copied into each launch. */
+typedef struct {
+  uint32_t magic;
+  int32_t rotary_dim, interleaved, streams, stream_end[4];
+  float magnitude;
+  int32_t reserved;
+  uint64_t turns[FC_ROTARY_MAX_PAIRS];   /* of each pair, per position, in units of 2^-64 turns */
+} fc_rotary_plan;
+
+/* Host only.  `frequencies` (host, rotary_dim / 2 of them, radians per position) replaces theta and the scaling; NULL: as the spec
+ * says.  FC_EINVAL for an odd rotary_dim, pairs that the streams do not share out exactly, a factor below 1 or values that are not finite;
+ * FC_EUNSUPPORTED beyond 256 columns. */
+fc_status flashcache_rotary_prepare(const fc_rotary_spec* spec, const double* frequencies, fc_rotary_plan* plan);
+
+/* Heads of new tokens: element (b,t,h,c) of the input is at base + b*stride_b + t*stride_t + h*stride_h + c, of the output by the out_
+ * strides (elements, the head dimension contiguous). */
+typedef struct {
+  int32_t batch, tokens, heads, head_dim;
+  int32_t dtype, reserved;                                   /* fc_dtype */
+  int64_t stride_b, stride_t, stride_h;
+  int64_t out_stride_b, out_stride_t, out_stride_h;
+} fc_heads_desc;
+
+/* Turns Q and, unless k_desc is NULL, K (same batch, tokens, head_dim and dtype, any number of heads) in one launch.
+ *   plan       host; read before the call returns
+ *   positions  device in, int32 [streams][batch][tokens]; any value, negative ones too
+ *   Q_out, K_out  device out, in the input dtype: sines, cosines and products in fp32, rounded once.  May be the inputs themselves
+ *              (same strides); any other overlap gives unspecified values
+ *   inverse    != 0: the transposed map, sin -> -sin: the gradient of the inputs from that of the outputs
+ * Any even head_dim from rotary_dim to 512; pointers and strides that are multiples of 16 bytes are fastest. */
+fc_status flashcache_rotary(const fc_rotary_plan* plan, const int32_t* positions, const void* Q, void* Q_out,
+                            const fc_heads_desc* q_desc, const void* K, void* K_out, const fc_heads_desc* k_desc,
+                            int32_t inverse, void* hip_stream);
+
+/* Block tables and slot maps, on the device.  Every head of layer l of sequence b holds rows[b][l] rows and adds add[b][l] of them (NULL:
+ * add_each); its pages are ceil(rows / page_size), and those that the added rows begin are taken from the free list, units in the order of
+ * sequence, layer, head:
+ *   rows, add    device in, int32 [batch][layers]; negative values count as 0
+ *   free_pages   device in, int32 [num_free] (NULL: page i is i); cursor device in, int64: pages of it already taken
+ *   block_table  device in/out, int32 [batch][layers][kv_heads][max_pages], as flashcache_select_gather_paged takes it: entries of pages that
+ *                are begun are written, -1 where the free list is at its end; the others stay as they are
+ *   slots        device out, int64 [batch][slots_per_seq], or NULL: page * page_size + row % page_size of the added rows of each sequence in
+ *                the order of layer, head, row (of a fresh cache: the packed order of flashcache_select_gather); -1 for a row without a
+ *                page and behind the last row; rows from slots_per_seq on get pages, but no place in the map
+ *   rows_out, cursor_out  device out: rows[b][l] + add[b][l], and the cursor behind the pages that were asked for (beyond num_free: that
+ *                many were missing).  They may be `rows` and `cursor` themselves (a second, tiny launch then updates them).
+ * Pages from max_pages on are neither taken nor written; rows count up to 2^25 - 1.  At most 1024 layers and 2^25 rows a page. */
+fc_status flashcache_assign_pages(const int32_t* rows, const int32_t* add, int32_t add_each, int32_t batch, int32_t layers,
+                                  int32_t kv_heads, int32_t page_size, int32_t max_pages, const int32_t* free_pages,
+                                  int64_t num_free, const int64_t* cursor, int32_t* block_table, int64_t* slots,
+                                  int64_t slots_per_seq, int32_t* rows_out, int64_t* cursor_out, void* hip_stream);
+
+/* ---- the 4-bit paged cache.  K and V rows in blocks of 32 columns that share a power of two 2^(E - 127); a value is e2m1 (0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6 and their negatives) times it, rounded to nearest, ties to the even code.  E is the least that puts the block's largest
+ * magnitude below 7 * 2^(E - 127), in [2, 252], what exceeds the largest value becomes it; a block with an infinity or NaN is NaN in all
+ * of its columns.  A row of K and V takes 17 d / 16 bytes (bf16: 4 d).
+ * head_dim is 64 or 128, page_size a multiple of 16; `pages` is [num_pages][flashcache_mx_page_bytes], 16-byte aligned.  Slot s is row s % 16
+ * of tile s / 16, 17 d bytes each: K codes [16][d/2], V codes [row/4][16][row%4][d/32] (d/16 neighbouring columns in one place), K scales
+ * [d/32][16], V scales [row/4][d/32][row%4]; the lower nibble is the even column.  Slots and pages that nothing was stored in hold
+ * whatever the memory holds; they may be read, and no attention reads rows from the given number on. */
+size_t flashcache_mx_page_bytes(int32_t page_size, int32_t head_dim);   /* 0 if unsupported */
+
+/* Rows of K and of V: row r of sequence b begins at base + b*stride_b + r*stride_r elements. */
+typedef struct {
+  int32_t batch, head_dim, dtype, reserved;
+  int64_t rows, stride_b, stride_r;
+} fc_rows_desc;
+
+/* K and V rows into their slots (device in, int64 [batch][rows]; negative ones and those beyond the pages: the row is left out).  No slot
+ * may come twice in a call (it would hold a mixture of both rows); other slots stay as they are.  Rows are 16-byte aligned. */
+fc_status flashcache_mx_store(const void* K, const void* V, const fc_rows_desc* desc, const int64_t* slots, int32_t page_size,
+                              int64_t num_pages, void* pages, void* hip_stream);
+
+/* ... and back, in the dtype of the descriptor (both hold every value exactly); zeros for rows without a slot. */
+fc_status flashcache_mx_load(const int64_t* slots, const void* pages, int32_t page_size, int64_t num_pages,
+                             const fc_rows_desc* desc, void* K, void* V, void* hip_stream);
+
+/* flashcache_select_gather_paged into a 4-bit cache: selection and idx_out as there (shared: as its shared mode), kept row j of a unit goes to
+ * slot j % page_size of page block_table[b][l][h][j / page_size]. */
+fc_status flashcache_select_gather_mx(const void* K, const void* V, const fc_kv_desc* desc, const float* scores,
+                                      const int32_t* budgets, const int64_t* layer_offsets, int64_t rows_per_seq,
+                                      int32_t shared, int32_t* idx_out, const int32_t* block_table, int32_t page_size,
+                                      int32_t max_pages, int64_t num_pages, void* pages, void* hip_stream);
+
+/* flashcache_decode_attention_paged over a 4-bit cache: one new token a sequence attends to the first rows[b][l] rows of each unit.
+ *   Q     device in, [B][L][q_heads][d], dtype per `dtype`; out device out, float [B][L][q_heads][d]
+ *   rows  device in, int32 [B][L].  Rows whose page entry is missing (negative, >= num_pages, from max_pages on) are not attended to; a unit
+ *         without attended rows gives zeros
+ *   workspace  device, 16-byte aligned, flashcache_mx_decode_workspace_bytes() bytes; calls that may run at the same time need one each
+ * 1 to 16 query heads a KV head for both dtypes.  Products of the cache's values (exact in bf16) on the matrix cores with queries and
+ * probabilities of 24 bits, sums and softmax in fp32. */
+size_t flashcache_mx_decode_workspace_bytes(int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads, int32_t head_dim);
+fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const int32_t* block_table, int32_t page_size,
+                                         int32_t max_pages, int64_t num_pages, int32_t batch, int32_t layers,
+                                         int32_t kv_heads, int32_t q_heads, int32_t head_dim, int32_t dtype,
+                                         const int32_t* rows, float scale, float* out, void* workspace,
+                                         size_t workspace_bytes, void* hip_stream);
+
 /* Measurement aid (off by default; not part of the method).  While enabled, every kernel the
  * library launches is bracketed by a pair of HIP events on its launch stream.
  * flashcache_profile_enable(on) clears the records and switches recording on or off.

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -32,6 +32,9 @@ EXPORTED_SYMBOLS = (
     "flashcache_decode_workspace_bytes", "flashcache_decode_attention",
     "flashcache_decode_attention_paged", "flashcache_decode_static_scratch_bytes",
     "flashcache_decode_attention_static", "flashcache_status_string",
+    "flashcache_rotary_prepare", "flashcache_rotary", "flashcache_assign_pages", "flashcache_mx_page_bytes",
+    "flashcache_mx_store", "flashcache_mx_load", "flashcache_select_gather_mx", "flashcache_mx_decode_workspace_bytes",
+    "flashcache_mx_decode_attention",
     "flashcache_profile_enable", "flashcache_profile_read",
 )
 
@@ -42,6 +45,44 @@ class FcKvDesc(ctypes.Structure):
         ("n_tokens", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("stride_b", ctypes.c_int64), ("stride_l", ctypes.c_int64),
         ("stride_h", ctypes.c_int64), ("stride_n", ctypes.c_int64),
+    ]
+
+
+MAX_ROTARY_PAIRS = 128
+FC_ROTARY_PLAIN, FC_ROTARY_LINEAR, FC_ROTARY_BASE, FC_ROTARY_PARTS = range(4)
+ROTARY_SCALINGS = {"none": FC_ROTARY_PLAIN, "linear": FC_ROTARY_LINEAR, "base": FC_ROTARY_BASE, "parts": FC_ROTARY_PARTS}
+
+
+class FcRotarySpec(ctypes.Structure):
+    _fields_ = [
+        ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scaling", ctypes.c_int32),
+        ("original_tokens", ctypes.c_int32), ("streams", ctypes.c_int32), ("stream_pairs", ctypes.c_int32 * 4),
+        ("reserved", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+        ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double), ("magnitude", ctypes.c_double),
+    ]
+
+
+class FcRotaryPlan(ctypes.Structure):
+    _fields_ = [
+        ("magic", ctypes.c_uint32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("streams", ctypes.c_int32), ("stream_end", ctypes.c_int32 * 4), ("magnitude", ctypes.c_float),
+        ("reserved", ctypes.c_int32), ("turns", ctypes.c_uint64 * MAX_ROTARY_PAIRS),
+    ]
+
+
+class FcHeadsDesc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+        ("out_stride_b", ctypes.c_int64), ("out_stride_t", ctypes.c_int64), ("out_stride_h", ctypes.c_int64),
+    ]
+
+
+class FcRowsDesc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("rows", ctypes.c_int64), ("stride_b", ctypes.c_int64), ("stride_r", ctypes.c_int64),
     ]
 
 
@@ -101,6 +142,20 @@ def _load() -> ctypes.CDLL:
     lib.flashcache_select_gather_paged.argtypes = [vp, vp, c_desc_p, vp, vp, vp, i64, i32, vp, vp, i32, i32,
                                                    i64, vp, vp, vp, sz, vp]
     lib.flashcache_select_gather_paged.restype = i32
+    lib.flashcache_rotary_prepare.argtypes = [ctypes.POINTER(FcRotarySpec), ctypes.POINTER(dbl), ctypes.POINTER(FcRotaryPlan)]
+    lib.flashcache_rotary.argtypes = [ctypes.POINTER(FcRotaryPlan), vp, vp, vp, ctypes.POINTER(FcHeadsDesc), vp, vp,
+                                      ctypes.POINTER(FcHeadsDesc), i32, vp]
+    lib.flashcache_assign_pages.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, vp, i64, vp, vp, vp, i64, vp, vp, vp]
+    lib.flashcache_mx_page_bytes.argtypes, lib.flashcache_mx_page_bytes.restype = [i32, i32], sz
+    lib.flashcache_mx_store.argtypes = [vp, vp, ctypes.POINTER(FcRowsDesc), vp, i32, i64, vp, vp]
+    lib.flashcache_mx_load.argtypes = [vp, vp, i32, i64, ctypes.POINTER(FcRowsDesc), vp, vp, vp]
+    lib.flashcache_select_gather_mx.argtypes = [vp, vp, c_desc_p, vp, vp, vp, i64, i32, vp, vp, i32, i32, i64, vp, vp]
+    lib.flashcache_mx_decode_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.flashcache_mx_decode_workspace_bytes.restype = sz
+    lib.flashcache_mx_decode_attention.argtypes = [vp, vp, vp, i32, i32, i64, i32, i32, i32, i32, i32, i32, vp,
+                                                   ctypes.c_float, vp, vp, sz, vp]
+    for name in ("rotary_prepare", "rotary", "assign_pages", "mx_store", "mx_load", "select_gather_mx", "mx_decode_attention"):
+        getattr(lib, "flashcache_" + name).restype = i32
     lib.flashcache_status_string.argtypes, lib.flashcache_status_string.restype = [i32], ctypes.c_char_p
     return lib
 
@@ -299,6 +354,196 @@ def decode_attention_paged(Q: torch.Tensor, K_pages: torch.Tensor, V_pages: torc
     return out
 
 
+# ---- the decode loop around a compacted cache --------------------------------------------------
+def _dtype(t: torch.Tensor) -> int:
+    if t.dtype == torch.bfloat16:
+        return FC_BF16
+    if t.dtype == torch.float32:
+        return FC_F32
+    raise ValueError(f"unsupported dtype {t.dtype}")
+
+
+def _want(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape: Tuple[int, ...], device: torch.device) -> None:
+    """A contiguous tensor of this type, shape and device, or nothing at all."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _here(t: torch.Tensor, what: str) -> torch.device:
+    """The tensor's device, which has to be the current one: that is the device whose current stream the call goes to."""
+    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{what} must be on the current GPU")
+    return t.device
+
+
+def rotary_plan(rotary_dim: int, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                factor: float = 1.0, original_tokens: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                magnitude: float = 0.0, sections: Optional[Sequence[int]] = None,
+                frequencies: Optional[Sequence[float]] = None) -> FcRotaryPlan:
+    """What `rotary` needs (host memory; may be kept and used by any number of calls and threads).
+
+    scaling: "none", "linear", "base" or "parts" (flashcache.h has the formulas); sections: pairs that each of 2 to 4 streams
+    of positions turns; frequencies: radians per position of each pair, instead of theta and the scaling."""
+    spec = FcRotarySpec(rotary_dim=rotary_dim, interleaved=1 if interleaved else 0, scaling=ROTARY_SCALINGS[scaling],
+                        original_tokens=original_tokens, streams=1, theta=theta, factor=factor, beta_fast=beta_fast,
+                        beta_slow=beta_slow, magnitude=magnitude)
+    if sections is not None:
+        if not 1 <= len(sections) <= 4:
+            raise ValueError("sections: one to four streams of positions")
+        spec.streams = len(sections)
+        for k, n in enumerate(sections):
+            spec.stream_pairs[k] = n
+        if len(sections) == 1 and 2 * sections[0] != rotary_dim:
+            raise ValueError("sections must share out all pairs")
+    given = None
+    if frequencies is not None:
+        if 2 * len(frequencies) != rotary_dim:
+            raise ValueError("a frequency for each pair")
+        given = (ctypes.c_double * len(frequencies))(*frequencies)
+    plan = FcRotaryPlan()
+    _check(_lib.flashcache_rotary_prepare(ctypes.byref(spec), given, ctypes.byref(plan)), "flashcache_rotary_prepare")
+    return plan
+
+
+def _heads(x: torch.Tensor, out: torch.Tensor, what: str) -> FcHeadsDesc:
+    B, T, H, d = x.shape
+    if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+        raise ValueError(f"{what} and its output must agree in shape, dtype and device")
+    if (x.stride(3) != 1 or out.stride(3) != 1) and d > 1:
+        raise ValueError("the head dimension must be contiguous")
+    return FcHeadsDesc(B, T, H, d, _dtype(x), 0, x.stride(0), x.stride(1), x.stride(2), out.stride(0), out.stride(1), out.stride(2))
+
+
+def rotary(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K: Optional[torch.Tensor] = None,
+           Q_out: Optional[torch.Tensor] = None, K_out: Optional[torch.Tensor] = None,
+           inverse: bool = False) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Rotary positions of Q [B, T, Hq, d] and K [B, T, Hk, d] (any strides, innermost contiguous); positions int32
+    [B, T], or [streams, B, T].  Q_out / K_out may be Q and K themselves; without them new tensors are returned.
+    inverse: the transposed map, which takes gradients of the outputs to gradients of the inputs."""
+    if Q.dim() != 4 or (K is not None and (K.dim() != 4 or K.shape[:2] != Q.shape[:2] or K.device != Q.device)):
+        raise ValueError("Q and K must have shape [B, T, H, d], with B and T in common")
+    _here(Q, "Q")
+    shape = tuple(Q.shape[:2]) if plan.streams == 1 and positions.dim() == 2 else (plan.streams, *Q.shape[:2])
+    _want(positions, "positions", torch.int32, shape, Q.device)
+    if Q_out is None:
+        Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if K is not None and K_out is None:
+        K_out = torch.empty(K.shape, dtype=K.dtype, device=K.device)
+    qd = _heads(Q, Q_out, "Q")
+    kd = None if K is None else _heads(K, K_out, "K")
+    _check(_lib.flashcache_rotary(ctypes.byref(plan), _ptr(positions), _ptr(Q), _ptr(Q_out), ctypes.byref(qd), _ptr(K),
+                                  None if K is None else _ptr(K_out), None if kd is None else ctypes.byref(kd),
+                                  1 if inverse else 0, _stream()), "flashcache_rotary")
+    return Q_out, (None if K is None else K_out)
+
+
+def assign_pages(rows: torch.Tensor, add, page_size: int, block_table: torch.Tensor, cursor: torch.Tensor,
+                 free_pages: Optional[torch.Tensor] = None, num_free: Optional[int] = None,
+                 slots: Optional[torch.Tensor] = None, rows_out: Optional[torch.Tensor] = None,
+                 cursor_out: Optional[torch.Tensor] = None) -> None:
+    """Pages and slots for the rows that each layer adds: rows int32 [B, L] held, add int32 [B, L] or a number for all;
+    block_table int32 [B, L, H, max_pages] (in/out); cursor int64 [1]; free_pages int32 [n] (None: pages 0 .. num_free - 1);
+    slots int64 [B, n] (out).  rows_out / cursor_out default to `rows` and `cursor`, updated in place."""
+    if block_table.dim() != 4:
+        raise ValueError("block_table must have shape [B, L, H, max_pages]")
+    B, L, H, most = block_table.shape
+    dev = _here(block_table, "block_table")
+    _want(block_table, "block_table", torch.int32, (B, L, H, most), dev)
+    each = 0 if isinstance(add, torch.Tensor) else int(add)
+    for t, what in ((rows, "rows"), (rows_out, "rows_out"), (add if isinstance(add, torch.Tensor) else None, "add")):
+        _want(t, what, torch.int32, (B, L), dev)
+    for t, what in ((cursor, "cursor"), (cursor_out, "cursor_out")):
+        _want(t, what, torch.int64, (1,), dev)
+    if free_pages is None and num_free is None:
+        raise ValueError("either free_pages or num_free")
+    if free_pages is not None:
+        _want(free_pages, "free_pages", torch.int32, (free_pages.numel(),), dev)
+        num_free = free_pages.numel() if num_free is None else num_free
+        if num_free > free_pages.numel():
+            raise ValueError("num_free exceeds the list")
+    if slots is not None:
+        _want(slots, "slots", torch.int64, (B, slots.numel() // max(B, 1)), dev)
+    _check(_lib.flashcache_assign_pages(
+        _ptr(rows), _ptr(add) if isinstance(add, torch.Tensor) else None, each, B, L, H, page_size, most, _ptr(free_pages),
+        num_free, _ptr(cursor), _ptr(block_table), _ptr(slots), 0 if slots is None else slots.numel() // max(B, 1),
+        _ptr(rows if rows_out is None else rows_out), _ptr(cursor if cursor_out is None else cursor_out), _stream()),
+        "flashcache_assign_pages")
+
+
+def mx_page_bytes(page_size: int, head_dim: int) -> int:
+    """Bytes of a page of the 4-bit cache, K and V; 0 if unsupported."""
+    return int(_lib.flashcache_mx_page_bytes(page_size, head_dim))
+
+
+def _mx_pages(pages: torch.Tensor, page_size: int, head_dim: int, device: torch.device) -> int:
+    nbytes = mx_page_bytes(page_size, head_dim)
+    if nbytes == 0:
+        raise FlashCacheError(FC_EUNSUPPORTED, "flashcache_mx_page_bytes")
+    _want(pages, "pages", torch.uint8, (pages.shape[0], nbytes), device)
+    return pages.shape[0]
+
+
+def _mx_rows(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor) -> FcRowsDesc:
+    if K.dim() != 3 or K.shape != V.shape or K.stride() != V.stride() or K.dtype != V.dtype or K.device != V.device:
+        raise ValueError("K and V must have shape [B, R, d], the same strides, dtype and device")
+    B, R, d = K.shape
+    if K.stride(2) != 1:
+        raise ValueError("the head dimension must be contiguous")
+    _want(slots, "slots", torch.int64, (B, R), _here(K, "K"))
+    return FcRowsDesc(B, d, _dtype(K), 0, R, K.stride(0), K.stride(1))
+
+
+def mx_store(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, page_size: int) -> None:
+    """Rows K, V [B, R, d] into slots int64 [B, R] (negative: left out) of pages uint8 [num_pages, mx_page_bytes]."""
+    desc = _mx_rows(K, V, slots)
+    n = _mx_pages(pages, page_size, K.shape[2], K.device)
+    _check(_lib.flashcache_mx_store(_ptr(K), _ptr(V), ctypes.byref(desc), _ptr(slots), page_size, n, _ptr(pages), _stream()),
+           "flashcache_mx_store")
+
+
+def mx_load(slots: torch.Tensor, pages: torch.Tensor, page_size: int, K_out: torch.Tensor, V_out: torch.Tensor) -> None:
+    """Rows of the slots int64 [B, R] into K_out, V_out [B, R, d] (bf16 or fp32, both exact); zeros without a slot."""
+    desc = _mx_rows(K_out, V_out, slots)
+    n = _mx_pages(pages, page_size, K_out.shape[2], K_out.device)
+    _check(_lib.flashcache_mx_load(_ptr(slots), _ptr(pages), page_size, n, ctypes.byref(desc), _ptr(K_out), _ptr(V_out), _stream()),
+           "flashcache_mx_load")
+
+
+def select_gather_mx(K: torch.Tensor, V: torch.Tensor, desc: FcKvDesc, scores: torch.Tensor, budgets: torch.Tensor,
+                     layer_offsets: torch.Tensor, rows_per_seq: int, idx_out: torch.Tensor, block_table: torch.Tensor,
+                     page_size: int, pages: torch.Tensor, shared: bool = False) -> None:
+    """select_gather_paged into a 4-bit cache: pages uint8 [num_pages, mx_page_bytes]."""
+    n = _mx_pages(pages, page_size, desc.head_dim, _here(K, "K"))
+    _check(_lib.flashcache_select_gather_mx(
+        _ptr(K), _ptr(V), ctypes.byref(desc), _ptr(scores), _ptr(budgets), _ptr(layer_offsets), rows_per_seq,
+        1 if shared else 0, _ptr(idx_out), _ptr(block_table), page_size, block_table.shape[-1], n, _ptr(pages), _stream()),
+        "flashcache_select_gather_mx")
+
+
+def mx_decode_attention(Q: torch.Tensor, pages: torch.Tensor, page_size: int, kv_heads: int, rows: torch.Tensor,
+                        block_table: torch.Tensor, scale: float, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Q [B, L, Hq, d]; pages uint8 [num_pages, mx_page_bytes]; rows int32 [B, L]; block_table int32
+    [B, L, H, max_pages]; returns float32 [B, L, Hq, d]."""
+    B, L, Hq, d = Q.shape
+    dev = _here(Q, "Q")
+    n = _mx_pages(pages, page_size, d, dev)
+    _want(Q, "Q", Q.dtype, (B, L, Hq, d), dev)
+    _want(rows, "rows", torch.int32, (B, L), dev)
+    _want(block_table, "block_table", torch.int32, (B, L, kv_heads, block_table.shape[-1]), dev)
+    if workspace is None:
+        need = int(_lib.flashcache_mx_decode_workspace_bytes(B, L, kv_heads, Hq, d))
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+    if out is None:
+        out = torch.empty((B, L, Hq, d), dtype=torch.float32, device=dev)
+    _want(out, "out", torch.float32, (B, L, Hq, d), dev)
+    _check(_lib.flashcache_mx_decode_attention(
+        _ptr(Q), _ptr(pages), _ptr(block_table), page_size, block_table.shape[-1], n, B, L, kv_heads, Hq, d, _dtype(Q),
+        _ptr(rows), scale, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()),
+        "flashcache_mx_decode_attention")
+    return out
+
+
 def profile_enable(on: bool) -> None:
     _check(_lib.flashcache_profile_enable(1 if on else 0), "flashcache_profile_enable")
 
@@ -366,3 +611,50 @@ class Compressor:
         self.run_score(K, V)
         self.run_allocate()
         self.run_select_gather(K, V)
+
+
+class MxCache:
+    """A 4-bit paged cache and its block tables: filled from a compression, then extended and attended to step by step.
+
+    Pure plumbing, as `Compressor`: buffers through torch, calls on the current stream, nothing read back.  Of `num_pages`
+    pages the first ones are taken as rows come; `missing()` (synchronising) says how many were asked for beyond them.
+    A step is rotary (outside), append(k, v), attend(q), and may be captured into a graph."""
+
+    def __init__(self, batch: int, layers: int, kv_heads: int, head_dim: int, page_size: int, max_pages: int,
+                 num_pages: int, device="cuda"):
+        nbytes = mx_page_bytes(page_size, head_dim)
+        if nbytes == 0:
+            raise FlashCacheError(FC_EUNSUPPORTED, "flashcache_mx_page_bytes")
+        self.page_size, self.num_pages = int(page_size), int(num_pages)
+        self.shape = (int(batch), int(layers), int(kv_heads), int(head_dim))
+        self.pages = torch.empty((num_pages, nbytes), dtype=torch.uint8, device=device)
+        self.block_table = torch.full((batch, layers, kv_heads, max_pages), -1, dtype=torch.int32, device=device)
+        self.rows = torch.zeros((batch, layers), dtype=torch.int32, device=device)
+        self.cursor = torch.zeros(1, dtype=torch.int64, device=device)
+        self.slots = torch.empty((batch, layers * kv_heads), dtype=torch.int64, device=device)
+        self.workspace = None
+
+    def fill(self, comp: Compressor, K: torch.Tensor, V: torch.Tensor) -> None:
+        """The rows that `comp` (scored and allocated for this K, V) keeps, into the empty cache."""
+        assign_pages(self.rows, comp.budgets, self.page_size, self.block_table, self.cursor, num_free=self.num_pages)
+        select_gather_mx(K, V, comp.desc, comp.scores, comp.budgets, comp.layer_offsets, comp.rows_per_seq, comp.idx,
+                         self.block_table, self.page_size, self.pages, shared=comp.shared)
+
+    def append(self, k: torch.Tensor, v: torch.Tensor) -> None:
+        """One row more for every unit: k, v [B, L, H, d] contiguous."""
+        B, L, H, d = self.shape
+        assign_pages(self.rows, 1, self.page_size, self.block_table, self.cursor, num_free=self.num_pages, slots=self.slots)
+        mx_store(k.view(B, L * H, d), v.view(B, L * H, d), self.slots, self.pages, self.page_size)
+
+    def attend(self, q: torch.Tensor, scale: float, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """q [B, L, Hq, d]; float32 [B, L, Hq, d]."""
+        B, L, H, d = self.shape
+        if self.workspace is None:
+            need = int(_lib.flashcache_mx_decode_workspace_bytes(B, L, H, q.shape[2], d))
+            self.workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        return mx_decode_attention(q, self.pages, self.page_size, H, self.rows, self.block_table, scale, out=out,
+                                   workspace=self.workspace)
+
+    def missing(self) -> int:
+        """Pages that were asked for and not there (their rows are not stored): reads the cursor back."""
+        return max(0, int(self.cursor.item()) - self.num_pages)

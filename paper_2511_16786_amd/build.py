@@ -21,6 +21,10 @@ UNITS = [
     ("resample.hip", "resample.o", []),
     ("dense.hip", "dense.o", []),
     ("decode.hip", "decode.o", []),
+    ("mx_decode.hip", "mx_decode.o", []),
+    ("mx_cache.hip", "mx_cache.o", []),
+    ("pages.hip", "pages.o", []),
+    ("rotary.hip", "rotary.o", []),
     ("select_gather.hip", "select_gather.o", []),
     ("allocate.hip", "allocate.o", []),
     ("api.hip", "api.o", []),

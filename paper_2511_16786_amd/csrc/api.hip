@@ -234,13 +234,13 @@ static fc_status select_gather_common(const void* K, const void* V, const fc_kv_
                                       const int64_t* layer_offsets, int64_t rows_per_seq, bool shared,
                                       int32_t* idx_out, void* K_out, void* V_out,
                                       const int32_t* block_table, int32_t page_size, int32_t max_pages,
-                                      int64_t num_pages, void* hip_stream) {
+                                      int64_t num_pages, void* hip_stream, bool copies = true) {
   fc_status st = check_desc(desc);
   if (st != FC_OK) return st;
   if (rows_per_seq < 0 || rows_per_seq > (int64_t)desc->layers * desc->kv_heads * desc->n_tokens)
     return FC_EINVAL;
   if (desc->batch == 0 || rows_per_seq == 0) return FC_OK;
-  if (!K || !V || !scores || !budgets || !layer_offsets || !idx_out || !K_out || !V_out) return FC_EINVAL;
+  if (!K || !V || !scores || !budgets || !layer_offsets || !idx_out || (copies && (!K_out || !V_out))) return FC_EINVAL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(K_out) || !aligned16(V_out)) return FC_EINVAL;
   if ((reinterpret_cast<uintptr_t>(scores) & 3u) || (reinterpret_cast<uintptr_t>(budgets) & 3u) ||
       (reinterpret_cast<uintptr_t>(idx_out) & 3u) || (reinterpret_cast<uintptr_t>(layer_offsets) & 7u))
@@ -372,6 +372,163 @@ fc_status flashcache_decode_attention_paged(const void* Q, const void* K_pages, 
   hipError_t e = decode_launch(Q, K_pages, V_pages, batch, layers, kv_heads, q_heads / kv_heads, head_dim,
                                dtype, budgets, nullptr, 0, scale, out, workspace, block_table, page_size,
                                max_pages, num_pages, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+static fc_status check_heads(const fc_rotary_plan& plan, const fc_heads_desc& d, const void* in, const void* out) {
+  if (d.batch < 0 || d.tokens < 0 || d.heads < 0 || d.head_dim < 1) return FC_EINVAL;
+  if (d.dtype != FC_F32 && d.dtype != FC_BF16) return FC_EINVAL;
+  if (d.head_dim % 2 || d.head_dim < plan.rotary_dim) return FC_EINVAL;
+  if (d.head_dim > 512) return FC_EUNSUPPORTED;
+  if (d.stride_b < 0 || d.stride_t < 0 || d.stride_h < 0) return FC_EINVAL;
+  if (d.out_stride_b < 0 || d.out_stride_t < 0 || d.out_stride_h < 0) return FC_EINVAL;
+  if ((int64_t)d.batch * d.tokens > 0x7FFFFFFFll || d.heads > 65535) return FC_EUNSUPPORTED;
+  if ((int64_t)d.batch * d.tokens * d.heads == 0) return FC_OK;
+  const uintptr_t e = d.dtype == FC_BF16 ? 2 : 4;
+  if (!in || !out || reinterpret_cast<uintptr_t>(in) % e || reinterpret_cast<uintptr_t>(out) % e) return FC_EINVAL;
+  // rows of the output must not lie on one another
+  if ((d.batch > 1 && d.out_stride_b < d.head_dim) || (d.tokens > 1 && d.out_stride_t < d.head_dim) ||
+      (d.heads > 1 && d.out_stride_h < d.head_dim))
+    return FC_EINVAL;
+  if (in == out && ((d.batch > 1 && d.stride_b != d.out_stride_b) || (d.tokens > 1 && d.stride_t != d.out_stride_t) ||
+                    (d.heads > 1 && d.stride_h != d.out_stride_h)))
+    return FC_EINVAL;
+  return FC_OK;
+}
+
+fc_status flashcache_rotary(const fc_rotary_plan* plan, const int32_t* positions, const void* Q, void* Q_out,
+                            const fc_heads_desc* q_desc, const void* K, void* K_out, const fc_heads_desc* k_desc,
+                            int32_t inverse, void* hip_stream) {
+  if (!plan || !q_desc || plan->magic != kWsMagic) return FC_EINVAL;
+  fc_status st = check_heads(*plan, *q_desc, Q, Q_out);
+  if (st != FC_OK) return st;
+  if (k_desc) {
+    st = check_heads(*plan, *k_desc, K, K_out);
+    if (st != FC_OK) return st;
+    if (k_desc->batch != q_desc->batch || k_desc->tokens != q_desc->tokens || k_desc->head_dim != q_desc->head_dim ||
+        k_desc->dtype != q_desc->dtype)
+      return FC_EINVAL;
+  }
+  const int64_t heads = (int64_t)q_desc->heads + (k_desc ? k_desc->heads : 0);
+  if (heads > 65535) return FC_EUNSUPPORTED;
+  if ((int64_t)q_desc->batch * q_desc->tokens * heads == 0) return FC_OK;
+  if (!positions || (reinterpret_cast<uintptr_t>(positions) & 3u)) return FC_EINVAL;
+  hipError_t e = rotary_launch(*plan, positions, Q, Q_out, *q_desc, K, K_out, k_desc, inverse != 0, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+fc_status flashcache_assign_pages(const int32_t* rows, const int32_t* add, int32_t add_each, int32_t batch, int32_t layers,
+                                  int32_t kv_heads, int32_t page_size, int32_t max_pages, const int32_t* free_pages,
+                                  int64_t num_free, const int64_t* cursor, int32_t* block_table, int64_t* slots,
+                                  int64_t slots_per_seq, int32_t* rows_out, int64_t* cursor_out, void* hip_stream) {
+  if (batch < 0 || layers < 1 || kv_heads < 1 || page_size < 1 || max_pages < 1 || num_free < 0 || slots_per_seq < 0) return FC_EINVAL;
+  if (layers > 1024 || page_size > (1 << 25) || (int64_t)batch * layers * kv_heads > kMaxUnits) return FC_EUNSUPPORTED;
+  if (batch == 0) return FC_OK;
+  if (!rows || !cursor || !block_table || !rows_out || !cursor_out || (slots_per_seq > 0 && !slots)) return FC_EINVAL;
+  auto misaligned = [](const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; };
+  if (misaligned(rows, 4) || misaligned(add, 4) || misaligned(free_pages, 4) || misaligned(block_table, 4) || misaligned(rows_out, 4) ||
+      misaligned(cursor, 8) || misaligned(cursor_out, 8) || misaligned(slots, 8))
+    return FC_EINVAL;
+  hipError_t e = assign_pages_launch(rows, add, add_each, batch, layers, kv_heads, page_size, max_pages, free_pages, num_free, block_table,
+                                     cursor, slots, slots_per_seq, rows_out, cursor_out, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+static fc_status check_mx_pages(int32_t page_size, int32_t head_dim, int64_t num_pages) {
+  if (page_size < 1 || num_pages < 1 || head_dim < 1) return FC_EINVAL;
+  if (head_dim != 64 && head_dim != 128) return FC_EUNSUPPORTED;
+  if (page_size % 16 || page_size > (1 << 25)) return FC_EUNSUPPORTED;
+  if (num_pages > 0x7FFFFFFFll) return FC_EUNSUPPORTED;      // (block tables hold 32 bits)
+  return FC_OK;
+}
+
+size_t flashcache_mx_page_bytes(int32_t page_size, int32_t head_dim) {
+  return check_mx_pages(page_size, head_dim, 1) == FC_OK ? (size_t)(page_size / 16) * 17 * head_dim : 0;
+}
+
+static fc_status check_mx_rows(const fc_rows_desc* d, const void* K, const void* V, const int64_t* slots, const void* pages,
+                               int32_t page_size, int64_t num_pages) {
+  if (!d || d->batch < 0 || d->rows < 0 || d->head_dim < 1) return FC_EINVAL;
+  if (d->dtype != FC_F32 && d->dtype != FC_BF16) return FC_EINVAL;
+  fc_status st = check_mx_pages(page_size, d->head_dim, num_pages);
+  if (st != FC_OK) return st;
+  const int64_t e = d->dtype == FC_BF16 ? 2 : 4;
+  if (d->stride_b < 0 || d->stride_r < 0 || (d->stride_b * e) % 16 || (d->stride_r * e) % 16) return FC_EINVAL;
+  if (d->batch > 65535 || d->rows > 0x7FFFFFFFll) return FC_EUNSUPPORTED;
+  if (d->batch == 0 || d->rows == 0) return FC_OK;
+  if (!K || !V || !slots || !pages) return FC_EINVAL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(pages) || (reinterpret_cast<uintptr_t>(slots) & 7u)) return FC_EINVAL;
+  return FC_OK;
+}
+
+fc_status flashcache_mx_store(const void* K, const void* V, const fc_rows_desc* desc, const int64_t* slots, int32_t page_size,
+                              int64_t num_pages, void* pages, void* hip_stream) {
+  fc_status st = check_mx_rows(desc, K, V, slots, pages, page_size, num_pages);
+  if (st != FC_OK || desc->batch == 0 || desc->rows == 0) return st;
+  hipError_t e = mx_store_launch(K, V, *desc, slots, pages, num_pages * page_size, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+fc_status flashcache_mx_load(const int64_t* slots, const void* pages, int32_t page_size, int64_t num_pages,
+                             const fc_rows_desc* desc, void* K, void* V, void* hip_stream) {
+  fc_status st = check_mx_rows(desc, K, V, slots, pages, page_size, num_pages);
+  if (st != FC_OK || desc->batch == 0 || desc->rows == 0) return st;
+  // rows of the output must not lie on one another
+  if ((desc->rows > 1 && desc->stride_r < desc->head_dim) || (desc->batch > 1 && desc->stride_b < desc->head_dim)) return FC_EINVAL;
+  hipError_t e = mx_load_launch(*desc, slots, pages, num_pages * page_size, K, V, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+fc_status flashcache_select_gather_mx(const void* K, const void* V, const fc_kv_desc* desc, const float* scores,
+                                      const int32_t* budgets, const int64_t* layer_offsets, int64_t rows_per_seq,
+                                      int32_t shared, int32_t* idx_out, const int32_t* block_table, int32_t page_size,
+                                      int32_t max_pages, int64_t num_pages, void* pages, void* hip_stream) {
+  fc_status st = check_desc(desc);
+  if (st != FC_OK) return st;
+  if (max_pages < 1) return FC_EINVAL;
+  st = check_mx_pages(page_size, desc->head_dim, num_pages);
+  if (st != FC_OK) return st;
+  if ((int64_t)desc->kv_heads * desc->n_tokens > 0xFFFFFFFFll || desc->batch > 65535) return FC_EUNSUPPORTED;
+  if (!block_table || (reinterpret_cast<uintptr_t>(block_table) & 3u)) return FC_EINVAL;
+  if (desc->batch > 0 && rows_per_seq > 0 && (!pages || !aligned16(pages))) return FC_EINVAL;
+  st = select_gather_common(K, V, desc, scores, budgets, layer_offsets, rows_per_seq, shared != 0, idx_out, nullptr, nullptr, nullptr, 0, 0,
+                            0, hip_stream, false);
+  if (st != FC_OK || desc->batch == 0 || rows_per_seq == 0) return st;
+  hipError_t e = mx_gather_launch(K, V, *desc, budgets, layer_offsets, rows_per_seq, idx_out, block_table, page_size, max_pages, pages,
+                                  num_pages * page_size, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+static bool mx_decode_shape(int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads) {
+  return batch >= 0 && layers >= 1 && kv_heads >= 1 && q_heads >= kv_heads && q_heads % kv_heads == 0;
+}
+
+size_t flashcache_mx_decode_workspace_bytes(int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads, int32_t head_dim) {
+  if (!mx_decode_shape(batch, layers, kv_heads, q_heads) || !mx_decode_supported(q_heads / kv_heads, head_dim)) return 0;
+  if ((int64_t)batch * layers * kv_heads > kMaxUnits) return 0;
+  return mx_decode_workspace_bytes(batch * layers * kv_heads, q_heads / kv_heads, head_dim);
+}
+
+fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const int32_t* block_table, int32_t page_size,
+                                         int32_t max_pages, int64_t num_pages, int32_t batch, int32_t layers,
+                                         int32_t kv_heads, int32_t q_heads, int32_t head_dim, int32_t dtype,
+                                         const int32_t* rows, float scale, float* out, void* workspace,
+                                         size_t workspace_bytes, void* hip_stream) {
+  if (!mx_decode_shape(batch, layers, kv_heads, q_heads) || head_dim < 1) return FC_EINVAL;
+  if (dtype != FC_F32 && dtype != FC_BF16) return FC_EINVAL;
+  if (max_pages < 1 || !(scale == scale)) return FC_EINVAL;
+  fc_status st = check_mx_pages(page_size, head_dim, num_pages);
+  if (st != FC_OK) return st;
+  if (!mx_decode_supported(q_heads / kv_heads, head_dim)) return FC_EUNSUPPORTED;
+  if ((int64_t)batch * layers * kv_heads > kMaxUnits) return FC_EUNSUPPORTED;
+  if (batch == 0) return FC_OK;
+  if (!Q || !pages || !block_table || !rows || !out) return FC_EINVAL;
+  if (!aligned16(Q) || !aligned16(pages) || !aligned16(out)) return FC_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(rows) & 3u) || (reinterpret_cast<uintptr_t>(block_table) & 3u)) return FC_EINVAL;
+  const size_t need = mx_decode_workspace_bytes(batch * layers * kv_heads, q_heads / kv_heads, head_dim);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < need) return FC_EWORKSPACE;
+  hipError_t e = mx_decode_launch(Q, pages, block_table, page_size, max_pages, num_pages, batch, layers, kv_heads, q_heads / kv_heads,
+                                  head_dim, dtype, rows, scale, out, workspace, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? FC_OK : FC_EHIP;
 }
 

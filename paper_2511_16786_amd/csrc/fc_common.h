@@ -94,6 +94,7 @@ hipError_t energy_reduce_launch(const double* epart, int tiles, int units, doubl
 hipError_t allocate_launch(const double* energy, int32_t B, int32_t L, int32_t H, int32_t N,
                            int64_t T, int32_t b_min, int32_t b_max, int32_t* budgets,
                            int64_t* layer_offsets, hipStream_t s);
+// (K_out = nullptr: the indices alone)
 hipError_t select_gather_launch(const void* K, const void* V, const fc_kv_desc& d,
                                 const float* scores, const int32_t* budgets,
                                 const int64_t* layer_offsets, int64_t rows_per_seq, bool shared,
@@ -108,6 +109,24 @@ hipError_t decode_launch(const void* Q, const void* Kc, const void* Vc, int B, i
                          int dtype, const int32_t* budgets, const int64_t* offs, int64_t rows_per_seq,
                          float scale, float* out, void* ws, const int32_t* block_table, int32_t page_size,
                          int32_t max_pages, int64_t num_pages, hipStream_t s);
+
+hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, const void* Q, void* Q_out, const fc_heads_desc& q,
+                         const void* K, void* K_out, const fc_heads_desc* k, bool inverse, hipStream_t s);
+hipError_t assign_pages_launch(const int32_t* rows, const int32_t* add, int32_t add_each, int B, int L, int H, int page_size,
+                               int max_pages, const int32_t* free_pages, int64_t num_free, int32_t* table, const int64_t* cursor,
+                               int64_t* slots, int64_t slots_per_seq, int32_t* rows_out, int64_t* cursor_out, hipStream_t s);
+hipError_t mx_store_launch(const void* K, const void* V, const fc_rows_desc& r, const int64_t* slots, void* pages, int64_t num_slots,
+                           hipStream_t s);
+hipError_t mx_load_launch(const fc_rows_desc& r, const int64_t* slots, const void* pages, int64_t num_slots, void* K, void* V,
+                          hipStream_t s);
+hipError_t mx_gather_launch(const void* K, const void* V, const fc_kv_desc& d, const int32_t* budgets, const int64_t* offsets,
+                            int64_t rows_per_seq, const int32_t* idx, const int32_t* table, int32_t page_size, int32_t max_pages,
+                            void* pages, int64_t num_slots, hipStream_t s);
+bool mx_decode_supported(int group, int d);
+size_t mx_decode_workspace_bytes(int units, int group, int d);
+hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* table, int page_size, int max_pages, int64_t num_pages,
+                            int B, int L, int H, int group, int d, int dtype, const int32_t* rows, float scale, float* out, void* ws,
+                            hipStream_t s);
 
 // Per-kernel event timing (see profile.hip): brackets the launches made while it is alive.
 bool profiling_on();

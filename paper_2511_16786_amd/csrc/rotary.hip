@@ -1,0 +1,269 @@
+// Rotary positions of the queries and keys that a step or a prompt brings: pair i of a head is turned by the angle
+// position * frequency_i,
+//   y0 = m (x0 cos - x1 sin),  y1 = m (x1 cos + x0 sin)        (transposed: sin -> -sin)
+// where a pair is (x_i, x_{i + R/2}) or (x_2i, x_2i+1) of the first R columns; the other columns are copied.
+//
+// Angles: a frequency is kept as turns per position in units of 2^-64, so that position * frequency is one product of
+// integers whose overflow drops the whole turns: exact to 2^-53 of the frequency for any int32 position, where an angle in
+// fp32 is off by 0.06 rad at position 10^6.  32 bits of the turn are left to an octant and the series of sine and cosine
+// on |theta| <= pi / 4 (terms up to theta^9 and theta^8, whose rest is below 2^-25).
+//
+// Bound by memory: every element is read and written once.  A thread keeps the sines of its pairs and walks over heads, so
+// that what they cost (about 40 operations a pair) is shared by them.
+#include <algorithm>
+#include <math.h>
+#include <string.h>
+
+#include "fc_common.h"
+
+namespace fc {
+
+namespace {
+
+constexpr int kRotThreads = 256;
+
+struct RotSide {                 // Q or K
+  const char* in;
+  char* out;
+  int64_t sb, st, sh, ob, ot, oh;    // strides in bytes
+  int heads;
+};
+struct RotArgs {
+  RotSide q, k;
+  const int32_t* positions;      // [streams][batch * tokens]
+  int tokens, rows;              // tokens of a sequence, of all sequences
+  int half, chunks, turned;      // pairs; chunks of a head; those that are turned
+  int per_group;                 // tokens of a workgroup
+  int heads_at_once;             // heads of a thread
+  int streams, end0, end1, end2; // first pair behind the first, second and third stream
+  float magnitude, sign;
+};
+
+template <int BYTES> struct Bytes;
+template <> struct Bytes<2> { typedef uint16_t type; };
+template <> struct Bytes<4> { typedef uint32_t type; };
+template <> struct Bytes<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Bytes<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Bytes<32> { struct type { Bytes<16>::type a, b; }; };
+
+template <typename T, int N> struct Vec {
+  typename Bytes<N * (int)sizeof(T)>::type raw;
+};
+template <typename T, int N> __device__ __forceinline__ void widen(const Vec<T, N>& v, float (&o)[N]) {
+  if constexpr (sizeof(T) == 4) {
+    struct F { float f[N]; };
+    const F f = __builtin_bit_cast(F, v.raw);
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = f.f[i];
+  } else {
+    struct H { uint16_t h[N]; };
+    const H h = __builtin_bit_cast(H, v.raw);
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = bf16_to_f32(h.h[i]);
+  }
+}
+template <typename T, int N> __device__ __forceinline__ Vec<T, N> narrow(const float (&x)[N]) {
+  Vec<T, N> v;
+  if constexpr (sizeof(T) == 4) {
+    struct F { float f[N]; } f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) f.f[i] = x[i];
+    v.raw = __builtin_bit_cast(decltype(v.raw), f);
+  } else {                                                 // (the one rounding: to nearest)
+    struct H { __bf16 h[N]; } h;
+#pragma unroll
+    for (int i = 0; i < N; ++i) h.h[i] = (__bf16)x[i];
+    v.raw = __builtin_bit_cast(decltype(v.raw), h);
+  }
+  return v;
+}
+
+// Sine and cosine of `turns` 2^-32 of a whole turn.
+__device__ __forceinline__ void sine_cosine(uint32_t turns, float& s, float& c) {
+  const uint32_t quarter = (turns + 0x20000000u) >> 30;
+  const float t = (float)(int32_t)(turns - (quarter << 30)) * 1.4629180792671596e-9f;      // 2 pi / 2^32
+  const float u = t * t;
+  const float a = t * fmaf(u, fmaf(u, fmaf(u, fmaf(u, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), 1.f);
+  const float b = fmaf(u, fmaf(u, fmaf(u, fmaf(u, 1.f / 40320, -1.f / 720), 1.f / 24), -0.5f), 1.f);
+  const float x = quarter & 1 ? b : a, y = quarter & 1 ? a : b;
+  s = quarter & 2 ? -x : x;
+  c = (quarter + 1) & 2 ? -y : y;
+}
+
+// P pairs a thread and head; a chunk behind the turned ones is 2 P columns to be copied.
+template <typename T, int P, bool INTERLEAVED>
+__global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc_rotary_plan plan) {
+  const int chunk = (int)(threadIdx.x % (unsigned)a.chunks), own = (int)(threadIdx.x / (unsigned)a.chunks);
+  const int64_t row64 = (int64_t)blockIdx.x * a.per_group + own;
+  if (own >= a.per_group || row64 >= a.rows) return;
+  const int row = (int)row64, b = row / a.tokens, t = row - b * a.tokens;
+  const bool turned = chunk < a.turned;
+  float sn[P], cs[P];
+  int at0, at1;                                            // columns of the chunk's two parts
+  if (turned) {
+    const int first = chunk * P;
+    at0 = INTERLEAVED ? 2 * first : first;
+    at1 = INTERLEAVED ? at0 + P : first + a.half;
+    int64_t where[4];
+    where[0] = a.positions[row];
+    for (int k = 1; k < 4; ++k) where[k] = k < a.streams ? a.positions[(int64_t)k * a.rows + row] : where[0];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int pair = first + i;
+      const int64_t pos = pair < a.end0 ? where[0] : pair < a.end1 ? where[1] : pair < a.end2 ? where[2] : where[3];
+      const uint64_t whole = (uint64_t)pos * plan.turns[pair];
+      sine_cosine((uint32_t)((whole + 0x80000000ull) >> 32), sn[i], cs[i]);
+      sn[i] *= a.magnitude * a.sign;
+      cs[i] *= a.magnitude;
+    }
+  } else {
+    at0 = 2 * a.half + (chunk - a.turned) * 2 * P;
+    at1 = at0 + P;
+  }
+  const int heads = a.q.heads + a.k.heads, h1 = min(heads, (int)(blockIdx.y + 1) * a.heads_at_once);
+#pragma unroll 2
+  for (int h = (int)blockIdx.y * a.heads_at_once; h < h1; ++h) {
+    const bool is_q = h < a.q.heads;
+    const int hh = is_q ? h : h - a.q.heads;
+    const char* in = (is_q ? a.q.in : a.k.in) + b * (is_q ? a.q.sb : a.k.sb) + t * (is_q ? a.q.st : a.k.st) + hh * (is_q ? a.q.sh : a.k.sh);
+    char* out = (is_q ? a.q.out : a.k.out) + b * (is_q ? a.q.ob : a.k.ob) + t * (is_q ? a.q.ot : a.k.ot) + hh * (is_q ? a.q.oh : a.k.oh);
+    const Vec<T, P> v0 = *reinterpret_cast<const Vec<T, P>*>(in + at0 * (int)sizeof(T));
+    const Vec<T, P> v1 = *reinterpret_cast<const Vec<T, P>*>(in + at1 * (int)sizeof(T));
+    if (!turned) {
+      *reinterpret_cast<Vec<T, P>*>(out + at0 * (int)sizeof(T)) = v0;
+      *reinterpret_cast<Vec<T, P>*>(out + at1 * (int)sizeof(T)) = v1;
+      continue;
+    }
+    float x[2 * P], y[2 * P], lo[P], hi[P];
+    widen<T, P>(v0, lo);
+    widen<T, P>(v1, hi);
+#pragma unroll
+    for (int i = 0; i < P; ++i) { x[i] = lo[i]; x[P + i] = hi[i]; }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int p = INTERLEAVED ? 2 * i : i, q = INTERLEAVED ? 2 * i + 1 : P + i;
+      y[p] = x[p] * cs[i] - x[q] * sn[i];
+      y[q] = x[q] * cs[i] + x[p] * sn[i];
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) { lo[i] = y[i]; hi[i] = y[P + i]; }
+    *reinterpret_cast<Vec<T, P>*>(out + at0 * (int)sizeof(T)) = narrow<T, P>(lo);
+    *reinterpret_cast<Vec<T, P>*>(out + at1 * (int)sizeof(T)) = narrow<T, P>(hi);
+  }
+}
+
+}  // namespace
+
+hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, const void* Q, void* Q_out, const fc_heads_desc& q,
+                         const void* K, void* K_out, const fc_heads_desc* k, bool inverse, hipStream_t s) {
+  const int e = q.dtype == FC_BF16 ? 2 : 4, half = plan.rotary_dim / 2, rest = q.head_dim - plan.rotary_dim;
+  auto side = [&](const void* in, void* out, const fc_heads_desc& d) {
+    return RotSide{static_cast<const char*>(in), static_cast<char*>(out), d.stride_b * e, d.stride_t * e, d.stride_h * e,
+                   d.out_stride_b * e, d.out_stride_t * e, d.out_stride_h * e, d.heads};
+  };
+  RotArgs a{};
+  a.q = side(Q, Q_out, q);
+  a.k = k ? side(K, K_out, *k) : RotSide{};
+  // the widest parts that every address is a multiple of
+  uint64_t bits = 0;
+  for (const RotSide* r : {&a.q, &a.k})
+    bits |= (uint64_t)(uintptr_t)r->in | (uint64_t)(uintptr_t)r->out | (uint64_t)(r->sb | r->st | r->sh | r->ob | r->ot | r->oh);
+  int pairs = 8;
+  while (pairs > 1 && (half % pairs || rest % (2 * pairs) || (bits & (uint64_t)(std::min(16, pairs * e) - 1)))) pairs /= 2;
+  a.positions = positions;
+  a.tokens = q.tokens;
+  a.rows = q.batch * q.tokens;
+  a.half = half;
+  a.turned = half / pairs;
+  a.chunks = a.turned + rest / (2 * pairs);
+  a.per_group = kRotThreads / a.chunks;
+  a.streams = plan.streams;
+  a.end0 = plan.stream_end[0];
+  a.end1 = plan.stream_end[1];
+  a.end2 = plan.stream_end[2];
+  a.magnitude = plan.magnitude;
+  a.sign = inverse ? -1.f : 1.f;
+  const int64_t groups = ((int64_t)a.rows + a.per_group - 1) / a.per_group;
+  const int heads = a.q.heads + a.k.heads;
+  a.heads_at_once = (int)std::min<int64_t>(heads, std::max<int64_t>(1, groups * heads / 2048));
+  const dim3 grid((unsigned)groups, (unsigned)((heads + a.heads_at_once - 1) / a.heads_at_once));
+  ProfileScope ps("rotary_kernel", s);
+  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a, plan); };
+#define FC_ROTARY(T, P) plan.interleaved ? launch(rotary_kernel<T, P, true>) : launch(rotary_kernel<T, P, false>)
+  if (q.dtype == FC_BF16) {
+    if (pairs == 8) FC_ROTARY(uint16_t, 8);
+    else if (pairs == 4) FC_ROTARY(uint16_t, 4);
+    else if (pairs == 2) FC_ROTARY(uint16_t, 2);
+    else FC_ROTARY(uint16_t, 1);
+  } else {
+    if (pairs == 8) FC_ROTARY(float, 8);
+    else if (pairs == 4) FC_ROTARY(float, 4);
+    else if (pairs == 2) FC_ROTARY(float, 2);
+    else FC_ROTARY(float, 1);
+  }
+#undef FC_ROTARY
+  return hipGetLastError();
+}
+
+}  // namespace fc
+
+using namespace fc;
+
+extern "C" {
+
+// Host only.  Frequencies f_i = theta^(-2i / R), rescaled for contexts longer than the one trained on:
+//   linear  f_i / s
+//   base    theta * s^(R / (R - 2)) in place of theta
+//   parts   a pair that makes n turns over the original context keeps f_i if n >= beta_fast, takes f_i / s if n <= beta_slow and a
+//           mixture linear in n between; magnitude 0.1 ln s + 1
+fc_status flashcache_rotary_prepare(const fc_rotary_spec* spec, const double* frequencies, fc_rotary_plan* plan) {
+  if (!spec || !plan) return FC_EINVAL;
+  const int R = spec->rotary_dim;
+  if (R < 2 || R % 2) return FC_EINVAL;
+  if (R > 2 * FC_ROTARY_MAX_PAIRS) return FC_EUNSUPPORTED;
+  if (spec->streams < 1 || spec->streams > 4) return FC_EINVAL;
+  if (spec->scaling < FC_ROTARY_PLAIN || spec->scaling > FC_ROTARY_PARTS) return FC_EINVAL;
+  if (!frequencies && !(spec->theta > 0.0 && isfinite(spec->theta))) return FC_EINVAL;
+  const bool scaled = !frequencies && spec->scaling != FC_ROTARY_PLAIN;
+  if (scaled && !(spec->factor >= 1.0 && isfinite(spec->factor))) return FC_EINVAL;
+  const bool parts = scaled && spec->scaling == FC_ROTARY_PARTS;
+  if (parts && (spec->original_tokens < 1 || !(spec->beta_fast > spec->beta_slow) || !isfinite(spec->beta_fast) || !isfinite(spec->beta_slow)))
+    return FC_EINVAL;
+  if (!(spec->magnitude >= 0.0 && isfinite(spec->magnitude))) return FC_EINVAL;
+  fc_rotary_plan p;
+  memset(&p, 0, sizeof(p));
+  p.rotary_dim = R;
+  p.interleaved = spec->interleaved != 0;
+  p.streams = spec->streams;
+  int end = 0;
+  for (int k = 0; k < 4; ++k) {
+    if (k < spec->streams) {
+      const int n = spec->streams == 1 ? R / 2 : spec->stream_pairs[k];
+      if (n < 0 || n > R / 2) return FC_EINVAL;
+      end += n;
+    }
+    p.stream_end[k] = k < spec->streams - 1 ? end : R / 2;
+  }
+  if (end != R / 2) return FC_EINVAL;
+  const double pi = 3.14159265358979323846, s = scaled ? spec->factor : 1.0;
+  p.magnitude = (float)(spec->magnitude > 0.0 ? spec->magnitude : parts ? 0.1 * log(s) + 1.0 : 1.0);
+  const double theta = scaled && spec->scaling == FC_ROTARY_BASE && R > 2 ? spec->theta * pow(s, (double)R / (R - 2)) : spec->theta;
+  for (int i = 0; i < R / 2; ++i) {
+    double f = frequencies ? frequencies[i] : pow(theta, -2.0 * i / R);
+    if (!isfinite(f)) return FC_EINVAL;
+    if (scaled && spec->scaling == FC_ROTARY_LINEAR) f /= s;
+    if (parts) {
+      const double n = spec->original_tokens * f / (2.0 * pi);
+      const double keep = fmin(1.0, fmax(0.0, (n - spec->beta_slow) / (spec->beta_fast - spec->beta_slow)));
+      f = f * keep + f / s * (1.0 - keep);
+    }
+    const double turns = f / (2.0 * pi), part = turns - floor(turns);      // (whole turns a position change nothing)
+    const double units = ldexp(part, 64);
+    p.turns[i] = units >= 18446744073709551616.0 ? 0u : (uint64_t)units;
+  }
+  p.magic = kWsMagic;
+  *plan = p;
+  return FC_OK;
+}
+
+}  // extern "C"

@@ -516,7 +516,7 @@ hipError_t select_gather_launch(const void* K, const void* V, const fc_kv_desc& 
     for (vpr_shift = 0; (1 << vpr_shift) < vec_per_row; ++vpr_shift) {}
   const PagedDst pg{block_table, page_size, max_pages, (long long)num_pages};
   const int lists = shared ? units / d.kv_heads : units;           // index sets to be found
-  const int groups = copy_groups(lists, d.layers, d.n_tokens, shared ? d.kv_heads : 1, (long long)rows_per_seq * d.batch, vec_per_row,
+  const int groups = !K_out ? 0 : copy_groups(lists, d.layers, d.n_tokens, shared ? d.kv_heads : 1, (long long)rows_per_seq * d.batch, vec_per_row,
                                  block_table != nullptr);
   {
     ProfileScope ps(shared ? "select_shared_kernel" : "select_kernel", s);
@@ -561,7 +561,7 @@ hipError_t select_gather_launch(const void* K, const void* V, const fc_kv_desc& 
     }
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || groups) return e;
+  if (e != hipSuccess || groups || !K_out) return e;
   // rows of a workgroup: one turn of its threads' copies, if it has a thread for each of them
   const int rows = std::min(kGatherThreads, std::max(1, kGatherThreads / vec_per_row));
   const long long blocks = (rows_per_seq + rows - 1) / rows;
