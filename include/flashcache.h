@@ -388,7 +388,7 @@ fc_status flashcache_select_gather_mx(const void* K, const void* V, const fc_kv_
  *   rows  device in, int32 [B][L].  Rows whose page entry is missing (negative, >= num_pages, from max_pages on) are not attended to; a unit
  *         without attended rows gives zeros
  *   workspace  device, 16-byte aligned, flashcache_mx_decode_workspace_bytes() bytes; calls that may run at the same time need one each
- * 1 to 16 query heads a KV head for both dtypes.  Products of the cache's values (exact in bf16) on the matrix cores with queries and
+ * 1 to 16 query heads a KV head for both dtypes; tables that reach 2^36 rows in all of their units are refused (FC_EUNSUPPORTED).  Products of the cache's values (exact in bf16) on the matrix cores with queries and
  * probabilities of 24 bits, sums and softmax in fp32. */
 size_t flashcache_mx_decode_workspace_bytes(int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads, int32_t head_dim);
 fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const int32_t* block_table, int32_t page_size,

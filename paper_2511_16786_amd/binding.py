@@ -7,6 +7,7 @@ library has not been built, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -363,17 +364,18 @@ def _dtype(t: torch.Tensor) -> int:
     raise ValueError(f"unsupported dtype {t.dtype}")
 
 
-def _want(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape: Tuple[int, ...], device: torch.device) -> None:
-    """A contiguous tensor of this type, shape and device, or nothing at all."""
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous()):
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+def _want(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape: Tuple[int, ...], index: int) -> None:
+    """A contiguous tensor of this type and shape on GPU `index`, or nothing at all."""
+    if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {index}")
 
 
-def _here(t: torch.Tensor, what: str) -> torch.device:
-    """The tensor's device, which has to be the current one: that is the device whose current stream the call goes to."""
-    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+def _here(t: torch.Tensor, what: str) -> int:
+    """Index of the tensor's GPU, which has to be the current one: that is the device whose current stream the call goes to."""
+    index = t.get_device()
+    if index < 0 or index != torch._C._cuda_getDevice():
         raise ValueError(f"{what} must be on the current GPU")
-    return t.device
+    return index
 
 
 def rotary_plan(rotary_dim: int, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none",
@@ -405,13 +407,14 @@ def rotary_plan(rotary_dim: int, theta: float = 10000.0, interleaved: bool = Fal
     return plan
 
 
-def _heads(x: torch.Tensor, out: torch.Tensor, what: str) -> FcHeadsDesc:
+def _heads(x: torch.Tensor, out: torch.Tensor, what: str, index: int) -> FcHeadsDesc:
+    if out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index or x.get_device() != index:
+        raise ValueError(f"{what} and its output must agree in shape and dtype and be on GPU {index}")
     B, T, H, d = x.shape
-    if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
-        raise ValueError(f"{what} and its output must agree in shape, dtype and device")
-    if (x.stride(3) != 1 or out.stride(3) != 1) and d > 1:
+    (sb, st, sh, sd), (ob, ot, oh, od) = x.stride(), out.stride()
+    if (sd != 1 or od != 1) and d > 1:
         raise ValueError("the head dimension must be contiguous")
-    return FcHeadsDesc(B, T, H, d, _dtype(x), 0, x.stride(0), x.stride(1), x.stride(2), out.stride(0), out.stride(1), out.stride(2))
+    return FcHeadsDesc(B, T, H, d, _dtype(x), 0, sb, st, sh, ob, ot, oh)
 
 
 def rotary(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K: Optional[torch.Tensor] = None,
@@ -420,21 +423,25 @@ def rotary(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K: Opti
     """Rotary positions of Q [B, T, Hq, d] and K [B, T, Hk, d] (any strides, innermost contiguous); positions int32
     [B, T], or [streams, B, T].  Q_out / K_out may be Q and K themselves; without them new tensors are returned.
     inverse: the transposed map, which takes gradients of the outputs to gradients of the inputs."""
-    if Q.dim() != 4 or (K is not None and (K.dim() != 4 or K.shape[:2] != Q.shape[:2] or K.device != Q.device)):
+    index = _here(Q, "Q")
+    if Q.dim() != 4 or (K is not None and (K.dim() != 4 or K.shape[:2] != Q.shape[:2])):
         raise ValueError("Q and K must have shape [B, T, H, d], with B and T in common")
-    _here(Q, "Q")
-    shape = tuple(Q.shape[:2]) if plan.streams == 1 and positions.dim() == 2 else (plan.streams, *Q.shape[:2])
-    _want(positions, "positions", torch.int32, shape, Q.device)
+    if plan.streams == 1 and positions.dim() == 2:
+        _want(positions, "positions", torch.int32, Q.shape[:2], index)
+    else:
+        _want(positions, "positions", torch.int32, (plan.streams, *Q.shape[:2]), index)
     if Q_out is None:
         Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-    if K is not None and K_out is None:
-        K_out = torch.empty(K.shape, dtype=K.dtype, device=K.device)
-    qd = _heads(Q, Q_out, "Q")
-    kd = None if K is None else _heads(K, K_out, "K")
-    _check(_lib.flashcache_rotary(ctypes.byref(plan), _ptr(positions), _ptr(Q), _ptr(Q_out), ctypes.byref(qd), _ptr(K),
-                                  None if K is None else _ptr(K_out), None if kd is None else ctypes.byref(kd),
-                                  1 if inverse else 0, _stream()), "flashcache_rotary")
-    return Q_out, (None if K is None else K_out)
+    qd = _heads(Q, Q_out, "Q", index)
+    if K is None:
+        K_ptr = Ko_ptr = kd_ref = K_out = None
+    else:
+        if K_out is None:
+            K_out = torch.empty(K.shape, dtype=K.dtype, device=K.device)
+        K_ptr, Ko_ptr, kd_ref = K.data_ptr(), K_out.data_ptr(), ctypes.byref(_heads(K, K_out, "K", index))
+    _check(_lib.flashcache_rotary(ctypes.byref(plan), positions.data_ptr(), Q.data_ptr(), Q_out.data_ptr(), ctypes.byref(qd),
+                                  K_ptr, Ko_ptr, kd_ref, 1 if inverse else 0, _stream()), "flashcache_rotary")
+    return Q_out, K_out
 
 
 def assign_pages(rows: torch.Tensor, add, page_size: int, block_table: torch.Tensor, cursor: torch.Tensor,
@@ -447,77 +454,105 @@ def assign_pages(rows: torch.Tensor, add, page_size: int, block_table: torch.Ten
     if block_table.dim() != 4:
         raise ValueError("block_table must have shape [B, L, H, max_pages]")
     B, L, H, most = block_table.shape
-    dev = _here(block_table, "block_table")
-    _want(block_table, "block_table", torch.int32, (B, L, H, most), dev)
-    each = 0 if isinstance(add, torch.Tensor) else int(add)
-    for t, what in ((rows, "rows"), (rows_out, "rows_out"), (add if isinstance(add, torch.Tensor) else None, "add")):
-        _want(t, what, torch.int32, (B, L), dev)
-    for t, what in ((cursor, "cursor"), (cursor_out, "cursor_out")):
-        _want(t, what, torch.int64, (1,), dev)
+    index = _here(block_table, "block_table")
+    _want(block_table, "block_table", torch.int32, (B, L, H, most), index)
+    each, add_ptr = 0, None
+    if isinstance(add, torch.Tensor):
+        _want(add, "add", torch.int32, (B, L), index)
+        add_ptr = add.data_ptr()
+    else:
+        each = int(add)
+    rows_out = rows if rows_out is None else rows_out
+    cursor_out = cursor if cursor_out is None else cursor_out
+    _want(rows, "rows", torch.int32, (B, L), index)
+    _want(rows_out, "rows_out", torch.int32, (B, L), index)
+    _want(cursor, "cursor", torch.int64, (1,), index)
+    _want(cursor_out, "cursor_out", torch.int64, (1,), index)
     if free_pages is None and num_free is None:
         raise ValueError("either free_pages or num_free")
     if free_pages is not None:
-        _want(free_pages, "free_pages", torch.int32, (free_pages.numel(),), dev)
-        num_free = free_pages.numel() if num_free is None else num_free
-        if num_free > free_pages.numel():
+        count = free_pages.numel()
+        _want(free_pages, "free_pages", torch.int32, (count,), index)
+        num_free = count if num_free is None else num_free
+        if num_free > count:
             raise ValueError("num_free exceeds the list")
+    per_seq = 0
     if slots is not None:
-        _want(slots, "slots", torch.int64, (B, slots.numel() // max(B, 1)), dev)
+        per_seq = slots.numel() // max(B, 1)
+        _want(slots, "slots", torch.int64, (B, per_seq), index)
     _check(_lib.flashcache_assign_pages(
-        _ptr(rows), _ptr(add) if isinstance(add, torch.Tensor) else None, each, B, L, H, page_size, most, _ptr(free_pages),
-        num_free, _ptr(cursor), _ptr(block_table), _ptr(slots), 0 if slots is None else slots.numel() // max(B, 1),
-        _ptr(rows if rows_out is None else rows_out), _ptr(cursor if cursor_out is None else cursor_out), _stream()),
+        rows.data_ptr(), add_ptr, each, B, L, H, page_size, most, _ptr(free_pages), num_free, cursor.data_ptr(),
+        block_table.data_ptr(), _ptr(slots), per_seq, rows_out.data_ptr(), cursor_out.data_ptr(), _stream()),
         "flashcache_assign_pages")
 
 
+@functools.lru_cache(maxsize=None)
 def mx_page_bytes(page_size: int, head_dim: int) -> int:
     """Bytes of a page of the 4-bit cache, K and V; 0 if unsupported."""
     return int(_lib.flashcache_mx_page_bytes(page_size, head_dim))
 
 
-def _mx_pages(pages: torch.Tensor, page_size: int, head_dim: int, device: torch.device) -> int:
+def _mx_pages(pages: torch.Tensor, page_size: int, head_dim: int, index: int) -> int:
     nbytes = mx_page_bytes(page_size, head_dim)
     if nbytes == 0:
         raise FlashCacheError(FC_EUNSUPPORTED, "flashcache_mx_page_bytes")
-    _want(pages, "pages", torch.uint8, (pages.shape[0], nbytes), device)
-    return pages.shape[0]
+    n = pages.shape[0]
+    _want(pages, "pages", torch.uint8, (n, nbytes), index)
+    return n
 
 
-def _mx_rows(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor) -> FcRowsDesc:
-    if K.dim() != 3 or K.shape != V.shape or K.stride() != V.stride() or K.dtype != V.dtype or K.device != V.device:
+def _mx_rows(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, index: int) -> FcRowsDesc:
+    strides = K.stride()
+    if K.dim() != 3 or K.shape != V.shape or strides != V.stride() or K.dtype is not V.dtype or V.get_device() != index:
         raise ValueError("K and V must have shape [B, R, d], the same strides, dtype and device")
     B, R, d = K.shape
-    if K.stride(2) != 1:
+    if strides[2] != 1:
         raise ValueError("the head dimension must be contiguous")
-    _want(slots, "slots", torch.int64, (B, R), _here(K, "K"))
-    return FcRowsDesc(B, d, _dtype(K), 0, R, K.stride(0), K.stride(1))
+    _want(slots, "slots", torch.int64, (B, R), index)
+    return FcRowsDesc(B, d, _dtype(K), 0, R, strides[0], strides[1])
 
 
 def mx_store(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, page_size: int) -> None:
     """Rows K, V [B, R, d] into slots int64 [B, R] (negative: left out) of pages uint8 [num_pages, mx_page_bytes]."""
-    desc = _mx_rows(K, V, slots)
-    n = _mx_pages(pages, page_size, K.shape[2], K.device)
-    _check(_lib.flashcache_mx_store(_ptr(K), _ptr(V), ctypes.byref(desc), _ptr(slots), page_size, n, _ptr(pages), _stream()),
-           "flashcache_mx_store")
+    index = _here(K, "K")
+    desc = _mx_rows(K, V, slots, index)
+    n = _mx_pages(pages, page_size, desc.head_dim, index)
+    _check(_lib.flashcache_mx_store(K.data_ptr(), V.data_ptr(), ctypes.byref(desc), slots.data_ptr(), page_size, n,
+                                    pages.data_ptr(), _stream()), "flashcache_mx_store")
 
 
 def mx_load(slots: torch.Tensor, pages: torch.Tensor, page_size: int, K_out: torch.Tensor, V_out: torch.Tensor) -> None:
     """Rows of the slots int64 [B, R] into K_out, V_out [B, R, d] (bf16 or fp32, both exact); zeros without a slot."""
-    desc = _mx_rows(K_out, V_out, slots)
-    n = _mx_pages(pages, page_size, K_out.shape[2], K_out.device)
-    _check(_lib.flashcache_mx_load(_ptr(slots), _ptr(pages), page_size, n, ctypes.byref(desc), _ptr(K_out), _ptr(V_out), _stream()),
-           "flashcache_mx_load")
+    index = _here(K_out, "K_out")
+    desc = _mx_rows(K_out, V_out, slots, index)
+    n = _mx_pages(pages, page_size, desc.head_dim, index)
+    _check(_lib.flashcache_mx_load(slots.data_ptr(), pages.data_ptr(), page_size, n, ctypes.byref(desc), K_out.data_ptr(),
+                                   V_out.data_ptr(), _stream()), "flashcache_mx_load")
 
 
 def select_gather_mx(K: torch.Tensor, V: torch.Tensor, desc: FcKvDesc, scores: torch.Tensor, budgets: torch.Tensor,
                      layer_offsets: torch.Tensor, rows_per_seq: int, idx_out: torch.Tensor, block_table: torch.Tensor,
                      page_size: int, pages: torch.Tensor, shared: bool = False) -> None:
     """select_gather_paged into a 4-bit cache: pages uint8 [num_pages, mx_page_bytes]."""
-    n = _mx_pages(pages, page_size, desc.head_dim, _here(K, "K"))
+    index = _here(K, "K")
+    n = _mx_pages(pages, page_size, desc.head_dim, index)
+    B, L, H, N = desc.batch, desc.layers, desc.kv_heads, desc.n_tokens
+    if V.shape != K.shape or V.stride() != K.stride() or V.dtype is not K.dtype or V.get_device() != index:
+        raise ValueError("K and V must agree in shape, strides, dtype and device")
+    _want(scores, "scores", torch.float32, (B, L, H, N), index)
+    _want(budgets, "budgets", torch.int32, (B, L), index)
+    _want(layer_offsets, "layer_offsets", torch.int64, (B, L + 1), index)
+    _want(idx_out, "idx_out", torch.int32, (B, rows_per_seq), index)
+    _want(block_table, "block_table", torch.int32, (B, L, H, block_table.shape[-1]), index)
     _check(_lib.flashcache_select_gather_mx(
         _ptr(K), _ptr(V), ctypes.byref(desc), _ptr(scores), _ptr(budgets), _ptr(layer_offsets), rows_per_seq,
         1 if shared else 0, _ptr(idx_out), _ptr(block_table), page_size, block_table.shape[-1], n, _ptr(pages), _stream()),
         "flashcache_select_gather_mx")
+
+
+@functools.lru_cache(maxsize=256)
+def _mx_decode_workspace(batch: int, layers: int, kv_heads: int, q_heads: int, head_dim: int) -> int:
+    return int(_lib.flashcache_mx_decode_workspace_bytes(batch, layers, kv_heads, q_heads, head_dim))
 
 
 def mx_decode_attention(Q: torch.Tensor, pages: torch.Tensor, page_size: int, kv_heads: int, rows: torch.Tensor,
@@ -525,21 +560,25 @@ def mx_decode_attention(Q: torch.Tensor, pages: torch.Tensor, page_size: int, kv
                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Q [B, L, Hq, d]; pages uint8 [num_pages, mx_page_bytes]; rows int32 [B, L]; block_table int32
     [B, L, H, max_pages]; returns float32 [B, L, Hq, d]."""
-    B, L, Hq, d = Q.shape
-    dev = _here(Q, "Q")
-    n = _mx_pages(pages, page_size, d, dev)
-    _want(Q, "Q", Q.dtype, (B, L, Hq, d), dev)
-    _want(rows, "rows", torch.int32, (B, L), dev)
-    _want(block_table, "block_table", torch.int32, (B, L, kv_heads, block_table.shape[-1]), dev)
+    shape = Q.shape
+    B, L, Hq, d = shape
+    index = _here(Q, "Q")
+    n = _mx_pages(pages, page_size, d, index)
+    most = block_table.shape[-1]
+    _want(Q, "Q", Q.dtype, shape, index)
+    _want(rows, "rows", torch.int32, (B, L), index)
+    _want(block_table, "block_table", torch.int32, (B, L, kv_heads, most), index)
     if workspace is None:
-        need = int(_lib.flashcache_mx_decode_workspace_bytes(B, L, kv_heads, Hq, d))
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(_mx_decode_workspace(B, L, kv_heads, Hq, d), 16), dtype=torch.uint8, device=Q.device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on GPU {index}")
     if out is None:
-        out = torch.empty((B, L, Hq, d), dtype=torch.float32, device=dev)
-    _want(out, "out", torch.float32, (B, L, Hq, d), dev)
+        out = torch.empty(shape, dtype=torch.float32, device=Q.device)
+    else:
+        _want(out, "out", torch.float32, shape, index)
     _check(_lib.flashcache_mx_decode_attention(
-        _ptr(Q), _ptr(pages), _ptr(block_table), page_size, block_table.shape[-1], n, B, L, kv_heads, Hq, d, _dtype(Q),
-        _ptr(rows), scale, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()),
+        Q.data_ptr(), pages.data_ptr(), block_table.data_ptr(), page_size, most, n, B, L, kv_heads, Hq, d, _dtype(Q),
+        rows.data_ptr(), scale, out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()),
         "flashcache_mx_decode_attention")
     return out
 
@@ -650,8 +689,7 @@ class MxCache:
         """q [B, L, Hq, d]; float32 [B, L, Hq, d]."""
         B, L, H, d = self.shape
         if self.workspace is None:
-            need = int(_lib.flashcache_mx_decode_workspace_bytes(B, L, H, q.shape[2], d))
-            self.workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+            self.workspace = torch.empty(max(_mx_decode_workspace(B, L, H, q.shape[2], d), 16), dtype=torch.uint8, device=q.device)
         return mx_decode_attention(q, self.pages, self.page_size, H, self.rows, self.block_table, scale, out=out,
                                    workspace=self.workspace)
 

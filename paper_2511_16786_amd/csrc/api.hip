@@ -438,7 +438,7 @@ static fc_status check_mx_pages(int32_t page_size, int32_t head_dim, int64_t num
   if (page_size < 1 || num_pages < 1 || head_dim < 1) return FC_EINVAL;
   if (head_dim != 64 && head_dim != 128) return FC_EUNSUPPORTED;
   if (page_size % 16 || page_size > (1 << 25)) return FC_EUNSUPPORTED;
-  if (num_pages > 0x7FFFFFFFll) return FC_EUNSUPPORTED;      // (block tables hold 32 bits)
+  if (num_pages * (page_size / 16) > 0x7FFFFFFFll) return FC_EUNSUPPORTED;      // (2 TB and more)
   return FC_OK;
 }
 
@@ -521,6 +521,7 @@ fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const
   if (st != FC_OK) return st;
   if (!mx_decode_supported(q_heads / kv_heads, head_dim)) return FC_EUNSUPPORTED;
   if ((int64_t)batch * layers * kv_heads > kMaxUnits) return FC_EUNSUPPORTED;
+  if (!mx_decode_reach((int64_t)batch * layers * kv_heads, max_pages, page_size)) return FC_EUNSUPPORTED;
   if (batch == 0) return FC_OK;
   if (!Q || !pages || !block_table || !rows || !out) return FC_EINVAL;
   if (!aligned16(Q) || !aligned16(pages) || !aligned16(out)) return FC_EINVAL;

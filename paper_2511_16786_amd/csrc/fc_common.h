@@ -123,6 +123,7 @@ hipError_t mx_gather_launch(const void* K, const void* V, const fc_kv_desc& d, c
                             int64_t rows_per_seq, const int32_t* idx, const int32_t* table, int32_t page_size, int32_t max_pages,
                             void* pages, int64_t num_slots, hipStream_t s);
 bool mx_decode_supported(int group, int d);
+bool mx_decode_reach(int64_t units, int64_t max_pages, int64_t page_size);
 size_t mx_decode_workspace_bytes(int units, int group, int d);
 hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* table, int page_size, int max_pages, int64_t num_pages,
                             int B, int L, int H, int group, int d, int dtype, const int32_t* rows, float scale, float* out, void* ws,

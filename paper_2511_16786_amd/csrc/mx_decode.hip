@@ -8,11 +8,12 @@
 //   output:  A = probabilities (head c16, rows 4 g4 + i of both tiles of a step: as the scores come out), B = V (the same rows, column
 //            D / 16 c16 + t for output tile t).  Probabilities are three bf16 terms, 24 bits: with two the result is off by 1e-6.
 //
-// Work is shared out by steps of 32 rows over all units at once: workgroup w has steps S w / W .. S (w + 1) / W of the launch's S, whichever
-// units they belong to, so that no workgroup waits for a long layer.  Budgets are on the device; every wave sums them up by itself.  A unit
-// that lies in one workgroup is finished there, the others' pieces (running maximum, sum, weighted V) are merged by a second kernel: piece
-// w + u of the workspace, no two alike since both only grow along the steps.
+// Work is shared out by steps of 32 rows over all units at once: every wave has an equal run of the launch's steps, whichever units they belong
+// to, so that none waits for a long layer.  Budgets are on the device; every wave sums them up by itself.  A unit within a wave's run is
+// finished there; parts of units (reference, sum, weighted V) meet in LDS once all waves of a workgroup are through, and what belongs to
+// units of several workgroups is merged by a second kernel: piece w + u of the workspace, no two alike since both only grow along the steps.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "fc_common.h"
@@ -23,7 +24,12 @@ namespace fc {
 namespace {
 
 constexpr int kMxdThreads = 256, kMxdWaves = 4;
-constexpr int kMxdGroups = 512;        // workgroups of a launch, two a compute unit
+constexpr int kAhead = 2;              // steps of rows under way in a wave
+constexpr int kLeastSteps = 4;         // of a workgroup, where there are enough
+constexpr int kMostGroups = 1024;
+// Waves that a SIMD holds by the registers of each form, and as many workgroups a compute unit, which all are resident: more of them wait for each
+// other's startup (28 layers of 4 heads that keep 6554 rows: 768 workgroups 32 us, 1024 36, 1536 39), fewer leave memory waiting.
+constexpr int waves_held(int d, int terms) { return (d == 64 ? 4 : 3) - (terms > 1 ? 1 : 0); }
 constexpr int kMostRows = (1 << 25) - 1;
 constexpr float kSlack = 16.f;         // how far scores (in log2) may exceed the running reference before it is moved
 
@@ -43,13 +49,15 @@ struct MxdArgs {
   int page_tiles, max_pages;
   int64_t num_pages;
   int groups;                    // workgroups of the launch
-  float scale_log2e;
+  float scale_log2e, limit_scale;        // of scores, above 0; its reciprocal
+  bool negate;                           // the scale is negative: queries change their signs
   float* pieces;
   int2* span;                    // first and last workgroup of each unit
   float* out;
 };
 
-__host__ __device__ inline size_t piece_floats(int G, int d) { return (size_t)G * (d + 2); }
+// a part of a unit, or a workgroup's piece: weighted V [G][d], references [G], sums [G]
+__host__ __device__ inline size_t piece_floats(int G, int d) { return ((size_t)G * (d + 2) + 3) / 4 * 4; }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(bf16x8, (u32x4{a, b, c, d}));
@@ -66,7 +74,36 @@ __device__ __forceinline__ void eight_values(uint32_t code, float unit, uint32_t
   o[2] = two_values<2>(code, unit);
   o[3] = two_values<3>(code, unit);
 }
+// in a scalar register
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v) {     // 0 where there is no source lane
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {          // sums up to and with each lane
+  v = dpp_add<0x111, 0xF>(v);      // row_shr:1, 2, 4, 8
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);      // row_bcast:15 into rows 1 and 3
+  return dpp_add<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
+}
+
+// Past the last-level cache: a step reads each row once, and before the next step a model's weights have been through it.  (Three caches in turn,
+// claiming it / not: 200 MB 58 / 54 us, 449 MB 96 / 86, 100 MB the same; one cache again and again, 200 MB 48 / 51.)
+template <typename V> __device__ __forceinline__ V load_past(const void* p) { return __builtin_nontemporal_load(static_cast<const V*>(p)); }
+
+// x less the lower or the upper of two bf16 values: exact where that value is x cut off.  (One operation; the constants are kept from the
+// compiler, which would take 0xBF800000 for an inline constant of another value in this instruction.)
+__device__ __forceinline__ float less_low(float x, uint32_t two) {
+  uint32_t c;
+  asm("s_mov_b32 %0, 0xbf80" : "=s"(c));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, c), x, false);
+}
+__device__ __forceinline__ float less_high(float x, uint32_t two) {
+  uint32_t c;
+  asm("s_mov_b32 %0, 0xbf800000" : "=s"(c));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, c), x, false);
+}
 
 __device__ __forceinline__ int rows_at(const MxdArgs& a, int bl) {
   return min(min(max(a.rows[bl], 0), kMostRows), (int)min((int64_t)kMostRows, (int64_t)a.max_pages * a.page_tiles * 16));
@@ -78,60 +115,84 @@ template <int D> struct Step {
   static constexpr int kWords = D / 32;
   uint32_t k[2][kWords], v[2][kWords];
   uint32_t ks[2], vs[2];
+  int gone[2], missing;          // negative: the tile, either tile has no page
 };
 
 template <int D, int QTERMS>
-__global__ __launch_bounds__(kMxdThreads, 2) void mx_decode_partial_kernel(MxdArgs a) {
+__global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_partial_kernel(MxdArgs a) {
   typedef MxTile<D> Tile;
   constexpr int KW = D / 32;             // dwords of K and of V a lane and tile; 32-column products of a score
   constexpr int VT = D / 16;             // output tiles
-  __shared__ float sm_m[kMxdWaves][16], sm_l[kMxdWaves][16];
-  __shared__ float sm_o[kMxdWaves][16][D];
+  extern __shared__ __align__(16) float parts[];       // [2 kMxdWaves][piece_floats]: the first and the last unit of each wave's run, if it has a part of them
+  __shared__ int part_unit[2 * kMxdWaves], part_ends[2 * kMxdWaves];   // -1: none; bit 0: the unit's first rows, bit 1: its last
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c16 = lane & 15, g4 = lane >> 4, G = a.G;
+  const int w = blockIdx.x, part_floats = (int)piece_floats(G, D);
+  if (lane < 2) part_unit[2 * wave + lane] = -1;
 
-  // ---- this workgroup's steps, and the unit that they begin in
-  const int per = (a.layers + 63) >> 6, first = min(a.layers, lane * per), last = min(a.layers, first + per);
-  int64_t mine = 0;
-  for (int i = first; i < last; ++i) mine += (int64_t)steps_of(rows_at(a, i)) * a.H;
-  int64_t upto = mine;
+  // ---- steps of all layers, each head of which has as many (the sum over all units fits 31 bits: mx_decode_reach)
+  constexpr int kChunks = 8;             // 64 layers each, whose rows are under way together and stay in registers
+  int held[kChunks];
+  auto load_rows = [&](int base) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t o = __shfl_up(upto, d, 64);
-    if (lane >= d) upto += o;
-  }
-  const int64_t all = __shfl(upto, 63, 64);
-  if (all == 0) return;
-  // (four steps a workgroup at least, one for each wave)
-  const int64_t groups = min((int64_t)a.groups, (all + 3) >> 2), w = blockIdx.x;
-  if (w >= groups) return;
-  int64_t at = all * w / groups;
-  const int64_t end = all * (w + 1) / groups;
-  int bl;                                // layer that step `at` is in
-  int64_t begin_of;                      // and `at`'s place in it (beyond 31 bits where heads have many rows)
-  {
-    const uint64_t behind = __ballot(upto > at);
-    const int owner = __builtin_ctzll(behind);
-    int64_t before = upto - mine;
-    int found = first;
-    if (lane == owner)
-      for (; found < last; ++found) {
-        const int64_t n = (int64_t)steps_of(rows_at(a, found)) * a.H;
-        if (before + n > at) break;
-        before += n;
+    for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j < a.layers ? rows_at(a, min(base + 64 * j + lane, a.layers - 1)) : 0;
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j + lane < a.layers ? held[j] : -1;      // (-1: no layer)
+  };
+  int total = 0;
+  for (int base = 0; base < a.layers; base += 64 * kChunks) {
+    load_rows(base);
+    int sum = 0;
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) {
+      sum += steps_of(max(held[j], 0));
+      // zeros for layers without rows, a workgroup's share of them
+      if (wave == 0 && __ballot(held[j] == 0)) {
+        uint64_t none = __ballot(held[j] == 0 && (base + 64 * j + lane) % a.groups == w);
+        for (; none; none &= none - 1) {
+          float4v* const out = reinterpret_cast<float4v*>(a.out + (size_t)(base + 64 * j + __builtin_ctzll(none)) * a.H * G * D);
+          for (int i = lane; i < a.H * G * (D / 4); i += 64) out[i] = float4v{0.f, 0.f, 0.f, 0.f};
+        }
       }
-    bl = __builtin_amdgcn_readlane(found, owner);
-    const uint64_t in = (uint64_t)(at - before);
-    begin_of = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(in >> 32), owner) << 32 |
-                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)in, owner));
+    }
+    total += __builtin_amdgcn_readlane(wave_scan(sum), 63);
   }
-  int rows = uniform(rows_at(a, bl)), steps = steps_of(rows);
-  int h = uniform((int)(begin_of / steps)), s = uniform((int)(begin_of - (int64_t)h * steps));
+  // ---- this wave's, and the unit that they begin in
+  const int all = total * a.H, groups = min(a.groups, (all + kLeastSteps - 1) / kLeastSteps);
+  if (w >= groups) return;
+  const int runs = groups * kMxdWaves, run = w * kMxdWaves + wave, each = all / runs, over = all - each * runs;
+  int at = run * each + min(run, over);
+  const int end = at + each + (run < over ? 1 : 0);
+  int bl = 0, h = 0, s = 0, rows = 0, steps = 1;
+  if (at < end) {
+    const int in_heads = at / a.H;
+    int before = 0, base = 0;
+    for (bool found = false; !found; base += 64 * kChunks) {
+      if (a.layers > 64 * kChunks) load_rows(base);
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j) {
+        if (!found && base + 64 * j < a.layers) {
+          const int upto = wave_scan(steps_of(max(held[j], 0))), chunk = __builtin_amdgcn_readlane(upto, 63);
+          if (before + chunk > in_heads) {
+            found = true;
+            const int owner = __builtin_ctzll(__ballot(before + upto > in_heads));
+            bl = base + 64 * j + owner;
+            rows = __builtin_amdgcn_readlane(held[j], owner);
+            steps = steps_of(rows);
+            const int place = at - (before + __builtin_amdgcn_readlane(upto, owner) - steps) * a.H;
+            h = place / steps;
+            s = place - h * steps;
+          }
+          before += chunk;
+        }
+      }
+    }
+  }
 
-  // ---- pieces of units, one after another
+  // ---- one unit after another
+  int part = 2 * wave;
   while (at < end) {
     const int unit = bl * a.H + h;
-    const int n = (int)min((int64_t)(steps - s), end - at), s_end = s + n;
-    const int s0 = s + (int)((int64_t)n * wave / kMxdWaves), s1 = s + (int)((int64_t)n * (wave + 1) / kMxdWaves);
+    const int n = min(steps - s, end - at), s0 = s, s1 = s + n;
 
     // queries: head c16 (zeros beyond G), columns D / 4 g4 + 8 i .. + 7
     uint32_t q[QTERMS][KW][4];
@@ -141,14 +202,15 @@ __global__ __launch_bounds__(kMxdThreads, 2) void mx_decode_partial_kernel(MxdAr
       for (int i = 0; i < KW; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[t][i][j] = 0u;
-    if (c16 < G && s0 < s1) {
+    if (c16 < G) {
       const size_t at_q = ((size_t)unit * G + c16) * D + g4 * (D / 4);
       if constexpr (QTERMS == 1) {
+        const uint32_t flip = a.negate ? 0x80008000u : 0u;
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
           const u32x4 u = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.Q) + at_q + 8 * i);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) q[0][i][j] = u[j];
+          for (int j = 0; j < 4; ++j) q[0][i][j] = u[j] ^ flip;
         }
       } else {
 #pragma unroll
@@ -156,7 +218,7 @@ __global__ __launch_bounds__(kMxdThreads, 2) void mx_decode_partial_kernel(MxdAr
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float2v x = *reinterpret_cast<const float2v*>(static_cast<const float*>(a.Q) + at_q + 8 * i + 2 * j);
-            float x0 = x[0], x1 = x[1];
+            float x0 = a.negate ? -x[0] : x[0], x1 = a.negate ? -x[1] : x[1];
 #pragma unroll
             for (int t = 0; t < QTERMS; ++t) {
               // (the first two cut off, so that nothing overflows to infinity; the last to nearest)
@@ -173,45 +235,62 @@ __global__ __launch_bounds__(kMxdThreads, 2) void mx_decode_partial_kernel(MxdAr
       }
     }
 
-    float m = -INFINITY, ls = 0.f;       // reference of head c16 (the same in its four lanes), and this lane's sum
+    // reference of head c16 (the same in its four lanes), in log2 units, and this lane's sum; the product from which on the reference is moved
+    float m = -INFINITY, ref = 0.f, ls = 0.f, limit = -INFINITY;
     float4v out[VT];
 #pragma unroll
     for (int t = 0; t < VT; ++t) out[t] = float4v{0.f, 0.f, 0.f, 0.f};
 
     const int32_t* const entries = a.table + (int64_t)unit * a.max_pages;
-    const int tiles = (rows + 15) >> 4;
-    // address of a tile (the cache's first one if it has no page: masked)
-    auto tile_at = [&](int t, bool& ok) -> const uint8_t* {
-      t = min(t, tiles - 1);
-      const int p = t / a.page_tiles;
-      const int64_t page = entries[p];
-      ok = page >= 0 && page < a.num_pages;
-      return a.pages + (ok ? page * a.page_tiles + (t - p * a.page_tiles) : 0) * Tile::kBytes;
+    const int last_tile = min((rows + 15) >> 4, 2 * s1);
+    const uint32_t k_off = Tile::k_code(c16, g4 * (D / 8)), v_off = Tile::v_code(4 * g4, c16);
+    const uint32_t ks_off = Tile::k_scale(c16, g4 * (D / 4) / 32), vs_off = Tile::v_scale(4 * g4, c16 * (D / 16) / 32);
+    // The tile to be loaded next, its page and its place there.  Lane i holds the first tile of page page0 + i of the table (-1: it has none), so
+    // that no load waits for a lookup.
+    int tile = 2 * s0, in_page, page;    // (page: counted from page0)
+    int page0 = uniform(tile / a.page_tiles);
+    in_page = tile - page0 * a.page_tiles;
+    page = 0;
+    auto lookup = [&]() -> int32_t {
+      const int32_t id = entries[min(page0 + lane, a.max_pages - 1)];
+      return id >= 0 && id < a.num_pages ? id * a.page_tiles : -1;
     };
-    const int k_off = Tile::k_code(c16, g4 * (D / 8)), v_off = Tile::v_code(4 * g4, c16);
-    const int ks_off = Tile::k_scale(c16, g4 * (D / 4) / 32), vs_off = Tile::v_scale(4 * g4, c16 * (D / 16) / 32);
-    auto load_step = [&](int st, Step<D>& x) -> unsigned {
-      unsigned ok2 = 0;
+    int32_t entry = lookup();
+    auto load_step = [&](Step<D>& x) {
+      x.missing = 0;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        bool ok;
-        const uint8_t* tile = tile_at(2 * st + tt, ok);
-        ok2 |= (ok ? 1u : 0u) << tt;
+        const int first_tile = __builtin_amdgcn_readlane(entry, page);
+        x.missing |= first_tile;                           // (negative if either is)
+        x.gone[tt] = first_tile;
+        // (the cache's first tiles in place of those that have no page: masked)
+        const uint8_t* const at_tile = a.pages + (uint64_t)(uint32_t)(max(first_tile, 0) + in_page) * Tile::kBytes;
+        if (tile + 1 < last_tile) {                        // (behind the last tile it comes again)
+          ++tile;
+          if (++in_page == a.page_tiles) {
+            in_page = 0;
+            if (++page == 64) {
+              page0 += 64;
+              page = 0;
+              entry = lookup();
+              asm volatile("" : "+v"(entry));              // (waited for here, not before every use)
+            }
+          }
+        }
         if constexpr (D == 128) {
-          const u32x4 k = *reinterpret_cast<const u32x4*>(tile + k_off), v = *reinterpret_cast<const u32x4*>(tile + v_off);
+          const u32x4 k = load_past<u32x4>(at_tile + k_off), v = load_past<u32x4>(at_tile + v_off);
 #pragma unroll
           for (int i = 0; i < KW; ++i) { x.k[tt][i] = k[i]; x.v[tt][i] = v[i]; }
         } else {
-          const u32x2 k = *reinterpret_cast<const u32x2*>(tile + k_off), v = *reinterpret_cast<const u32x2*>(tile + v_off);
+          const u32x2 k = load_past<u32x2>(at_tile + k_off), v = load_past<u32x2>(at_tile + v_off);
 #pragma unroll
           for (int i = 0; i < KW; ++i) { x.k[tt][i] = k[i]; x.v[tt][i] = v[i]; }
         }
-        x.ks[tt] = tile[ks_off];
-        x.vs[tt] = *reinterpret_cast<const uint32_t*>(tile + vs_off);
+        x.ks[tt] = load_past<uint8_t>(at_tile + ks_off);
+        x.vs[tt] = load_past<uint32_t>(at_tile + vs_off);
       }
-      return ok2;
     };
-    auto work = [&](int st, unsigned ok2, Step<D>& x) {
+    auto work = [&](int st, Step<D>& x) {
       float sc[2][4];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
@@ -227,26 +306,28 @@ __global__ __launch_bounds__(kMxdThreads, 2) void mx_decode_partial_kernel(MxdAr
             acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, as_bf16x8(q[t][i][0], q[t][i][1], q[t][i][2], q[t][i][3]), acc, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[tt][i] = acc[i] * a.scale_log2e;
+        for (int i = 0; i < 4; ++i) sc[tt][i] = acc[i];
       }
       const int rb = 32 * st + 4 * g4;
-      if (ok2 != 3u || 32 * st + 32 > rows) {              // (the same for the wave)
+      if (x.missing < 0 || 32 * st + 32 > rows) {              // (the same for the wave)
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (rb + 16 * tt + i >= rows || !((ok2 >> tt) & 1u)) {
+            if (rb + 16 * tt + i >= rows || x.gone[tt] < 0) {
               sc[tt][i] = -INFINITY;
               x.vs[tt] = (x.vs[tt] & ~(0xFFu << (8 * i))) | (127u << (8 * i));     // (no NaN from a row that is not there)
             }
       }
       float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
                        fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      if (__ballot(mx > m + kSlack)) {                     // (-inf + 16: any score at all)
+      if (__ballot(mx > limit)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m, mx), alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+        const float m_new = fmaxf(m, mx * a.scale_log2e), alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
         m = m_new;
+        limit = (m + kSlack) * a.limit_scale;
+        ref = m > -INFINITY ? m : 0.f;
         ls *= alpha;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -255,36 +336,31 @@ __global__ __launch_bounds__(kMxdThreads, 2) void mx_decode_partial_kernel(MxdAr
           for (int t = 0; t < VT; ++t) out[t][i] *= a_i;
         }
       }
-      const float ref = m > -INFINITY ? m : 0.f;
       uint32_t hi[4], mid[4], lo[4];
-      float psum = 0.f;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
-          float p0 = __builtin_amdgcn_exp2f(sc[tt][i] - ref), p1 = __builtin_amdgcn_exp2f(sc[tt][i + 1] - ref);
-          psum += p0;
-          psum += p1;
+          float p0 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i], a.scale_log2e, -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i + 1], a.scale_log2e, -ref));
+          ls += p0;
+          ls += p1;
           const int w2 = 2 * tt + i / 2;
-          uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-          hi[w2] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
-          p0 -= __uint_as_float(u0 & 0xFFFF0000u);
-          p1 -= __uint_as_float(u1 & 0xFFFF0000u);
-          u0 = __float_as_uint(p0);
-          u1 = __float_as_uint(p1);
-          mid[w2] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
-          lo[w2] = pack_bf16(p0 - __uint_as_float(u0 & 0xFFFF0000u), p1 - __uint_as_float(u1 & 0xFFFF0000u));
+          hi[w2] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+          p0 = less_low(p0, hi[w2]);
+          p1 = less_high(p1, hi[w2]);
+          mid[w2] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+          lo[w2] = pack_bf16(less_low(p0, mid[w2]), less_high(p1, mid[w2]));
         }
-      ls += psum;
       const bf16x8 ph = as_bf16x8(hi[0], hi[1], hi[2], hi[3]), pm = as_bf16x8(mid[0], mid[1], mid[2], mid[3]),
                    pl = as_bf16x8(lo[0], lo[1], lo[2], lo[3]);
       float unit_v[2][4];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        unit_v[tt][0] = __uint_as_float((x.vs[tt] << 23) & 0x7F800000u);
-        unit_v[tt][1] = __uint_as_float((x.vs[tt] << 15) & 0x7F800000u);
-        unit_v[tt][2] = __uint_as_float((x.vs[tt] << 7) & 0x7F800000u);
-        unit_v[tt][3] = __uint_as_float((x.vs[tt] >> 1) & 0x7F800000u);
+        // (the conversion looks at the exponent alone)
+        unit_v[tt][0] = __uint_as_float(x.vs[tt] << 23);
+        unit_v[tt][1] = __uint_as_float(x.vs[tt] << 15);
+        unit_v[tt][2] = __uint_as_float(x.vs[tt] << 7);
+        unit_v[tt][3] = __uint_as_float(x.vs[tt] >> 1);
       }
       // byte c of a row's D / 32 bytes has the columns of output tiles 2 c and 2 c + 1
       auto tiles_of = [&](auto byte) {
@@ -315,114 +391,195 @@ __global__ __launch_bounds__(kMxdThreads, 2) void mx_decode_partial_kernel(MxdAr
         tiles_of(std::integral_constant<int, 3>{});
       }
     };
+    // kAhead steps under way; a step's registers are filled again in place.  (Loads without conditions, behind the wave's last step of that
+    // step's last tile again: where a load may or may not have been made the next wait is for all of them.)
     {
-      Step<D> xa, xb;
-      unsigned oka = 0, okb = 0;
-      if (s0 < s1) oka = load_step(s0, xa);
-      for (int st = s0; st < s1; st += 2) {
-        if (st + 1 < s1) okb = load_step(st + 1, xb);
-        work(st, oka, xa);
-        if (st + 1 >= s1) break;
-        if (st + 2 < s1) oka = load_step(st + 2, xa);
-        work(st + 1, okb, xb);
+      Step<D> x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) load_step(x[i]);
+      for (int st = s0; st < s1; st += kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (st + i < s1) work(st + i, x[i]);
+          load_step(x[i]);
+        }
       }
     }
 
-    // the four lanes of a head add their sums; then the waves merge through LDS in a fixed order
+    // the four lanes of a head add their sums
     ls += __shfl_xor(ls, 16, 64);
     ls += __shfl_xor(ls, 32, 64);
-    if (g4 == 0) { sm_m[wave][c16] = m; sm_l[wave][c16] = ls; }
+    if (n == steps) {
 #pragma unroll
-    for (int t = 0; t < VT; ++t)
+      for (int i = 0; i < 4; ++i) {
+        const float lt = __shfl(ls, 4 * g4 + i, 64), share = lt == 0.f ? 0.f : 1.f / lt;     // (1 and more, if there is a row at all)
+        if (4 * g4 + i < G)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sm_o[wave][4 * g4 + i][VT * c16 + t] = out[t][i];
-    __syncthreads();
-    const bool whole = n == steps;
-    float* const piece = a.pieces + (size_t)(w + unit) * piece_floats(G, D);
-    for (int item = tid; item < G * D; item += kMxdThreads) {
-      const int g = item / D, dim = item % D;
-      float top = -INFINITY;
-#pragma unroll
-      for (int v = 0; v < kMxdWaves; ++v) top = fmaxf(top, sm_m[v][g]);
-      const float ref = top > -INFINITY ? top : 0.f;       // (none has a finite score: zeros, or NaN)
-      float acc = 0.f, lt = 0.f;
-#pragma unroll
-      for (int v = 0; v < kMxdWaves; ++v) {
-        const float wt = __builtin_amdgcn_exp2f(sm_m[v][g] - ref);
-        acc = fmaf(sm_o[v][g][dim], wt, acc);
-        lt = fmaf(sm_l[v][g], wt, lt);
+          for (int t = 0; t < VT; t += 4)
+            *reinterpret_cast<float4v*>(a.out + ((size_t)unit * G + 4 * g4 + i) * D + VT * c16 + t) =
+                float4v{out[t][i] * share, out[t + 1][i] * share, out[t + 2][i] * share, out[t + 3][i] * share};
       }
-      if (whole) {
-        a.out[((size_t)unit * G + g) * D + dim] = lt == 0.f ? 0.f : acc / lt;
-      } else {
-        piece[2 * G + (size_t)g * D + dim] = acc;
-        if (dim == 0) { piece[g] = top; piece[G + g] = lt; }
+      if (lane == 0) a.span[unit] = int2{w, w};
+    } else {
+      float* const mine = parts + part * part_floats;
+      if (g4 == 0 && c16 < G) { mine[G * D + c16] = m; mine[G * D + G + c16] = ls; }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * g4 + i < G)
+#pragma unroll
+          for (int t = 0; t < VT; t += 4)
+            *reinterpret_cast<float4v*>(mine + (4 * g4 + i) * D + VT * c16 + t) =
+                float4v{out[t][i], out[t + 1][i], out[t + 2][i], out[t + 3][i]};
+      if (lane == 0) {
+        part_unit[part] = unit;
+        part_ends[part] = (s == 0 ? 1 : 0) | (s1 == steps ? 2 : 0);
       }
-    }
-    if (tid == 0) {
-      if (s == 0) a.span[unit].x = (int)w;
-      if (s_end == steps) a.span[unit].y = (int)w;
+      ++part;
     }
     // on to the next unit that has rows
     at += n;
-    if (at < end) {
-      __syncthreads();                                     // (the LDS arrays are still being read)
-      s = 0;
-      if (++h == a.H) {
-        h = 0;
-        do {
-          ++bl;
-          rows = uniform(rows_at(a, bl));
-        } while (rows == 0);
-        steps = steps_of(rows);
+    s = 0;
+    if (at < end && ++h == a.H) {
+      h = 0;
+      do {
+        ++bl;
+        rows = uniform(rows_at(a, bl));
+      } while (rows == 0);
+      steps = steps_of(rows);
+    }
+  }
+  __syncthreads();
+
+  // ---- parts of one unit, one a wave at most and next to each other, become one in their order
+  const int units_of = lane < 2 * kMxdWaves ? part_unit[lane] : -1, ends_of = lane < 2 * kMxdWaves ? part_ends[lane] : 0;
+  uint32_t left = (uint32_t)__ballot(units_of >= 0);
+  while (left) {
+    const int unit = __builtin_amdgcn_readlane(units_of, __builtin_ctz(left));
+    uint32_t same = (uint32_t)__ballot(units_of == unit);
+    left &= ~same;
+    const bool begins = __ballot(units_of == unit && (ends_of & 1)), ends = __ballot(units_of == unit && (ends_of & 2));
+    int from[kMxdWaves];                 // (the first again, without weight, where there are fewer)
+    bool have[kMxdWaves];
+#pragma unroll
+    for (int v = 0; v < kMxdWaves; ++v) {
+      have[v] = same != 0;
+      from[v] = (have[v] ? __builtin_ctz(same) * part_floats : from[0]);
+      same &= same - 1;
+    }
+    float* const piece = a.pieces + (size_t)(w + unit) * part_floats;
+    for (int item = tid; item < G * D / 4; item += kMxdThreads) {       // four columns
+      const int g = item / (D / 4);
+      float m[kMxdWaves], l[kMxdWaves], top = -INFINITY;
+      float4v o[kMxdWaves];
+#pragma unroll
+      for (int v = 0; v < kMxdWaves; ++v) {
+        m[v] = parts[from[v] + G * D + g];
+        l[v] = parts[from[v] + G * D + G + g];
+        o[v] = *reinterpret_cast<const float4v*>(parts + from[v] + 4 * item);
+        top = fmaxf(top, m[v]);
       }
+      const float ref = top > -INFINITY ? top : 0.f;       // (none has a finite score: zeros, or NaN)
+      float4v acc = {0.f, 0.f, 0.f, 0.f};
+      float lt = 0.f;
+#pragma unroll
+      for (int v = 0; v < kMxdWaves; ++v)
+        if (have[v]) {
+          const float wt = __builtin_amdgcn_exp2f(m[v] - ref);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] = fmaf(o[v][i], wt, acc[i]);
+          lt = fmaf(l[v], wt, lt);
+        }
+      if (begins && ends) {
+        const float share = lt == 0.f ? 0.f : 1.f / lt;
+        *reinterpret_cast<float4v*>(a.out + (size_t)unit * G * D + 4 * item) = acc * share;
+      } else {
+        *reinterpret_cast<float4v*>(piece + 4 * item) = acc;
+        if (4 * item % D == 0) { piece[G * D + g] = top; piece[G * D + G + g] = lt; }
+      }
+    }
+    if (tid == 0) {
+      if (begins) a.span[unit].x = w;
+      if (ends) a.span[unit].y = w;
     }
   }
 }
 
-// out[unit][g][:] of units that several workgroups had a piece of, and zeros for those without rows.  grid = (G, units), a thread for each
-// column and every kMergeSets-th piece.
-constexpr int kMergeSets = 4;
-__global__ void mx_decode_merge_kernel(MxdArgs a, int d) {
-  extern __shared__ float lds[];                           // [kMergeSets][2][d]
-  const int g = blockIdx.x, unit = blockIdx.y, dim = threadIdx.x % d, set = threadIdx.x / d, G = a.G;
-  float* const out = a.out + ((size_t)unit * G + g) * d;
-  if (rows_at(a, unit / a.H) == 0) {
-    if (set == 0) out[dim] = 0.f;
-    return;
-  }
+// out[unit][g][:] of units that several workgroups had a piece of.  grid = (slices of the heads, units); `sets` groups of d threads have
+// kAtOnce pieces each at a time, all of them under way together.
+constexpr int kAtOnce = 8;
+__global__ void mx_decode_merge_kernel(MxdArgs a, int d, int heads) {
+  extern __shared__ float lds[];                           // [sets][3][d]: largest reference, sum, weighted sum
+  const int unit = blockIdx.y, dim = threadIdx.x % d, set = threadIdx.x / d, sets = blockDim.x / d, G = a.G;
+  if (rows_at(a, unit / a.H) == 0) return;
   const int2 span = a.span[unit];
   if (span.x == span.y) return;                            // (written by its workgroup)
   const size_t stride = piece_floats(G, d);
-  const float* const base = a.pieces + (size_t)(span.x + unit) * stride;
-  const int n = span.y - span.x + 1;
-  float top = -INFINITY;
-  for (int i = 0; i < n; ++i) top = fmaxf(top, base[i * stride + g]);
-  const float ref = top > -INFINITY ? top : 0.f;
-  float acc = 0.f, lt = 0.f;
-  for (int i = set; i < n; i += kMergeSets) {
-    const float* const piece = base + i * stride;
-    const float wt = __builtin_amdgcn_exp2f(piece[g] - ref);
-    acc = fmaf(piece[2 * G + (size_t)g * d + dim], wt, acc);
-    lt = fmaf(piece[G + g], wt, lt);
+  const int first = min(max(span.x, 0), a.groups - 1), n = min(max(span.y, first), a.groups - 1) - first + 1;
+  const float* const base = a.pieces + (size_t)(first + unit) * stride;
+  const int g1 = min(G, (int)(blockIdx.x + 1) * heads);
+  for (int g = blockIdx.x * heads; g < g1; ++g) {
+    float top = -INFINITY, acc = 0.f, lt = 0.f;
+    for (int i0 = set * kAtOnce; i0 < n; i0 += sets * kAtOnce) {
+      float m[kAtOnce], l[kAtOnce], o[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const float* const piece = base + (size_t)min(i0 + i, n - 1) * stride;
+        const bool have = i0 + i < n;
+        m[i] = have ? piece[G * d + g] : -INFINITY;
+        l[i] = have ? piece[G * d + G + g] : 0.f;
+        o[i] = have ? piece[g * d + dim] : 0.f;
+      }
+      float up = top;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) up = fmaxf(up, m[i]);
+      const float ref = up > -INFINITY ? up : 0.f, before = __builtin_amdgcn_exp2f(top - ref);
+      acc *= before;
+      lt *= before;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const float wt = __builtin_amdgcn_exp2f(m[i] - ref);
+        acc = fmaf(o[i], wt, acc);
+        lt = fmaf(l[i], wt, lt);
+      }
+      top = up;
+    }
+    if (sets > 1) {
+      float* const mine = lds + (size_t)set * 3 * d + dim;
+      if (g > (int)blockIdx.x * heads) __syncthreads();    // (the head before is still being read)
+      mine[0] = top;
+      mine[d] = lt;
+      mine[2 * d] = acc;
+      __syncthreads();
+      if (set == 0) {
+        float up = top;
+        for (int v = 1; v < sets; ++v) up = fmaxf(up, mine[v * 3 * d]);
+        const float ref = up > -INFINITY ? up : 0.f;
+        acc = lt = 0.f;
+        for (int v = 0; v < sets; ++v) {
+          const float wt = __builtin_amdgcn_exp2f(mine[v * 3 * d] - ref);
+          acc = fmaf(mine[(v * 3 + 2) * d], wt, acc);
+          lt = fmaf(mine[(v * 3 + 1) * d], wt, lt);
+        }
+      }
+    }
+    if (set == 0) a.out[((size_t)unit * G + g) * d + dim] = lt == 0.f ? 0.f : acc / lt;
   }
-  lds[(set * 2) * d + dim] = acc;
-  lds[(set * 2 + 1) * d + dim] = lt;
-  __syncthreads();
-  if (set > 0) return;
-  for (int v = 1; v < kMergeSets; ++v) {
-    acc += lds[(v * 2) * d + dim];
-    lt += lds[(v * 2 + 1) * d + dim];
-  }
-  out[dim] = lt == 0.f ? 0.f : acc / lt;
 }
 
 }  // namespace
 
 bool mx_decode_supported(int group, int d) { return (d == 64 || d == 128) && group >= 1 && group <= 16; }
 
+// Whether the steps of the rows that the tables reach are counted in 31 bits.
+bool mx_decode_reach(int64_t units, int64_t max_pages, int64_t page_size) {
+  return units * ((std::min<int64_t>(kMostRows, max_pages * page_size) + 31) / 32) < (1ll << 31);
+}
+
+static size_t pieces_bytes(int units, int group, int d) {
+  return ((size_t)(units + kMostGroups) * piece_floats(group, d) * sizeof(float) + 15) / 16 * 16;
+}
 size_t mx_decode_workspace_bytes(int units, int group, int d) {
-  return units == 0 ? 0 : ((size_t)(units + kMxdGroups) * piece_floats(group, d) * sizeof(float) + 15) / 16 * 16 + (size_t)units * sizeof(int2);
+  return units == 0 ? 0 : pieces_bytes(units, group, d) + (size_t)units * sizeof(int2);
 }
 
 hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* table, int page_size, int max_pages, int64_t num_pages,
@@ -431,21 +588,32 @@ hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* tab
   const int units = B * L * H;
   // no more workgroups than the rows that tables and pages have room for make
   const int64_t room = std::min((int64_t)units * (((int64_t)max_pages * page_size + 31) / 32), num_pages * (page_size / 16) + units);
-  const int groups = (int)std::min<int64_t>(kMxdGroups, (room + 3) / 4);
-  float* const pieces = static_cast<float*>(ws);
-  int2* const span = reinterpret_cast<int2*>(static_cast<char*>(ws) + ((size_t)(units + kMxdGroups) * piece_floats(group, d) * sizeof(float) + 15) / 16 * 16);
+  const int held = 256 * waves_held(d, dtype == FC_BF16 ? 1 : 3), groups = (int)std::min<int64_t>(held, (room + kLeastSteps - 1) / kLeastSteps);
+  // (a scale of zero: the smallest there is, which leaves all scores as alike as they can be told)
+  const float positive = std::max(std::fabs(scale) * 1.4426950408889634f, 1.17549435e-38f);
   const MxdArgs a{Q, static_cast<const uint8_t*>(pages), rows, table, B * L, H, group, page_size / 16, max_pages, num_pages, groups,
-                  scale * 1.4426950408889634f, pieces, span, out};
+                  positive, std::min(1.f / positive, 3.4e38f), scale < 0.f, static_cast<float*>(ws),
+                  reinterpret_cast<int2*>(static_cast<char*>(ws) + pieces_bytes(units, group, d)), out};
   {
     ProfileScope ps("mx_decode_partial_kernel", s);
-    auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups), dim3(kMxdThreads), 0, s, a); };
+    const size_t lds = 2 * kMxdWaves * piece_floats(group, d) * sizeof(float);
+    hipError_t e = hipSuccess;
+    auto launch = [&](auto kern) {
+      if (lds > 65536)                                     // (16 query heads of 128 columns)
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e == hipSuccess) hipLaunchKernelGGL(kern, dim3(groups), dim3(kMxdThreads), lds, s, a);
+    };
     if (dtype == FC_BF16) d == 128 ? launch(mx_decode_partial_kernel<128, 1>) : launch(mx_decode_partial_kernel<64, 1>);
     else d == 128 ? launch(mx_decode_partial_kernel<128, 3>) : launch(mx_decode_partial_kernel<64, 3>);
+    if (e != hipSuccess) return e;
   }
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || groups == 1) return e;            // (no unit in two workgroups)
+  // pieces of a unit if all units are alike, and two more; a workgroup for each head where that is no more than a few thousand
+  const int sets = std::min(1024 / d, std::max(1, (groups / units + 2 + kAtOnce - 1) / kAtOnce));
+  const int heads = std::min(group, std::max(1, units * group / 2048)), slices = (group + heads - 1) / heads;
   ProfileScope ps("mx_decode_merge_kernel", s);
-  hipLaunchKernelGGL(mx_decode_merge_kernel, dim3(group, units), dim3(kMergeSets * d), (size_t)kMergeSets * 2 * d * sizeof(float), s, a, d);
+  hipLaunchKernelGGL(mx_decode_merge_kernel, dim3(slices, units), dim3(sets * d), (size_t)sets * 3 * d * sizeof(float), s, a, d, heads);
   return hipGetLastError();
 }
 
