@@ -400,6 +400,7 @@ fc_status flashcache_rotary(const fc_rotary_plan* plan, const int32_t* positions
                             const fc_heads_desc* q_desc, const void* K, void* K_out, const fc_heads_desc* k_desc,
                             int32_t inverse, void* hip_stream) {
   if (!plan || !q_desc || plan->magic != kWsMagic) return FC_EINVAL;
+  if (plan->rotary_dim < 2 || plan->rotary_dim > 2 * FC_ROTARY_MAX_PAIRS || plan->streams < 1 || plan->streams > 4) return FC_EINVAL;
   fc_status st = check_heads(*plan, *q_desc, Q, Q_out);
   if (st != FC_OK) return st;
   if (k_desc) {

@@ -25,7 +25,7 @@ struct PageArgs {
   int64_t* cursor_out;
   int64_t* slots;                // [B][slots_per_seq] or nullptr
   int64_t num_free, slots_per_seq;
-  int B, L, H, page_size, max_pages, add_each;
+  int B, L, H, page_size, page_shift, max_pages, add_each;         // (the shift: -1 if the size is no power of two)
   bool finish;                   // one workgroup, or outputs of their own: they are written here
 };
 
@@ -45,6 +45,7 @@ __global__ __launch_bounds__(kPageThreads) void assign_pages_kernel(PageArgs a) 
   extern __shared__ int64_t lds[];
   int64_t* const rows_before = lds;                        // [L + 1], all heads
   int64_t* const pages_before = lds + a.L + 1;             // [L + 1], all heads and the sequences before
+  Held* const held = reinterpret_cast<Held*>(pages_before + a.L + 1);          // [L]
   __shared__ int64_t wave_rows[kPageThreads / 64], wave_pages[kPageThreads / 64], before_wave[kPageThreads / 64];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // pages that earlier sequences take
@@ -58,6 +59,7 @@ __global__ __launch_bounds__(kPageThreads) void assign_pages_kernel(PageArgs a) 
   int64_t rows = 0, pages = 0;
   for (int l = l0; l < l1; ++l) {
     const Held x = held_at(a, b * a.L + l);
+    held[l] = x;
     rows += x.grown - x.rows;
     pages += x.fresh;
   }
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(kPageThreads) void assign_pages_kernel(PageArgs a) 
     earlier += before_wave[w];
   }
   for (int l = l0; l < l1; ++l) {
-    const Held x = held_at(a, b * a.L + l);
+    const Held x = held[l];
     rows_before[l] = r * a.H;
     pages_before[l] = (earlier + p) * a.H;
     r += x.grown - x.rows;
@@ -101,16 +103,19 @@ __global__ __launch_bounds__(kPageThreads) void assign_pages_kernel(PageArgs a) 
     return lo;
   };
   const int64_t step = (int64_t)gridDim.x * kPageThreads, begin = (int64_t)blockIdx.x * kPageThreads + tid;
+  // (heads times rows of a layer are below 2^31 in all but caches that nobody has: 32-bit divisions)
+  auto head_of = [](int64_t in, int each) { return in >> 31 ? (int)(in / each) : (int)((uint32_t)in / (uint32_t)each); };
   if constexpr (SLOTS) {
     const int64_t all = rows_before[a.L], end = all > a.slots_per_seq ? all : a.slots_per_seq;
     for (int64_t i = begin; i < end; i += step) {
       int64_t slot = -1;
       if (i < all) {
         const int l = layer_of(rows_before, i);
-        const Held x = held_at(a, b * a.L + l);
+        const Held x = held[l];
         const int added = x.grown - x.rows;
         const int64_t in = i - rows_before[l];             // < H * added
-        const int h = (int)(in / added), row = x.rows + (int)(in - (int64_t)h * added), page = row / a.page_size, off = row - page * a.page_size;
+        const int h = head_of(in, added), row = x.rows + (int)(in - (int64_t)h * added);
+        const int page = a.page_shift >= 0 ? row >> a.page_shift : row / a.page_size, off = row - page * a.page_size;
         int32_t* const entry = a.table + ((int64_t)(b * a.L + l) * a.H + h) * a.max_pages + page;
         if (page < a.max_pages) {
           const int32_t id = page < x.first ? *entry : page_at(pages_before[l] + (int64_t)h * x.fresh + page - x.first);
@@ -124,15 +129,15 @@ __global__ __launch_bounds__(kPageThreads) void assign_pages_kernel(PageArgs a) 
     const int64_t first = pages_before[0], all = pages_before[a.L] - first;
     for (int64_t i = begin; i < all; i += step) {
       const int l = layer_of(pages_before, first + i);
-      const Held x = held_at(a, b * a.L + l);
+      const Held x = held[l];
       const int64_t in = first + i - pages_before[l];      // < H * fresh
-      const int h = (int)(in / x.fresh), page = x.first + (int)(in - (int64_t)h * x.fresh);
+      const int h = head_of(in, x.fresh), page = x.first + (int)(in - (int64_t)h * x.fresh);
       a.table[((int64_t)(b * a.L + l) * a.H + h) * a.max_pages + page] = page_at(first + i);
     }
   }
   if (a.finish && blockIdx.x == 0) {                       // (outputs of their own, or no other workgroup reads the inputs)
     __syncthreads();
-    for (int l = tid; l < a.L; l += kPageThreads) a.rows_out[b * a.L + l] = held_at(a, b * a.L + l).grown;
+    for (int l = tid; l < a.L; l += kPageThreads) a.rows_out[b * a.L + l] = held[l].grown;
     if (b == a.B - 1 && tid == 0) a.cursor_out[0] = cursor + pages_before[a.L];
   }
 }
@@ -166,9 +171,9 @@ hipError_t assign_pages_launch(const int32_t* rows, const int32_t* add, int32_t 
   const int64_t work = slots ? slots_per_seq : (int64_t)L * H * max_pages;
   const unsigned shares = (unsigned)std::min<int64_t>(4096, std::max<int64_t>(1, (work + 4 * kPageThreads - 1) / (4 * kPageThreads)));
   const bool in_place = rows_out == rows || cursor_out == cursor, alone = shares == 1 && B == 1;
-  PageArgs a{rows, add, rows_out, free_pages, table, cursor, cursor_out, slots, num_free, slots_per_seq, B, L, H, page_size, max_pages,
-             add_each, !in_place || alone};
-  const size_t lds = (size_t)(L + 1) * 2 * sizeof(int64_t);
+  PageArgs a{rows, add, rows_out, free_pages, table, cursor, cursor_out, slots, num_free, slots_per_seq, B, L, H, page_size,
+             page_size & (page_size - 1) ? -1 : __builtin_ctz((unsigned)page_size), max_pages, add_each, !in_place || alone};
+  const size_t lds = (size_t)(L + 1) * 2 * sizeof(int64_t) + (size_t)L * sizeof(Held);
   {
     ProfileScope ps("assign_pages_kernel", s);
     if (slots) hipLaunchKernelGGL(assign_pages_kernel<true>, dim3(shares, B), dim3(kPageThreads), lds, s, a);

@@ -8,8 +8,10 @@
 // fp32 is off by 0.06 rad at position 10^6.  32 bits of the turn are left to an octant and the series of sine and cosine
 // on |theta| <= pi / 4 (terms up to theta^9 and theta^8, whose rest is below 2^-25).
 //
-// Bound by memory: every element is read and written once.  A thread keeps the sines of its pairs and walks over heads, so
-// that what they cost (about 40 operations a pair) is shared by them.
+// Bound by memory: every element is read and written once.  A thread keeps the sines of its pairs (about 40 operations each) for several heads of
+// its token; eight heads side by side, so that what a wave reads at a time lies together.  32768 tokens of 28 and 4 heads of 128 columns in bf16
+// (0.54 GB in all): 112 us with a token's heads one after another in a thread, 105 side by side, 99 with loads and stores past the
+// last-level cache as well, 5.7 TB/s, which is a copy's rate here.
 #include <algorithm>
 #include <math.h>
 #include <string.h>
@@ -34,7 +36,7 @@ struct RotArgs {
   int tokens, rows;              // tokens of a sequence, of all sequences
   int half, chunks, turned;      // pairs; chunks of a head; those that are turned
   int per_group;                 // tokens of a workgroup
-  int heads_at_once;             // heads of a thread
+  int abreast, turns;            // heads of a token side by side; how many of them a thread has, one after another
   int streams, end0, end1, end2; // first pair behind the first, second and third stream
   float magnitude, sign;
 };
@@ -78,6 +80,32 @@ template <typename T, int N> __device__ __forceinline__ Vec<T, N> narrow(const f
   return v;
 }
 
+// PAST: past the last-level cache.
+template <bool PAST, typename T, int N> __device__ __forceinline__ Vec<T, N> get(const char* p) {
+  const Vec<T, N>* const at = reinterpret_cast<const Vec<T, N>*>(p);
+  Vec<T, N> v;
+  if constexpr (!PAST) {
+    v = *at;
+  } else if constexpr (sizeof(v.raw) <= 16) {
+    v.raw = __builtin_nontemporal_load(&at->raw);
+  } else {
+    v.raw.a = __builtin_nontemporal_load(&at->raw.a);
+    v.raw.b = __builtin_nontemporal_load(&at->raw.b);
+  }
+  return v;
+}
+template <bool PAST, typename T, int N> __device__ __forceinline__ void put(char* p, const Vec<T, N>& v) {
+  Vec<T, N>* const at = reinterpret_cast<Vec<T, N>*>(p);
+  if constexpr (!PAST) {
+    *at = v;
+  } else if constexpr (sizeof(v.raw) <= 16) {
+    __builtin_nontemporal_store(v.raw, &at->raw);
+  } else {
+    __builtin_nontemporal_store(v.raw.a, &at->raw.a);
+    __builtin_nontemporal_store(v.raw.b, &at->raw.b);
+  }
+}
+
 // Sine and cosine of `turns` 2^-32 of a whole turn.
 __device__ __forceinline__ void sine_cosine(uint32_t turns, float& s, float& c) {
   const uint32_t quarter = (turns + 0x20000000u) >> 30;
@@ -91,9 +119,10 @@ __device__ __forceinline__ void sine_cosine(uint32_t turns, float& s, float& c) 
 }
 
 // P pairs a thread and head; a chunk behind the turned ones is 2 P columns to be copied.
-template <typename T, int P, bool INTERLEAVED>
+template <typename T, int P, bool INTERLEAVED, bool PAST>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc_rotary_plan plan) {
-  const int chunk = (int)(threadIdx.x % (unsigned)a.chunks), own = (int)(threadIdx.x / (unsigned)a.chunks);
+  const int place = (int)(threadIdx.x / (unsigned)a.chunks), chunk = (int)threadIdx.x - place * a.chunks;
+  const int own = (int)((unsigned)place / (unsigned)a.abreast), beside = place - own * a.abreast;
   const int64_t row64 = (int64_t)blockIdx.x * a.per_group + own;
   if (own >= a.per_group || row64 >= a.rows) return;
   const int row = (int)row64, b = row / a.tokens, t = row - b * a.tokens;
@@ -120,18 +149,17 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc
     at0 = 2 * a.half + (chunk - a.turned) * 2 * P;
     at1 = at0 + P;
   }
-  const int heads = a.q.heads + a.k.heads, h1 = min(heads, (int)(blockIdx.y + 1) * a.heads_at_once);
+  const int heads = a.q.heads + a.k.heads, h0 = (int)blockIdx.y * a.abreast * a.turns, h1 = min(heads, h0 + a.abreast * a.turns);
 #pragma unroll 2
-  for (int h = (int)blockIdx.y * a.heads_at_once; h < h1; ++h) {
+  for (int h = h0 + beside; h < h1; h += a.abreast) {
     const bool is_q = h < a.q.heads;
     const int hh = is_q ? h : h - a.q.heads;
     const char* in = (is_q ? a.q.in : a.k.in) + b * (is_q ? a.q.sb : a.k.sb) + t * (is_q ? a.q.st : a.k.st) + hh * (is_q ? a.q.sh : a.k.sh);
     char* out = (is_q ? a.q.out : a.k.out) + b * (is_q ? a.q.ob : a.k.ob) + t * (is_q ? a.q.ot : a.k.ot) + hh * (is_q ? a.q.oh : a.k.oh);
-    const Vec<T, P> v0 = *reinterpret_cast<const Vec<T, P>*>(in + at0 * (int)sizeof(T));
-    const Vec<T, P> v1 = *reinterpret_cast<const Vec<T, P>*>(in + at1 * (int)sizeof(T));
+    const Vec<T, P> v0 = get<PAST, T, P>(in + at0 * (int)sizeof(T)), v1 = get<PAST, T, P>(in + at1 * (int)sizeof(T));
     if (!turned) {
-      *reinterpret_cast<Vec<T, P>*>(out + at0 * (int)sizeof(T)) = v0;
-      *reinterpret_cast<Vec<T, P>*>(out + at1 * (int)sizeof(T)) = v1;
+      put<PAST>(out + at0 * (int)sizeof(T), v0);
+      put<PAST>(out + at1 * (int)sizeof(T), v1);
       continue;
     }
     float x[2 * P], y[2 * P], lo[P], hi[P];
@@ -147,8 +175,8 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) { lo[i] = y[i]; hi[i] = y[P + i]; }
-    *reinterpret_cast<Vec<T, P>*>(out + at0 * (int)sizeof(T)) = narrow<T, P>(lo);
-    *reinterpret_cast<Vec<T, P>*>(out + at1 * (int)sizeof(T)) = narrow<T, P>(hi);
+    put<PAST>(out + at0 * (int)sizeof(T), narrow<T, P>(lo));
+    put<PAST>(out + at1 * (int)sizeof(T), narrow<T, P>(hi));
   }
 }
 
@@ -176,20 +204,25 @@ hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, c
   a.half = half;
   a.turned = half / pairs;
   a.chunks = a.turned + rest / (2 * pairs);
-  a.per_group = kRotThreads / a.chunks;
   a.streams = plan.streams;
   a.end0 = plan.stream_end[0];
   a.end1 = plan.stream_end[1];
   a.end2 = plan.stream_end[2];
   a.magnitude = plan.magnitude;
   a.sign = inverse ? -1.f : 1.f;
-  const int64_t groups = ((int64_t)a.rows + a.per_group - 1) / a.per_group;
-  const int heads = a.q.heads + a.k.heads;
-  a.heads_at_once = (int)std::min<int64_t>(heads, std::max<int64_t>(1, groups * heads / 2048));
-  const dim3 grid((unsigned)groups, (unsigned)((heads + a.heads_at_once - 1) / a.heads_at_once));
+  const int heads = a.q.heads + a.k.heads, places = kRotThreads / a.chunks;
+  const int64_t one_turn = ((int64_t)a.rows * heads + places - 1) / places;    // workgroups if every thread has a single head
+  // few tokens: all heads side by side, so that a step's launch is spread over the chip; else several turns of eight
+  a.abreast = std::min(std::min(heads, places), one_turn > 2048 ? 8 : heads);
+  a.turns = (int)std::max<int64_t>(1, std::min<int64_t>((heads + a.abreast - 1) / a.abreast, one_turn / 2048));
+  a.per_group = places / a.abreast;
+  const dim3 grid((unsigned)(((int64_t)a.rows + a.per_group - 1) / a.per_group), (unsigned)((heads + a.abreast * a.turns - 1) / (a.abreast * a.turns)));
   ProfileScope ps("rotary_kernel", s);
   auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a, plan); };
-#define FC_ROTARY(T, P) plan.interleaved ? launch(rotary_kernel<T, P, true>) : launch(rotary_kernel<T, P, false>)
+  const bool past = 2LL * a.rows * heads * q.head_dim * e > 256000000;         // (what is read and written exceeds the cache)
+#define FC_ROTARY(T, P)                                                                                                                        \
+  plan.interleaved ? (past ? launch(rotary_kernel<T, P, true, true>) : launch(rotary_kernel<T, P, true, false>))                               \
+                   : (past ? launch(rotary_kernel<T, P, false, true>) : launch(rotary_kernel<T, P, false, false>))
   if (q.dtype == FC_BF16) {
     if (pairs == 8) FC_ROTARY(uint16_t, 8);
     else if (pairs == 4) FC_ROTARY(uint16_t, 4);
