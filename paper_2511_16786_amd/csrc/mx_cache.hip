@@ -6,6 +6,7 @@
 // Bound by memory: a row of K and V is read once (4 D or 8 D bytes) and 17 D / 16 bytes are written.  Eight columns a lane, so that a row's
 // load is one run of 16-byte pieces (fp32: two), four lanes have a block in common and find its largest magnitude by two lane exchanges.
 #include <algorithm>
+#include <type_traits>
 
 #include "fc_common.h"
 #include "mx.h"
@@ -99,9 +100,11 @@ __device__ __forceinline__ void write_row(uint8_t* tile, int row, int part, cons
 struct RowsOf {                  // rows [B][R][D] with strides, and a slot for each
   int64_t sb, sr;
   const int64_t* slots;
-  __device__ __forceinline__ void where(int b, int64_t i, int64_t rows, int64_t num_slots, int64_t& from, int64_t& slot) const {
-    slot = slots[(int64_t)b * rows + i];
-    if (slot >= num_slots) slot = -1;
+  size_t lds_bytes() const { return 0; }
+  __device__ __forceinline__ void stage(int, int64_t*) const {}
+  __device__ __forceinline__ int64_t look(int b, int64_t i, int64_t rows) const { return slots[(int64_t)b * rows + i]; }
+  __device__ __forceinline__ void where(int b, int64_t i, int64_t seen, int64_t num_slots, const int64_t*, int64_t& from, int64_t& slot) const {
+    slot = seen < num_slots ? seen : -1;
     from = b * sb + i * sr;
   }
 };
@@ -112,18 +115,24 @@ struct KeptRows {                // kept rows of a cache [B][L][H][N][D], in the
   const int64_t* offsets;
   const int32_t* idx;
   const int32_t* table;
-  __device__ __forceinline__ void where(int b, int64_t i, int64_t rows, int64_t num_slots, int64_t& from, int64_t& slot) const {
+  size_t lds_bytes() const { return (size_t)(st.L + 1) * sizeof(int64_t) + (size_t)st.L * sizeof(int32_t); }
+  // the sequence's offsets and budgets in LDS (read from there by every row's search for its layer: 5 loads one after another)
+  __device__ __forceinline__ void stage(int b, int64_t* offs) const {
+    int32_t* const kept = reinterpret_cast<int32_t*>(offs + st.L + 1);
+    for (int l = threadIdx.x; l <= st.L; l += kMxThreads) offs[l] = offsets[(int64_t)b * (st.L + 1) + l];
+    for (int l = threadIdx.x; l < st.L; l += kMxThreads) kept[l] = budgets[(int64_t)b * st.L + l];
+  }
+  __device__ __forceinline__ int look(int b, int64_t i, int64_t rows) const { return idx[(int64_t)b * rows + i]; }
+  __device__ __forceinline__ void where(int b, int64_t i, int token, int64_t num_slots, const int64_t* offs, int64_t& from, int64_t& slot) const {
     slot = -1;
     from = 0;
-    const int64_t* offs = offsets + (int64_t)b * (st.L + 1);
-    const int token = idx[(int64_t)b * rows + i];
     if (token < 0 || token >= n || i < offs[0] || i >= offs[st.L]) return;
     int lo = 0, hi = st.L;                                 // largest l with offs[l] <= i
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (offs[mid] <= i) lo = mid; else hi = mid;
     }
-    const int k = budgets[(int64_t)b * st.L + lo];
+    const int k = reinterpret_cast<const int32_t*>(offs + st.L + 1)[lo];
     const int64_t in = i - offs[lo];
     if (k <= 0 || in >= (int64_t)st.H * k) return;
     const int h = (int)((uint32_t)in / (uint32_t)k), j = (int)(in - (int64_t)h * k), p = j / page_size;
@@ -143,9 +152,14 @@ __global__ __launch_bounds__(kMxThreads) void mx_store_kernel(const char* __rest
   __shared__ int64_t from[kMxThreads], to[kMxThreads];
   const int b = blockIdx.y, tid = threadIdx.x;
   const int64_t first = (int64_t)blockIdx.x * share;
+  extern __shared__ int64_t staged[];
+  src.stage(b, staged);
+  const bool mine = tid < share && first + tid < rows;
+  const auto seen = mine ? src.look(b, first + tid, rows) : -1;
+  if constexpr (!std::is_same<Source, RowsOf>::value) __syncthreads();
   if (tid < share) {
     int64_t f = 0, s = -1;
-    if (first + tid < rows) src.where(b, first + tid, rows, num_slots, f, s);
+    if (mine) src.where(b, first + tid, seen, num_slots, staged, f, s);
     from[tid] = f;
     to[tid] = s < 0 ? -1 : (s >> 4) * (MxTile<D>::kBytes * 16) + (s & 15);     // the tile's place, and the row in its last four bits
   }
@@ -223,7 +237,7 @@ hipError_t store(const void* K, const void* V, const Source& src, int B, int64_t
   const dim3 grid((unsigned)((rows + share - 1) / share), (unsigned)B);
   ProfileScope ps(name, s);
   auto launch = [&](auto kern) {
-    hipLaunchKernelGGL(kern, grid, dim3(kMxThreads), 0, s, static_cast<const char*>(K), static_cast<const char*>(V), src, rows, share,
+    hipLaunchKernelGGL(kern, grid, dim3(kMxThreads), src.lds_bytes(), s, static_cast<const char*>(K), static_cast<const char*>(V), src, rows, share,
                        num_slots, static_cast<uint8_t*>(pages));
   };
   if (dtype == FC_BF16) d == 128 ? launch(mx_store_kernel<128, uint16_t, Source>) : launch(mx_store_kernel<64, uint16_t, Source>);
