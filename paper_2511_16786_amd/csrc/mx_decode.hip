@@ -8,10 +8,12 @@
 //   output:  A = probabilities (head c16, rows 4 g4 + i of both tiles of a step: as the scores come out), B = V (the same rows, column
 //            D / 16 c16 + t for output tile t).  Probabilities are three bf16 terms, 24 bits: with two the result is off by 1e-6.
 //
-// Work is shared out by steps of 32 rows over all units at once: every wave has an equal run of the launch's steps, whichever units they belong
-// to, so that none waits for a long layer.  Budgets are on the device; every wave sums them up by itself.  A unit within a wave's run is
-// finished there; parts of units (reference, sum, weighted V) meet in LDS once all waves of a workgroup are through, and what belongs to
-// units of several workgroups is merged by a second kernel: piece w + u of the workspace, no two alike since both only grow along the steps.
+// A workgroup has a piece of one unit, in steps of 32 rows of which each of its waves takes a quarter; the waves merge in LDS, the pieces of a
+// unit in a second kernel.  Budgets are on the device, so that every wave finds out by itself how many pieces the layers make and which of
+// them is its own.  A unit's piece is never shared with another unit's: equal runs of steps over all units at once, whichever they
+// belong to, leave no workgroup waiting, but most of them then have two units, load twice from nothing and write two pieces (512 units
+// of 3600 rows 58 us, a workgroup each 48; 448 of 300 rows 18.6 and 9.8).  A single kernel whose last workgroup merges would need a
+// release of the L2 by each of them: 155 us instead of 30.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -25,11 +27,10 @@ namespace {
 
 constexpr int kMxdThreads = 256, kMxdWaves = 4;
 constexpr int kAhead = 2;              // steps of rows under way in a wave
-constexpr int kLeastSteps = 4;         // of a workgroup, where there are enough
-constexpr int kMostGroups = 1024;
-// Waves that a SIMD holds by the registers of each form, and as many workgroups a compute unit, which all are resident: more of them wait for each
-// other's startup (28 layers of 4 heads that keep 6554 rows: 768 workgroups 32 us, 1024 36, 1536 39), fewer leave memory waiting.
-constexpr int waves_held(int d, int terms) { return (d == 64 ? 4 : 3) - (terms > 1 ? 1 : 0); }
+constexpr int kLeastSteps = 4;         // of a piece
+// Waves that a SIMD holds by the registers of each form, and as many workgroups a compute unit, which all are resident together.  (With one step
+// under way and four workgroups in place of three: 28 layers of 4 heads that keep 6554 rows 29.2 us, 28.2 so.)
+constexpr int waves_held(int d, int terms) { return d == 64 ? 4 : terms > 1 ? 2 : 3; }
 constexpr int kMostRows = (1 << 25) - 1;
 constexpr float kSlack = 16.f;         // how far scores (in log2) may exceed the running reference before it is moved
 
@@ -48,11 +49,12 @@ struct MxdArgs {
   int layers, H, G;              // (layers of all sequences)
   int page_tiles, max_pages;
   int64_t num_pages;
-  int groups;                    // workgroups of the launch
+  int groups;                    // pieces that the launch aims at
+  bool whole;                    // a workgroup for each unit
   float scale_log2e, limit_scale;        // of scores, above 0; its reciprocal
   bool negate;                           // the scale is negative: queries change their signs
   float* pieces;
-  int2* span;                    // first and last workgroup of each unit
+  int2* span;                    // first piece of each unit and how many it has
   float* out;
 };
 
@@ -110,6 +112,14 @@ __device__ __forceinline__ int rows_at(const MxdArgs& a, int bl) {
 }
 __device__ __forceinline__ int steps_of(int rows) { return (rows + 31) >> 5; }
 
+// Steps of a piece, for a launch of `all` steps: as many pieces as stay resident together, a part of one more for each unit among them; where
+// there are more units than that, pieces twice as long as a unit on average, so that only the longest are cut.
+__host__ __device__ inline int most_pieces(int groups, int units) { return groups > units + units / 2 ? groups : units + units / 2; }
+__device__ __forceinline__ int steps_a_piece(int all, int groups, int units) {
+  const int pieces = max(1, most_pieces(groups, units) - units);
+  return max(kLeastSteps, all / pieces + (all % pieces != 0));
+}
+
 // A step's codes and scales of one lane.
 template <int D> struct Step {
   static constexpr int kWords = D / 32;
@@ -123,77 +133,63 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
   typedef MxTile<D> Tile;
   constexpr int KW = D / 32;             // dwords of K and of V a lane and tile; 32-column products of a score
   constexpr int VT = D / 16;             // output tiles
-  extern __shared__ __align__(16) float parts[];       // [2 kMxdWaves][piece_floats]: the first and the last unit of each wave's run, if it has a part of them
-  __shared__ int part_unit[2 * kMxdWaves], part_ends[2 * kMxdWaves];   // -1: none; bit 0: the unit's first rows, bit 1: its last
+  extern __shared__ __align__(16) float parts[];       // [kMxdWaves][piece_floats]
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c16 = lane & 15, g4 = lane >> 4, G = a.G;
   const int w = blockIdx.x, part_floats = (int)piece_floats(G, D);
-  if (lane < 2) part_unit[2 * wave + lane] = -1;
-
-  // ---- steps of all layers, each head of which has as many (the sum over all units fits 31 bits: mx_decode_reach)
-  constexpr int kChunks = 8;             // 64 layers each, whose rows are under way together and stay in registers
-  int held[kChunks];
-  auto load_rows = [&](int base) {
+  int bl = 0, h = 0, rows = 0, piece = 0, pieces = 1;    // layer, head and rows of the unit; which of its pieces
+  if (a.whole) {
+    bl = w / a.H;
+    h = w - bl * a.H;
+    rows = uniform(rows_at(a, bl));
+  } else {
+    // steps and pieces of all layers, each head of which has as many (all units' steps fit 31 bits: mx_decode_reach)
+    constexpr int kChunks = 8;           // 64 layers each, whose rows are under way together and stay in registers
+    int held[kChunks];
+    auto load_rows = [&](int base) {
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j < a.layers ? rows_at(a, min(base + 64 * j + lane, a.layers - 1)) : 0;
+      for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j < a.layers ? rows_at(a, min(base + 64 * j + lane, a.layers - 1)) : 0;
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j + lane < a.layers ? held[j] : -1;      // (-1: no layer)
-  };
-  int total = 0;
-  for (int base = 0; base < a.layers; base += 64 * kChunks) {
-    load_rows(base);
-    int sum = 0;
+      for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j + lane < a.layers ? held[j] : 0;
+    };
+    int total = 0;
+    for (int base = 0; base < a.layers; base += 64 * kChunks) {
+      load_rows(base);
+      int sum = 0;
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-      sum += steps_of(max(held[j], 0));
-      // zeros for layers without rows, a workgroup's share of them
-      if (wave == 0 && __ballot(held[j] == 0)) {
-        uint64_t none = __ballot(held[j] == 0 && (base + 64 * j + lane) % a.groups == w);
-        for (; none; none &= none - 1) {
-          float4v* const out = reinterpret_cast<float4v*>(a.out + (size_t)(base + 64 * j + __builtin_ctzll(none)) * a.H * G * D);
-          for (int i = lane; i < a.H * G * (D / 4); i += 64) out[i] = float4v{0.f, 0.f, 0.f, 0.f};
-        }
-      }
+      for (int j = 0; j < kChunks; ++j) sum += steps_of(held[j]);
+      total += __builtin_amdgcn_readlane(wave_scan(sum), 63);
     }
-    total += __builtin_amdgcn_readlane(wave_scan(sum), 63);
-  }
-  // ---- this wave's, and the unit that they begin in
-  const int all = total * a.H, groups = min(a.groups, (all + kLeastSteps - 1) / kLeastSteps);
-  if (w >= groups) return;
-  const int runs = groups * kMxdWaves, run = w * kMxdWaves + wave, each = all / runs, over = all - each * runs;
-  int at = run * each + min(run, over);
-  const int end = at + each + (run < over ? 1 : 0);
-  int bl = 0, h = 0, s = 0, rows = 0, steps = 1;
-  if (at < end) {
-    const int in_heads = at / a.H;
-    int before = 0, base = 0;
-    for (bool found = false; !found; base += 64 * kChunks) {
+    const int each = steps_a_piece(total * a.H, a.groups, a.layers * a.H), in_heads = w / a.H;
+    int before = 0;
+    bool found = false;
+    for (int base = 0; base < a.layers && !found; base += 64 * kChunks) {
       if (a.layers > 64 * kChunks) load_rows(base);
 #pragma unroll
       for (int j = 0; j < kChunks; ++j) {
         if (!found && base + 64 * j < a.layers) {
-          const int upto = wave_scan(steps_of(max(held[j], 0))), chunk = __builtin_amdgcn_readlane(upto, 63);
+          const int mine = (steps_of(held[j]) + each - 1) / each;
+          const int upto = wave_scan(mine), chunk = __builtin_amdgcn_readlane(upto, 63);
           if (before + chunk > in_heads) {
             found = true;
             const int owner = __builtin_ctzll(__ballot(before + upto > in_heads));
             bl = base + 64 * j + owner;
             rows = __builtin_amdgcn_readlane(held[j], owner);
-            steps = steps_of(rows);
-            const int place = at - (before + __builtin_amdgcn_readlane(upto, owner) - steps) * a.H;
-            h = place / steps;
-            s = place - h * steps;
+            pieces = __builtin_amdgcn_readlane(mine, owner);
+            const int place = w - (before + __builtin_amdgcn_readlane(upto, owner) - pieces) * a.H;
+            h = place / pieces;
+            piece = place - h * pieces;
           }
           before += chunk;
         }
       }
     }
+    if (!found) return;
   }
-
-  // ---- one unit after another
-  int part = 2 * wave;
-  while (at < end) {
-    const int unit = bl * a.H + h;
-    const int n = min(steps - s, end - at), s0 = s, s1 = s + n;
-
+  const int unit = bl * a.H + h, steps = steps_of(rows);
+  const int share = steps / pieces, over = steps - share * pieces, first = piece * share + min(piece, over), n = share + (piece < over ? 1 : 0);
+  const int s0 = first + n * wave / kMxdWaves, s1 = first + n * (wave + 1) / kMxdWaves;
+  if (!a.whole && piece == 0 && tid == 0) a.span[unit] = int2{w, pieces};
+  {
     // queries: head c16 (zeros beyond G), columns D / 4 g4 + 8 i .. + 7
     uint32_t q[QTERMS][KW][4];
 #pragma unroll
@@ -202,7 +198,7 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
       for (int i = 0; i < KW; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[t][i][j] = 0u;
-    if (c16 < G) {
+    if (c16 < G && s0 < s1) {
       const size_t at_q = ((size_t)unit * G + c16) * D + g4 * (D / 4);
       if constexpr (QTERMS == 1) {
         const uint32_t flip = a.negate ? 0x80008000u : 0u;
@@ -255,7 +251,7 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
       const int32_t id = entries[min(page0 + lane, a.max_pages - 1)];
       return id >= 0 && id < a.num_pages ? id * a.page_tiles : -1;
     };
-    int32_t entry = lookup();
+    int32_t entry = s0 < s1 ? lookup() : -1;
     auto load_step = [&](Step<D>& x) {
       x.missing = 0;
 #pragma unroll
@@ -393,7 +389,7 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
     };
     // kAhead steps under way; a step's registers are filled again in place.  (Loads without conditions, behind the wave's last step of that
     // step's last tile again: where a load may or may not have been made the next wait is for all of them.)
-    {
+    if (s0 < s1) {
       Step<D> x[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) load_step(x[i]);
@@ -409,115 +405,69 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
     // the four lanes of a head add their sums
     ls += __shfl_xor(ls, 16, 64);
     ls += __shfl_xor(ls, 32, 64);
-    if (n == steps) {
+    float* const mine = parts + wave * part_floats;
+    if (g4 == 0 && c16 < G) { mine[G * D + c16] = m; mine[G * D + G + c16] = ls; }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float lt = __shfl(ls, 4 * g4 + i, 64), share = lt == 0.f ? 0.f : 1.f / lt;     // (1 and more, if there is a row at all)
-        if (4 * g4 + i < G)
+    for (int i = 0; i < 4; ++i)
+      if (4 * g4 + i < G)
 #pragma unroll
-          for (int t = 0; t < VT; t += 4)
-            *reinterpret_cast<float4v*>(a.out + ((size_t)unit * G + 4 * g4 + i) * D + VT * c16 + t) =
-                float4v{out[t][i] * share, out[t + 1][i] * share, out[t + 2][i] * share, out[t + 3][i] * share};
-      }
-      if (lane == 0) a.span[unit] = int2{w, w};
-    } else {
-      float* const mine = parts + part * part_floats;
-      if (g4 == 0 && c16 < G) { mine[G * D + c16] = m; mine[G * D + G + c16] = ls; }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (4 * g4 + i < G)
-#pragma unroll
-          for (int t = 0; t < VT; t += 4)
-            *reinterpret_cast<float4v*>(mine + (4 * g4 + i) * D + VT * c16 + t) =
-                float4v{out[t][i], out[t + 1][i], out[t + 2][i], out[t + 3][i]};
-      if (lane == 0) {
-        part_unit[part] = unit;
-        part_ends[part] = (s == 0 ? 1 : 0) | (s1 == steps ? 2 : 0);
-      }
-      ++part;
-    }
-    // on to the next unit that has rows
-    at += n;
-    s = 0;
-    if (at < end && ++h == a.H) {
-      h = 0;
-      do {
-        ++bl;
-        rows = uniform(rows_at(a, bl));
-      } while (rows == 0);
-      steps = steps_of(rows);
-    }
+        for (int t = 0; t < VT; t += 4)
+          *reinterpret_cast<float4v*>(mine + (4 * g4 + i) * D + VT * c16 + t) = float4v{out[t][i], out[t + 1][i], out[t + 2][i], out[t + 3][i]};
   }
   __syncthreads();
 
-  // ---- parts of one unit, one a wave at most and next to each other, become one in their order
-  const int units_of = lane < 2 * kMxdWaves ? part_unit[lane] : -1, ends_of = lane < 2 * kMxdWaves ? part_ends[lane] : 0;
-  uint32_t left = (uint32_t)__ballot(units_of >= 0);
-  while (left) {
-    const int unit = __builtin_amdgcn_readlane(units_of, __builtin_ctz(left));
-    uint32_t same = (uint32_t)__ballot(units_of == unit);
-    left &= ~same;
-    const bool begins = __ballot(units_of == unit && (ends_of & 1)), ends = __ballot(units_of == unit && (ends_of & 2));
-    int from[kMxdWaves];                 // (the first again, without weight, where there are fewer)
-    bool have[kMxdWaves];
+  // the waves' parts, in their order
+  float* const record = a.pieces + (size_t)w * part_floats;
+  for (int item = tid; item < G * D / 4; item += kMxdThreads) {         // four columns
+    const int g = item / (D / 4);
+    float m[kMxdWaves], l[kMxdWaves], top = -INFINITY;
+    float4v o[kMxdWaves];
 #pragma unroll
     for (int v = 0; v < kMxdWaves; ++v) {
-      have[v] = same != 0;
-      from[v] = (have[v] ? __builtin_ctz(same) * part_floats : from[0]);
-      same &= same - 1;
+      const float* const one = parts + v * part_floats;
+      m[v] = one[G * D + g];
+      l[v] = one[G * D + G + g];
+      o[v] = *reinterpret_cast<const float4v*>(one + 4 * item);
+      top = fmaxf(top, m[v]);
     }
-    float* const piece = a.pieces + (size_t)(w + unit) * part_floats;
-    for (int item = tid; item < G * D / 4; item += kMxdThreads) {       // four columns
-      const int g = item / (D / 4);
-      float m[kMxdWaves], l[kMxdWaves], top = -INFINITY;
-      float4v o[kMxdWaves];
+    const float ref = top > -INFINITY ? top : 0.f;         // (none has a finite score: zeros, or NaN)
+    float4v acc = {0.f, 0.f, 0.f, 0.f};
+    float lt = 0.f;
 #pragma unroll
-      for (int v = 0; v < kMxdWaves; ++v) {
-        m[v] = parts[from[v] + G * D + g];
-        l[v] = parts[from[v] + G * D + G + g];
-        o[v] = *reinterpret_cast<const float4v*>(parts + from[v] + 4 * item);
-        top = fmaxf(top, m[v]);
-      }
-      const float ref = top > -INFINITY ? top : 0.f;       // (none has a finite score: zeros, or NaN)
-      float4v acc = {0.f, 0.f, 0.f, 0.f};
-      float lt = 0.f;
+    for (int v = 0; v < kMxdWaves; ++v) {
+      const float wt = __builtin_amdgcn_exp2f(m[v] - ref);
 #pragma unroll
-      for (int v = 0; v < kMxdWaves; ++v)
-        if (have[v]) {
-          const float wt = __builtin_amdgcn_exp2f(m[v] - ref);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[i] = fmaf(o[v][i], wt, acc[i]);
-          lt = fmaf(l[v], wt, lt);
-        }
-      if (begins && ends) {
-        const float share = lt == 0.f ? 0.f : 1.f / lt;
-        *reinterpret_cast<float4v*>(a.out + (size_t)unit * G * D + 4 * item) = acc * share;
-      } else {
-        *reinterpret_cast<float4v*>(piece + 4 * item) = acc;
-        if (4 * item % D == 0) { piece[G * D + g] = top; piece[G * D + G + g] = lt; }
-      }
+      for (int i = 0; i < 4; ++i) acc[i] = fmaf(o[v][i], wt, acc[i]);
+      lt = fmaf(l[v], wt, lt);
     }
-    if (tid == 0) {
-      if (begins) a.span[unit].x = w;
-      if (ends) a.span[unit].y = w;
+    if (pieces == 1) {
+      const float part = lt == 0.f ? 0.f : 1.f / lt;       // (1 and more, if there is a row at all)
+      *reinterpret_cast<float4v*>(a.out + (size_t)unit * G * D + 4 * item) = acc * part;
+    } else {
+      *reinterpret_cast<float4v*>(record + 4 * item) = acc;
+      if (4 * item % D == 0) { record[G * D + g] = top; record[G * D + G + g] = lt; }
     }
   }
 }
 
-// out[unit][g][:] of units that several workgroups had a piece of.  grid = (slices of the heads, units); `sets` groups of d threads have
+// out[unit][g][:] of units of several pieces, and zeros for those without rows.  grid = (slices of the heads, units); `sets` groups of d threads have
 // kAtOnce pieces each at a time, all of them under way together.
 constexpr int kAtOnce = 8;
 __global__ void mx_decode_merge_kernel(MxdArgs a, int d, int heads) {
   extern __shared__ float lds[];                           // [sets][3][d]: largest reference, sum, weighted sum
   const int unit = blockIdx.y, dim = threadIdx.x % d, set = threadIdx.x / d, sets = blockDim.x / d, G = a.G;
-  if (rows_at(a, unit / a.H) == 0) return;
+  const int g0 = blockIdx.x * heads, g1 = min(G, g0 + heads);
   const int2 span = a.span[unit];
-  if (span.x == span.y) return;                            // (written by its workgroup)
+  if (rows_at(a, unit / a.H) == 0) {
+    for (int g = g0 + set; g < g1; g += sets) a.out[((size_t)unit * G + g) * d + dim] = 0.f;
+    return;
+  }
+  if (span.y <= 1) return;                                 // (written by its workgroup)
   const size_t stride = piece_floats(G, d);
-  const int first = min(max(span.x, 0), a.groups - 1), n = min(max(span.y, first), a.groups - 1) - first + 1;
-  const float* const base = a.pieces + (size_t)(first + unit) * stride;
-  const int g1 = min(G, (int)(blockIdx.x + 1) * heads);
-  for (int g = blockIdx.x * heads; g < g1; ++g) {
+  // (within the workspace whatever it holds)
+  const int most = most_pieces(a.groups, a.layers * a.H), first = min(max(span.x, 0), most - 1), n = min(span.y, most - first);
+  const float* const base = a.pieces + (size_t)first * stride;
+  for (int g = g0; g < g1; ++g) {
     float top = -INFINITY, acc = 0.f, lt = 0.f;
     for (int i0 = set * kAtOnce; i0 < n; i0 += sets * kAtOnce) {
       float m[kAtOnce], l[kAtOnce], o[kAtOnce];
@@ -545,7 +495,7 @@ __global__ void mx_decode_merge_kernel(MxdArgs a, int d, int heads) {
     }
     if (sets > 1) {
       float* const mine = lds + (size_t)set * 3 * d + dim;
-      if (g > (int)blockIdx.x * heads) __syncthreads();    // (the head before is still being read)
+      if (g > g0) __syncthreads();    // (the head before is still being read)
       mine[0] = top;
       mine[d] = lt;
       mine[2 * d] = acc;
@@ -575,8 +525,9 @@ bool mx_decode_reach(int64_t units, int64_t max_pages, int64_t page_size) {
   return units * ((std::min<int64_t>(kMostRows, max_pages * page_size) + 31) / 32) < (1ll << 31);
 }
 
-static size_t pieces_bytes(int units, int group, int d) {
-  return ((size_t)(units + kMostGroups) * piece_floats(group, d) * sizeof(float) + 15) / 16 * 16;
+constexpr int groups_held(int d, int dtype) { return 256 * waves_held(d, dtype == FC_BF16 ? 1 : 3); }
+static size_t pieces_bytes(int units, int group, int d) {               // (bf16's: they hold more)
+  return ((size_t)most_pieces(groups_held(d, FC_BF16), units) * piece_floats(group, d) * sizeof(float) + 15) / 16 * 16;
 }
 size_t mx_decode_workspace_bytes(int units, int group, int d) {
   return units == 0 ? 0 : pieces_bytes(units, group, d) + (size_t)units * sizeof(int2);
@@ -586,31 +537,31 @@ hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* tab
                             int B, int L, int H, int group, int d, int dtype, const int32_t* rows, float scale, float* out, void* ws,
                             hipStream_t s) {
   const int units = B * L * H;
-  // no more workgroups than the rows that tables and pages have room for make
-  const int64_t room = std::min((int64_t)units * (((int64_t)max_pages * page_size + 31) / 32), num_pages * (page_size / 16) + units);
-  const int held = 256 * waves_held(d, dtype == FC_BF16 ? 1 : 3), groups = (int)std::min<int64_t>(held, (room + kLeastSteps - 1) / kLeastSteps);
+  // Tables that reach no further than kWholeSteps, and more units than four rounds of workgroups: one for each unit, and no merge.  (4 units of 115, 460 and 921 rows 12.6, 12.0, 12.0 us with
+  // pieces of four steps, 9.8, 9.5, 10.0 whole; 64 units of 921 13.2 and 10.7, of 1843 15.2 and 15.7; 4 of 1843 12.3 and 15.2; 3584 of 1500 177 and 151,
+  // 1792 of 1500 83 and 80, of which a layer far longer than the others would keep a single workgroup busy.)
+  constexpr int64_t kWholeSteps = 32;
+  const int64_t reach = ((int64_t)max_pages * page_size + 31) / 32;
+  const int groups = groups_held(d, dtype);
+  const bool whole = reach <= kWholeSteps || units >= 4 * groups;
   // (a scale of zero: the smallest there is, which leaves all scores as alike as they can be told)
   const float positive = std::max(std::fabs(scale) * 1.4426950408889634f, 1.17549435e-38f);
-  const MxdArgs a{Q, static_cast<const uint8_t*>(pages), rows, table, B * L, H, group, page_size / 16, max_pages, num_pages, groups,
+  const MxdArgs a{Q, static_cast<const uint8_t*>(pages), rows, table, B * L, H, group, page_size / 16, max_pages, num_pages, groups, whole,
                   positive, std::min(1.f / positive, 3.4e38f), scale < 0.f, static_cast<float*>(ws),
                   reinterpret_cast<int2*>(static_cast<char*>(ws) + pieces_bytes(units, group, d)), out};
   {
     ProfileScope ps("mx_decode_partial_kernel", s);
-    const size_t lds = 2 * kMxdWaves * piece_floats(group, d) * sizeof(float);
-    hipError_t e = hipSuccess;
-    auto launch = [&](auto kern) {
-      if (lds > 65536)                                     // (16 query heads of 128 columns)
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-      if (e == hipSuccess) hipLaunchKernelGGL(kern, dim3(groups), dim3(kMxdThreads), lds, s, a);
-    };
+    // no more workgroups than the rows that the tables have room for make
+    const int grid = whole ? units : (int)std::min<int64_t>(most_pieces(groups, units), units * ((reach + kLeastSteps - 1) / kLeastSteps));
+    const size_t lds = kMxdWaves * piece_floats(group, d) * sizeof(float);
+    auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(grid), dim3(kMxdThreads), lds, s, a); };
     if (dtype == FC_BF16) d == 128 ? launch(mx_decode_partial_kernel<128, 1>) : launch(mx_decode_partial_kernel<64, 1>);
     else d == 128 ? launch(mx_decode_partial_kernel<128, 3>) : launch(mx_decode_partial_kernel<64, 3>);
-    if (e != hipSuccess) return e;
   }
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || groups == 1) return e;            // (no unit in two workgroups)
-  // pieces of a unit if all units are alike, and two more; a workgroup for each head where that is no more than a few thousand
-  const int sets = std::min(1024 / d, std::max(1, (groups / units + 2 + kAtOnce - 1) / kAtOnce));
+  if (e != hipSuccess || whole) return e;
+  // sets for the pieces of a unit if all units are alike; a workgroup for each head where that is no more than a few thousand
+  const int sets = std::min(1024 / d, std::max(1, (groups / units + kAtOnce - 1) / kAtOnce));
   const int heads = std::min(group, std::max(1, units * group / 2048)), slices = (group + heads - 1) / heads;
   ProfileScope ps("mx_decode_merge_kernel", s);
   hipLaunchKernelGGL(mx_decode_merge_kernel, dim3(slices, units), dim3(sets * d), (size_t)sets * 3 * d * sizeof(float), s, a, d, heads);
