@@ -502,11 +502,13 @@ def _mx_pages(pages: torch.Tensor, page_size: int, head_dim: int, index: int) ->
 
 
 def _mx_rows(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, index: int) -> FcRowsDesc:
-    strides = K.stride()
-    if K.dim() != 3 or K.shape != V.shape or strides != V.stride() or K.dtype is not V.dtype or V.get_device() != index:
+    if K.dim() != 3 or K.shape != V.shape or K.dtype is not V.dtype or V.get_device() != index:
         raise ValueError("K and V must have shape [B, R, d], the same strides, dtype and device")
     B, R, d = K.shape
-    if strides[2] != 1:
+    strides, others = K.stride(), V.stride()
+    if strides != others and any(n > 1 and s != o for n, s, o in zip(K.shape, strides, others)):
+        raise ValueError("K and V must have the same strides")
+    if strides[2] != 1 and d > 1:
         raise ValueError("the head dimension must be contiguous")
     _want(slots, "slots", torch.int64, (B, R), index)
     return FcRowsDesc(B, d, _dtype(K), 0, R, strides[0], strides[1])
@@ -657,7 +659,8 @@ class MxCache:
 
     Pure plumbing, as `Compressor`: buffers through torch, calls on the current stream, nothing read back.  Of `num_pages`
     pages the first ones are taken as rows come; `missing()` (synchronising) says how many were asked for beyond them.
-    A step is rotary (outside), append(k, v), attend(q), and may be captured into a graph."""
+    A step is rotary (outside), append(k, v), attend(q), and may be captured into a graph (after one eager attend, which
+    makes the workspace).  Calls of one cache have to follow each other: on one stream, or ordered by events."""
 
     def __init__(self, batch: int, layers: int, kv_heads: int, head_dim: int, page_size: int, max_pages: int,
                  num_pages: int, device="cuda"):
@@ -671,10 +674,24 @@ class MxCache:
         self.rows = torch.zeros((batch, layers), dtype=torch.int32, device=device)
         self.cursor = torch.zeros(1, dtype=torch.int64, device=device)
         self.slots = torch.empty((batch, layers * kv_heads), dtype=torch.int64, device=device)
-        self.workspace = None
+        self._workspaces = {}                # by query heads; kept, since captured graphs hold their addresses
+        self._empty = True
+
+    def reset(self) -> None:
+        """An empty cache again."""
+        self.block_table.fill_(-1)
+        self.rows.zero_()
+        self.cursor.zero_()
+        self._empty = True
 
     def fill(self, comp: Compressor, K: torch.Tensor, V: torch.Tensor) -> None:
         """The rows that `comp` (scored and allocated for this K, V) keeps, into the empty cache."""
+        B, L, H, d = self.shape
+        if comp.shape[:3] != (B, L, H) or comp.shape[4] != d:
+            raise ValueError("the compression is of another shape")
+        if not self._empty:
+            raise ValueError("fill takes an empty cache: reset() first")
+        self._empty = False
         assign_pages(self.rows, comp.budgets, self.page_size, self.block_table, self.cursor, num_free=self.num_pages)
         select_gather_mx(K, V, comp.desc, comp.scores, comp.budgets, comp.layer_offsets, comp.rows_per_seq, comp.idx,
                          self.block_table, self.page_size, self.pages, shared=comp.shared)
@@ -682,16 +699,25 @@ class MxCache:
     def append(self, k: torch.Tensor, v: torch.Tensor) -> None:
         """One row more for every unit: k, v [B, L, H, d] contiguous."""
         B, L, H, d = self.shape
+        if k.shape != self.shape or v.shape != self.shape:
+            raise ValueError("k and v must have shape [B, L, H, d]")
+        k, v = k.view(B, L * H, d), v.view(B, L * H, d)
+        self._empty = False
         assign_pages(self.rows, 1, self.page_size, self.block_table, self.cursor, num_free=self.num_pages, slots=self.slots)
-        mx_store(k.view(B, L * H, d), v.view(B, L * H, d), self.slots, self.pages, self.page_size)
+        mx_store(k, v, self.slots, self.pages, self.page_size)
 
     def attend(self, q: torch.Tensor, scale: float, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """q [B, L, Hq, d]; float32 [B, L, Hq, d]."""
         B, L, H, d = self.shape
-        if self.workspace is None:
-            self.workspace = torch.empty(max(_mx_decode_workspace(B, L, H, q.shape[2], d), 16), dtype=torch.uint8, device=q.device)
+        if q.dim() != 4 or q.shape[:2] != (B, L) or q.shape[3] != d:
+            raise ValueError("q must have shape [B, L, Hq, d]")
+        heads = q.shape[2]
+        workspace = self._workspaces.get(heads)
+        if workspace is None:
+            workspace = torch.empty(max(_mx_decode_workspace(B, L, H, heads, d), 16), dtype=torch.uint8, device=q.device)
+            self._workspaces[heads] = workspace
         return mx_decode_attention(q, self.pages, self.page_size, H, self.rows, self.block_table, scale, out=out,
-                                   workspace=self.workspace)
+                                   workspace=workspace)
 
     def missing(self) -> int:
         """Pages that were asked for and not there (their rows are not stored): reads the cursor back."""

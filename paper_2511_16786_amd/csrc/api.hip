@@ -430,6 +430,7 @@ fc_status flashcache_assign_pages(const int32_t* rows, const int32_t* add, int32
   if (misaligned(rows, 4) || misaligned(add, 4) || misaligned(free_pages, 4) || misaligned(block_table, 4) || misaligned(rows_out, 4) ||
       misaligned(cursor, 8) || misaligned(cursor_out, 8) || misaligned(slots, 8))
     return FC_EINVAL;
+  if (rows_out == add || rows_out == free_pages || block_table == rows || block_table == add || block_table == free_pages) return FC_EINVAL;
   hipError_t e = assign_pages_launch(rows, add, add_each, batch, layers, kv_heads, page_size, max_pages, free_pages, num_free, block_table,
                                      cursor, slots, slots_per_seq, rows_out, cursor_out, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? FC_OK : FC_EHIP;
@@ -454,7 +455,7 @@ static fc_status check_mx_rows(const fc_rows_desc* d, const void* K, const void*
   fc_status st = check_mx_pages(page_size, d->head_dim, num_pages);
   if (st != FC_OK) return st;
   const int64_t e = d->dtype == FC_BF16 ? 2 : 4;
-  if (d->stride_b < 0 || d->stride_r < 0 || (d->stride_b * e) % 16 || (d->stride_r * e) % 16) return FC_EINVAL;
+  if (d->stride_b < 0 || d->stride_r < 0 || (d->batch > 1 && (d->stride_b * e) % 16) || (d->rows > 1 && (d->stride_r * e) % 16)) return FC_EINVAL;
   if (d->batch > 65535 || d->rows > 0x7FFFFFFFll) return FC_EUNSUPPORTED;
   if (d->batch == 0 || d->rows == 0) return FC_OK;
   if (!K || !V || !slots || !pages) return FC_EINVAL;

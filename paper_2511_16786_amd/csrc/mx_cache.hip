@@ -134,7 +134,7 @@ struct KeptRows {                // kept rows of a cache [B][L][H][N][D], in the
     }
     const int k = reinterpret_cast<const int32_t*>(offs + st.L + 1)[lo];
     const int64_t in = i - offs[lo];
-    if (k <= 0 || in >= (int64_t)st.H * k) return;
+    if (k <= 0 || k > n || in >= (int64_t)st.H * k) return;      // (bad budgets; H * n is below 2^32)
     const int h = (int)((uint32_t)in / (uint32_t)k), j = (int)(in - (int64_t)h * k), p = j / page_size;
     if (p >= max_pages) return;
     const int64_t page = table[(((int64_t)b * st.L + lo) * st.H + h) * max_pages + p];

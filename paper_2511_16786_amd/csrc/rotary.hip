@@ -185,13 +185,16 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc
 hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, const void* Q, void* Q_out, const fc_heads_desc& q,
                          const void* K, void* K_out, const fc_heads_desc* k, bool inverse, hipStream_t s) {
   const int e = q.dtype == FC_BF16 ? 2 : 4, half = plan.rotary_dim / 2, rest = q.head_dim - plan.rotary_dim;
+  // (the step of an axis of one says nothing: left out, as it would count in what addresses are multiples of)
+  auto step = [&](int n, int64_t stride) { return n > 1 ? stride * e : 0; };
   auto side = [&](const void* in, void* out, const fc_heads_desc& d) {
-    return RotSide{static_cast<const char*>(in), static_cast<char*>(out), d.stride_b * e, d.stride_t * e, d.stride_h * e,
-                   d.out_stride_b * e, d.out_stride_t * e, d.out_stride_h * e, d.heads};
+    return RotSide{static_cast<const char*>(in), static_cast<char*>(out),
+                   step(d.batch, d.stride_b), step(d.tokens, d.stride_t), step(d.heads, d.stride_h),
+                   step(d.batch, d.out_stride_b), step(d.tokens, d.out_stride_t), step(d.heads, d.out_stride_h), d.heads};
   };
   RotArgs a{};
   a.q = side(Q, Q_out, q);
-  a.k = k ? side(K, K_out, *k) : RotSide{};
+  a.k = k && k->heads ? side(K, K_out, *k) : RotSide{};
   // the widest parts that every address is a multiple of
   uint64_t bits = 0;
   for (const RotSide* r : {&a.q, &a.k})

@@ -101,12 +101,14 @@ def test_rotary_refusals():
 def test_assign_pages_refusals():
     from paper_2511_16786_amd import binding as b
 
-    def call(rows=16, add=16, B=1, L=2, H=2, ps=16, most=4, free=16, n=8, cur=16, table=16, slots=16, per=8, ro=32, co=32):
+    def call(rows=48, add=16, B=1, L=2, H=2, ps=16, most=4, free=64, n=8, cur=16, table=80, slots=16, per=8, ro=32, co=32):
         return b._lib.flashcache_assign_pages(rows, add, 0, B, L, H, ps, most, free, n, cur, table, slots, per, ro, co, None)
     for bad in (dict(L=0), dict(H=0), dict(B=-1), dict(ps=0), dict(most=0), dict(n=-1), dict(per=-1), dict(rows=None), dict(cur=None),
                 dict(table=None), dict(ro=None), dict(co=None), dict(slots=None), dict(rows=18), dict(add=18), dict(free=18), dict(table=18),
                 dict(ro=18), dict(cur=20), dict(co=20), dict(slots=20)):
         assert call(**bad) == b.FC_EINVAL, bad
+    for bad in (dict(ro=16), dict(table=16), dict(free=16, ro=16)):                # outputs on inputs other than their own
+        assert call(**{**dict(rows=48, add=16, free=64, table=80), **bad}) == b.FC_EINVAL, bad
     for bad in (dict(L=1025), dict(ps=(1 << 25) + 1), dict(B=1024, L=33), dict(H=32768)):
         assert call(**bad) == b.FC_EUNSUPPORTED, bad
     assert call(B=0, rows=None, table=None) == b.FC_OK
@@ -167,7 +169,8 @@ def test_mx_decode_refusals_and_workspace():
                dict(rows=33), dict(table=34), dict(most=0), dict(n=0), dict(ps=0), dict(Hq=7), dict(Hq=0), dict(dtype=2), dict(B=-1), dict(L=0),
                dict(scale=float("nan"))):
         assert call(**kw) == b.FC_EINVAL, kw
-    for kw in (dict(Hq=34), dict(d=96), dict(d=256), dict(ps=40), dict(B=8192, L=4)):
+    for kw in (dict(Hq=34), dict(d=96), dict(d=256), dict(ps=40), dict(B=8192, L=4), dict(ps=1 << 25, most=1 << 10, B=1, L=2048, H=1, Hq=1),
+               dict(ps=64, n=1 << 30)):
         assert call(**kw) == b.FC_EUNSUPPORTED, kw
     need = size(1, 2, 2, 8, 128)
     assert need > 0 and call(ws=None) == b.FC_EWORKSPACE and call(ws=40) == b.FC_EWORKSPACE and call(wsb=need - 1) == b.FC_EWORKSPACE

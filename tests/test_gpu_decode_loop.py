@@ -315,6 +315,33 @@ def test_select_gather_mx(dtype, d, shared):
     assert torch.equal(pages, want)
 
 
+def test_select_gather_mx_leaves_out_layers_of_bad_budgets():
+    """A budget beyond the tokens selects and stores nothing, however large it is; the other layers are as they should be."""
+    fc = _fc()
+    rng = np.random.default_rng(77)
+    B, L, H, N, d, ps = 1, 3, 2, 100, 64, 16
+    K, V = _rand(rng, (B, L, H, N, d), torch.bfloat16), _rand(rng, (B, L, H, N, d), torch.bfloat16)
+    scores = torch.rand((B, L, H, N), device="cuda")
+    for wrong in (N + 1, 2 ** 31 - 1, -3):
+        budgets = torch.tensor([[20, wrong, 30]], dtype=torch.int32, device="cuda")
+        offs = torch.tensor([[0, 40, 60, 120]], dtype=torch.int64, device="cuda")
+        table = torch.arange(L * H * 7, dtype=torch.int32, device="cuda").view(B, L, H, 7)
+        pages = torch.full((L * H * 7, fc.mx_page_bytes(ps, d)), 3, dtype=torch.uint8, device="cuda")
+        idx = torch.full((1, 120), 5, dtype=torch.int32, device="cuda")
+        fc.select_gather_mx(K, V, fc.describe(K), scores, budgets, offs, 120, idx, table, ps, pages)
+        assert bool((pages[14:28] == 3).all()) and bool((idx[0, 40:60] == 5).all())
+        for l, k in ((0, 20), (2, 30)):
+            for h in range(H):
+                o = int(offs[0, l]) + h * k
+                want = torch.topk(scores[0, l, h], k).indices.sort().values.to(torch.int32)
+                assert torch.equal(idx[0, o:o + k], want)
+                slots = (int(table[0, l, h, 0]) * ps + torch.arange(k, device="cuda")).view(1, k)
+                Ko, Vo = torch.empty((1, k, d), device="cuda"), torch.empty((1, k, d), device="cuda")
+                fc.mx_load(slots, pages, ps, Ko, Vo)
+                assert np.array_equal(_f64(Ko)[0], dr.grid(K[0, l, h].float().cpu().numpy()[want.cpu().numpy()]))
+                assert np.array_equal(_f64(Vo)[0], dr.grid(V[0, l, h].float().cpu().numpy()[want.cpu().numpy()]))
+
+
 # ---- attention ------------------------------------------------------------------------------------
 def _cache(fc, rng, B, L, H, d, ps, rows, pool=None, sigma=1.0, dtype=torch.float32):
     """A cache whose units hold rows[b][l] rows in pages in any order; (pages, table, K, V [unit] in float64)."""
@@ -434,8 +461,13 @@ def test_mx_decode_attention_shared_pages_large_logits_and_nan():
 def test_mx_decode_attention_many_units_and_long_caches():
     fc = _fc()
     rng = np.random.default_rng(2)
-    # (units beyond the workgroups; a single unit of many)
-    for B, L, H, G, d, ps, rows in ((4, 200, 2, 2, 64, 16, rng.integers(0, 60, 800)), (1, 1, 1, 7, 128, 64, np.array([70001]))):
+    # (units beyond the workgroups; a single unit of many; more layers than a wave's registers hold, one far longer than the others;
+    # tables that reach 1024 rows and a page more)
+    long = rng.integers(0, 40, 700)
+    long[613] = 9000
+    for B, L, H, G, d, ps, rows in ((4, 200, 2, 2, 64, 16, rng.integers(0, 60, 800)), (1, 1, 1, 7, 128, 64, np.array([70001])),
+                                    (1, 700, 1, 1, 64, 16, long), (1, 3, 2, 4, 128, 16, np.array([1024, 1000, 0])),
+                                    (1, 3, 2, 4, 128, 16, np.array([1025, 7, 0]))):
         rows = rows.astype(np.int32).reshape(B, L)
         pages, table, Ks, Vs = _cache(fc, rng, B, L, H, d, ps, rows)
         Q = _rand(rng, (B, L, H * G, d), torch.bfloat16)
@@ -559,6 +591,46 @@ def test_cache_without_pages_left_keeps_what_it_has():
     Q = _rand(rng, (B, L, H * G, d), torch.bfloat16)
     _check_attend(cache.attend(Q, 0.1), Q, Ks, Vs, B, L, H, G, 0.1, keep)
     assert cache.missing() == 3
+
+
+def test_cache_is_filled_again_after_a_reset_and_takes_any_group():
+    fc = _fc()
+    rng = np.random.default_rng(34)
+    B, L, H, N, d, ps = 1, 2, 2, 300, 128, 16
+    cache = fc.MxCache(B, L, H, d, ps, -(-N // ps), B * L * H * (-(-N // ps)))
+    for turn in range(2):
+        comp, K, V = _compressed(fc, rng, B, L, H, N, d)
+        cache.fill(comp, K, V)
+        Ks, Vs = _history(comp, K, V, B, L, H, d)
+        for G in (1, 16, 5):
+            Q = _rand(rng, (B, L, H * G, d), torch.bfloat16)
+            _check_attend(cache.attend(Q, 0.1), Q, Ks, Vs, B, L, H, G, 0.1)
+        with pytest.raises(ValueError):
+            cache.fill(comp, K, V)
+        cache.reset()
+    other, K, V = _compressed(fc, rng, B, L, H, N, 64)
+    with pytest.raises(ValueError):
+        cache.fill(other, K, V)
+    with pytest.raises(ValueError):
+        cache.attend(_rand(rng, (B, L, H, 64), torch.bfloat16), 0.1)
+    with pytest.raises(ValueError):
+        cache.append(_rand(rng, (B, L, H + 1, d), torch.bfloat16), _rand(rng, (B, L, H + 1, d), torch.bfloat16))
+
+
+def test_strides_of_axes_of_one_do_not_matter():
+    fc = _fc()
+    rng = np.random.default_rng(35)
+    d, ps = 64, 16
+    wide = _rand(rng, (3, 7, 5 * d + 1), torch.bfloat16)
+    K, V = wide[:1, 2:3, :d], _rand(rng, (1, 1, d), torch.bfloat16)          # (strides of 321 and 2247 elements)
+    slots = torch.tensor([[9]], device="cuda")
+    pages = torch.zeros((1, fc.mx_page_bytes(ps, d)), dtype=torch.uint8, device="cuda")
+    if K.data_ptr() % 16:
+        K = K.clone().as_strided((1, 1, d), (2247, 321, 1))
+    fc.mx_store(K, V, slots, pages, ps)
+    Ko, Vo = torch.empty((1, 1, d), device="cuda"), torch.empty((1, 1, d), device="cuda").as_strided((1, 1, d), (77, 33, 1))
+    fc.mx_load(slots, pages, ps, Ko, Vo)
+    assert np.array_equal(_f64(Ko), dr.grid(K.float().cpu().numpy())) and np.array_equal(_f64(Vo), dr.grid(V.float().cpu().numpy()))
 
 
 def test_operators_on_two_streams_at_once():
