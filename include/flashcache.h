@@ -328,7 +328,7 @@ typedef struct {
  *   Q_out, K_out  device out, in the input dtype: sines, cosines and products in fp32, rounded once.  May be the inputs themselves
  *              (same strides); any other overlap gives unspecified values
  *   inverse    != 0: the transposed map, sin -> -sin: the gradient of the inputs from that of the outputs
- * Any even head_dim from rotary_dim to 512; pointers and strides that are multiples of 16 bytes are fastest. */
+ * Any even head_dim from rotary_dim to 512, fewer than 2^24 tokens of all sequences; pointers and strides that are multiples of 16 bytes are fastest. */
 fc_status flashcache_rotary(const fc_rotary_plan* plan, const int32_t* positions, const void* Q, void* Q_out,
                             const fc_heads_desc* q_desc, const void* K, void* K_out, const fc_heads_desc* k_desc,
                             int32_t inverse, void* hip_stream);
@@ -388,8 +388,8 @@ fc_status flashcache_select_gather_mx(const void* K, const void* V, const fc_kv_
  *   rows  device in, int32 [B][L].  Rows whose page entry is missing (negative, >= num_pages, from max_pages on) are not attended to; a unit
  *         without attended rows gives zeros
  *   workspace  device, 16-byte aligned, flashcache_mx_decode_workspace_bytes() bytes; calls that may run at the same time need one each
- * 1 to 16 query heads a KV head for both dtypes; tables that reach 2^36 rows in all of their units are refused (FC_EUNSUPPORTED).  Products of the cache's values (exact in bf16) on the matrix cores with queries and
- * probabilities of 24 bits, sums and softmax in fp32. */
+ * 1 to 16 query heads a KV head for both dtypes; tables that reach 2^36 rows in all of their units are refused (FC_EUNSUPPORTED).  The cache's
+ * values are exact in bf16 and multiply queries and probabilities of 24 bits on the matrix cores; sums and softmax are in fp32. */
 size_t flashcache_mx_decode_workspace_bytes(int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads, int32_t head_dim);
 fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const int32_t* block_table, int32_t page_size,
                                          int32_t max_pages, int64_t num_pages, int32_t batch, int32_t layers,

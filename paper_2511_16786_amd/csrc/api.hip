@@ -382,7 +382,8 @@ static fc_status check_heads(const fc_rotary_plan& plan, const fc_heads_desc& d,
   if (d.head_dim > 512) return FC_EUNSUPPORTED;
   if (d.stride_b < 0 || d.stride_t < 0 || d.stride_h < 0) return FC_EINVAL;
   if (d.out_stride_b < 0 || d.out_stride_t < 0 || d.out_stride_h < 0) return FC_EINVAL;
-  if ((int64_t)d.batch * d.tokens > 0x7FFFFFFFll || d.heads > 65535) return FC_EUNSUPPORTED;
+  // (a workgroup of 256 threads has a token at least, and a launch fewer than 2^32 threads)
+  if ((int64_t)d.batch * d.tokens >= (1 << 24) || d.heads > 65535) return FC_EUNSUPPORTED;
   if ((int64_t)d.batch * d.tokens * d.heads == 0) return FC_OK;
   const uintptr_t e = d.dtype == FC_BF16 ? 2 : 4;
   if (!in || !out || reinterpret_cast<uintptr_t>(in) % e || reinterpret_cast<uintptr_t>(out) % e) return FC_EINVAL;
@@ -400,7 +401,7 @@ fc_status flashcache_rotary(const fc_rotary_plan* plan, const int32_t* positions
                             const fc_heads_desc* q_desc, const void* K, void* K_out, const fc_heads_desc* k_desc,
                             int32_t inverse, void* hip_stream) {
   if (!plan || !q_desc || plan->magic != kWsMagic) return FC_EINVAL;
-  if (plan->rotary_dim < 2 || plan->rotary_dim > 2 * FC_ROTARY_MAX_PAIRS || plan->streams < 1 || plan->streams > 4) return FC_EINVAL;
+  if (plan->rotary_dim < 2 || plan->rotary_dim % 2 || plan->rotary_dim > 2 * FC_ROTARY_MAX_PAIRS || plan->streams < 1 || plan->streams > 4) return FC_EINVAL;
   fc_status st = check_heads(*plan, *q_desc, Q, Q_out);
   if (st != FC_OK) return st;
   if (k_desc) {

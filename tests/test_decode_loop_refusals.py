@@ -93,6 +93,11 @@ def test_rotary_refusals():
     assert call(_heads(b, out_stride_h=32)) == b.FC_EINVAL                         # heads of the output on one another
     assert call(_heads(b, out_stride_t=512), Q=64, Qo=64) == b.FC_EINVAL           # in place with other strides
     assert call(_heads(b, B=1 << 20, T=1 << 20)) == b.FC_EUNSUPPORTED
+    assert call(_heads(b, B=1 << 12, T=1 << 12)) == b.FC_EUNSUPPORTED               # 2^24 tokens
+    odd = b.FcRotaryPlan()
+    ctypes.pointer(odd)[0] = plan
+    odd.rotary_dim = 63
+    assert call(plan=odd) == b.FC_EINVAL
     assert call(k=_heads(b, T=2)) == b.FC_EINVAL and call(k=_heads(b, dtype=0)) == b.FC_EINVAL and call(k=_heads(b), K=None) == b.FC_EINVAL
     assert call(_heads(b, B=0), Q=None, Qo=None, pos=None) == b.FC_OK
     assert call(_heads(b, T=0), Q=None, Qo=None, pos=None) == b.FC_OK
