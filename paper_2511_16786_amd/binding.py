@@ -532,6 +532,15 @@ def mx_load(slots: torch.Tensor, pages: torch.Tensor, page_size: int, K_out: tor
                                    V_out.data_ptr(), _stream()), "flashcache_mx_load")
 
 
+def _described(K: torch.Tensor, V: torch.Tensor, desc: FcKvDesc, index: int) -> None:
+    shape = (desc.batch, desc.layers, desc.kv_heads, desc.n_tokens, desc.head_dim)
+    strides = (desc.stride_b, desc.stride_l, desc.stride_h, desc.stride_n, 1)
+    for t in (K, V):
+        if t.shape != shape or _dtype(t) != desc.dtype or t.get_device() != index or any(
+                n > 1 and s != o for n, s, o in zip(shape, strides, t.stride())):
+            raise ValueError("K and V must be what the descriptor describes")
+
+
 def select_gather_mx(K: torch.Tensor, V: torch.Tensor, desc: FcKvDesc, scores: torch.Tensor, budgets: torch.Tensor,
                      layer_offsets: torch.Tensor, rows_per_seq: int, idx_out: torch.Tensor, block_table: torch.Tensor,
                      page_size: int, pages: torch.Tensor, shared: bool = False) -> None:
@@ -539,8 +548,7 @@ def select_gather_mx(K: torch.Tensor, V: torch.Tensor, desc: FcKvDesc, scores: t
     index = _here(K, "K")
     n = _mx_pages(pages, page_size, desc.head_dim, index)
     B, L, H, N = desc.batch, desc.layers, desc.kv_heads, desc.n_tokens
-    if V.shape != K.shape or V.stride() != K.stride() or V.dtype is not K.dtype or V.get_device() != index:
-        raise ValueError("K and V must agree in shape, strides, dtype and device")
+    _described(K, V, desc, index)
     _want(scores, "scores", torch.float32, (B, L, H, N), index)
     _want(budgets, "budgets", torch.int32, (B, L), index)
     _want(layer_offsets, "layer_offsets", torch.int64, (B, L + 1), index)
@@ -691,6 +699,7 @@ class MxCache:
             raise ValueError("the compression is of another shape")
         if not self._empty:
             raise ValueError("fill takes an empty cache: reset() first")
+        _described(K, V, comp.desc, _here(K, "K"))
         self._empty = False
         assign_pages(self.rows, comp.budgets, self.page_size, self.block_table, self.cursor, num_free=self.num_pages)
         select_gather_mx(K, V, comp.desc, comp.scores, comp.budgets, comp.layer_offsets, comp.rows_per_seq, comp.idx,
@@ -702,6 +711,10 @@ class MxCache:
         if k.shape != self.shape or v.shape != self.shape:
             raise ValueError("k and v must have shape [B, L, H, d]")
         k, v = k.view(B, L * H, d), v.view(B, L * H, d)
+        # (what the store would refuse, before the rows are counted)
+        _mx_rows(k, v, self.slots, _here(k, "k"))
+        if (k.data_ptr() | v.data_ptr()) % 16:
+            raise ValueError("k and v must be aligned to 16 bytes")
         self._empty = False
         assign_pages(self.rows, 1, self.page_size, self.block_table, self.cursor, num_free=self.num_pages, slots=self.slots)
         mx_store(k, v, self.slots, self.pages, self.page_size)

@@ -617,6 +617,32 @@ def test_cache_is_filled_again_after_a_reset_and_takes_any_group():
         cache.append(_rand(rng, (B, L, H + 1, d), torch.bfloat16), _rand(rng, (B, L, H + 1, d), torch.bfloat16))
 
 
+def test_refused_rows_are_not_counted():
+    """What fill and append refuse leaves the cache as it was."""
+    fc = _fc()
+    rng = np.random.default_rng(36)
+    B, L, H, N, d, ps = 1, 2, 2, 200, 64, 16
+    comp, K, V = _compressed(fc, rng, B, L, H, N, d)
+    cache = fc.MxCache(B, L, H, d, ps, -(-N // ps) + 1, 64)
+    held = cache.rows.clone(), cache.cursor.clone(), cache.block_table.clone()
+    odd = torch.zeros(B * L * H * d + 4, dtype=torch.bfloat16, device="cuda")[4:].view(B, L, H, d)     # off by 8 bytes
+    k = odd.clone()
+    with pytest.raises(ValueError):
+        cache.fill(comp, K[:, :, :, :N - 8], V[:, :, :, :N - 8])             # fewer tokens than the descriptor has
+    with pytest.raises(ValueError):
+        cache.fill(comp, K, V.transpose(1, 2).contiguous().transpose(1, 2))  # other strides
+    with pytest.raises(ValueError):
+        cache.fill(comp, K.float(), V.float())
+    for bad in ((k.half(), k.half()), (odd, k), (k, odd), (k, k.float()), (k.cpu(), k.cpu())):
+        with pytest.raises(ValueError):
+            cache.append(*bad)
+    for t, s in zip((cache.rows, cache.cursor, cache.block_table), held):
+        assert torch.equal(t, s)
+    cache.fill(comp, K, V)
+    cache.append(k, k)
+    assert torch.equal(cache.rows, comp.budgets + 1)
+
+
 def test_strides_of_axes_of_one_do_not_matter():
     fc = _fc()
     rng = np.random.default_rng(35)
