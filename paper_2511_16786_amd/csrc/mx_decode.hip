@@ -189,231 +189,229 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
   const int share = steps / pieces, over = steps - share * pieces, first = piece * share + min(piece, over), n = share + (piece < over ? 1 : 0);
   const int s0 = first + n * wave / kMxdWaves, s1 = first + n * (wave + 1) / kMxdWaves;
   if (!a.whole && piece == 0 && tid == 0) a.span[unit] = int2{w, pieces};
-  {
-    // queries: head c16 (zeros beyond G), columns D / 4 g4 + 8 i .. + 7
-    uint32_t q[QTERMS][KW][4];
+  // queries: head c16 (zeros beyond G), columns D / 4 g4 + 8 i .. + 7
+  uint32_t q[QTERMS][KW][4];
 #pragma unroll
-    for (int t = 0; t < QTERMS; ++t)
+  for (int t = 0; t < QTERMS; ++t)
+#pragma unroll
+    for (int i = 0; i < KW; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[t][i][j] = 0u;
+  if (c16 < G && s0 < s1) {
+    const size_t at_q = ((size_t)unit * G + c16) * D + g4 * (D / 4);
+    if constexpr (QTERMS == 1) {
+      const uint32_t flip = a.negate ? 0x80008000u : 0u;
+#pragma unroll
+      for (int i = 0; i < KW; ++i) {
+        const u32x4 u = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.Q) + at_q + 8 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[0][i][j] = u[j] ^ flip;
+      }
+    } else {
 #pragma unroll
       for (int i = 0; i < KW; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[t][i][j] = 0u;
-    if (c16 < G && s0 < s1) {
-      const size_t at_q = ((size_t)unit * G + c16) * D + g4 * (D / 4);
-      if constexpr (QTERMS == 1) {
-        const uint32_t flip = a.negate ? 0x80008000u : 0u;
+        for (int j = 0; j < 4; ++j) {
+          const float2v x = *reinterpret_cast<const float2v*>(static_cast<const float*>(a.Q) + at_q + 8 * i + 2 * j);
+          float x0 = a.negate ? -x[0] : x[0], x1 = a.negate ? -x[1] : x[1];
 #pragma unroll
-        for (int i = 0; i < KW; ++i) {
-          const u32x4 u = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.Q) + at_q + 8 * i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) q[0][i][j] = u[j] ^ flip;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < KW; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2v x = *reinterpret_cast<const float2v*>(static_cast<const float*>(a.Q) + at_q + 8 * i + 2 * j);
-            float x0 = a.negate ? -x[0] : x[0], x1 = a.negate ? -x[1] : x[1];
-#pragma unroll
-            for (int t = 0; t < QTERMS; ++t) {
-              // (the first two cut off, so that nothing overflows to infinity; the last to nearest)
-              const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
-              if (t == QTERMS - 1) {
-                q[t][i][j] = pack_bf16(x0, x1);
-              } else {
-                q[t][i][j] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
-                x0 -= __uint_as_float(u0 & 0xFFFF0000u);
-                x1 -= __uint_as_float(u1 & 0xFFFF0000u);
-              }
+          for (int t = 0; t < QTERMS; ++t) {
+            // (the first two cut off, so that nothing overflows to infinity; the last to nearest)
+            const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+            if (t == QTERMS - 1) {
+              q[t][i][j] = pack_bf16(x0, x1);
+            } else {
+              q[t][i][j] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+              x0 -= __uint_as_float(u0 & 0xFFFF0000u);
+              x1 -= __uint_as_float(u1 & 0xFFFF0000u);
             }
           }
-      }
+        }
     }
+  }
 
-    // reference of head c16 (the same in its four lanes), in log2 units, and this lane's sum; the product from which on the reference is moved
-    float m = -INFINITY, ref = 0.f, ls = 0.f, limit = -INFINITY;
-    float4v out[VT];
+  // reference of head c16 (the same in its four lanes), in log2 units, and this lane's sum; the product from which on the reference is moved
+  float m = -INFINITY, ref = 0.f, ls = 0.f, limit = -INFINITY;
+  float4v out[VT];
 #pragma unroll
-    for (int t = 0; t < VT; ++t) out[t] = float4v{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < VT; ++t) out[t] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    const int32_t* const entries = a.table + (int64_t)unit * a.max_pages;
-    const int last_tile = min((rows + 15) >> 4, 2 * s1);
-    const uint32_t k_off = Tile::k_code(c16, g4 * (D / 8)), v_off = Tile::v_code(4 * g4, c16);
-    const uint32_t ks_off = Tile::k_scale(c16, g4 * (D / 4) / 32), vs_off = Tile::v_scale(4 * g4, c16 * (D / 16) / 32);
-    // The tile to be loaded next, its page and its place there.  Lane i holds the first tile of page page0 + i of the table (-1: it has none), so
-    // that no load waits for a lookup.
-    int tile = 2 * s0, in_page, page;    // (page: counted from page0)
-    int page0 = uniform(tile / a.page_tiles);
-    in_page = tile - page0 * a.page_tiles;
-    page = 0;
-    auto lookup = [&]() -> int32_t {
-      const int32_t id = entries[min(page0 + lane, a.max_pages - 1)];
-      return id >= 0 && id < a.num_pages ? id * a.page_tiles : -1;
-    };
-    int32_t entry = s0 < s1 ? lookup() : -1;
-    auto load_step = [&](Step<D>& x) {
-      x.missing = 0;
+  const int32_t* const entries = a.table + (int64_t)unit * a.max_pages;
+  const int last_tile = min((rows + 15) >> 4, 2 * s1);
+  const uint32_t k_off = Tile::k_code(c16, g4 * (D / 8)), v_off = Tile::v_code(4 * g4, c16);
+  const uint32_t ks_off = Tile::k_scale(c16, g4 * (D / 4) / 32), vs_off = Tile::v_scale(4 * g4, c16 * (D / 16) / 32);
+  // The tile to be loaded next, its page and its place there.  Lane i holds the first tile of page page0 + i of the table (-1: it has none), so
+  // that no load waits for a lookup.
+  int tile = 2 * s0, in_page, page;    // (page: counted from page0)
+  int page0 = uniform(tile / a.page_tiles);
+  in_page = tile - page0 * a.page_tiles;
+  page = 0;
+  auto lookup = [&]() -> int32_t {
+    const int32_t id = entries[min(page0 + lane, a.max_pages - 1)];
+    return id >= 0 && id < a.num_pages ? id * a.page_tiles : -1;
+  };
+  int32_t entry = s0 < s1 ? lookup() : -1;
+  auto load_step = [&](Step<D>& x) {
+    x.missing = 0;
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const int first_tile = __builtin_amdgcn_readlane(entry, page);
-        x.missing |= first_tile;                           // (negative if either is)
-        x.gone[tt] = first_tile;
-        // (the cache's first tiles in place of those that have no page: masked)
-        const uint8_t* const at_tile = a.pages + (uint64_t)(uint32_t)(max(first_tile, 0) + in_page) * Tile::kBytes;
-        if (tile + 1 < last_tile) {                        // (behind the last tile it comes again)
-          ++tile;
-          if (++in_page == a.page_tiles) {
-            in_page = 0;
-            if (++page == 64) {
-              page0 += 64;
-              page = 0;
-              entry = lookup();
-              asm volatile("" : "+v"(entry));              // (waited for here, not before every use)
-            }
+    for (int tt = 0; tt < 2; ++tt) {
+      const int first_tile = __builtin_amdgcn_readlane(entry, page);
+      x.missing |= first_tile;                           // (negative if either is)
+      x.gone[tt] = first_tile;
+      // (the cache's first tiles in place of those that have no page: masked)
+      const uint8_t* const at_tile = a.pages + (uint64_t)(uint32_t)(max(first_tile, 0) + in_page) * Tile::kBytes;
+      if (tile + 1 < last_tile) {                        // (behind the last tile it comes again)
+        ++tile;
+        if (++in_page == a.page_tiles) {
+          in_page = 0;
+          if (++page == 64) {
+            page0 += 64;
+            page = 0;
+            entry = lookup();
+            asm volatile("" : "+v"(entry));              // (waited for here, not before every use)
           }
         }
-        if constexpr (D == 128) {
-          const u32x4 k = load_past<u32x4>(at_tile + k_off), v = load_past<u32x4>(at_tile + v_off);
-#pragma unroll
-          for (int i = 0; i < KW; ++i) { x.k[tt][i] = k[i]; x.v[tt][i] = v[i]; }
-        } else {
-          const u32x2 k = load_past<u32x2>(at_tile + k_off), v = load_past<u32x2>(at_tile + v_off);
-#pragma unroll
-          for (int i = 0; i < KW; ++i) { x.k[tt][i] = k[i]; x.v[tt][i] = v[i]; }
-        }
-        x.ks[tt] = load_past<uint8_t>(at_tile + ks_off);
-        x.vs[tt] = load_past<uint32_t>(at_tile + vs_off);
       }
-    };
-    auto work = [&](int st, Step<D>& x) {
-      float sc[2][4];
+      if constexpr (D == 128) {
+        const u32x4 k = load_past<u32x4>(at_tile + k_off), v = load_past<u32x4>(at_tile + v_off);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const float unit_k = __uint_as_float(x.ks[tt] << 23);
-        float4v acc = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < KW; ++i) { x.k[tt][i] = k[i]; x.v[tt][i] = v[i]; }
+      } else {
+        const u32x2 k = load_past<u32x2>(at_tile + k_off), v = load_past<u32x2>(at_tile + v_off);
 #pragma unroll
-        for (int i = 0; i < KW; ++i) {
-          uint32_t kv[4];
-          eight_values(x.k[tt][i], unit_k, kv);
-          const bf16x8 ka = as_bf16x8(kv[0], kv[1], kv[2], kv[3]);
-#pragma unroll
-          for (int t = QTERMS - 1; t >= 0; --t)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, as_bf16x8(q[t][i][0], q[t][i][1], q[t][i][2], q[t][i][3]), acc, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sc[tt][i] = acc[i];
+        for (int i = 0; i < KW; ++i) { x.k[tt][i] = k[i]; x.v[tt][i] = v[i]; }
       }
-      const int rb = 32 * st + 4 * g4;
-      if (x.missing < 0 || 32 * st + 32 > rows) {              // (the same for the wave)
+      x.ks[tt] = load_past<uint8_t>(at_tile + ks_off);
+      x.vs[tt] = load_past<uint32_t>(at_tile + vs_off);
+    }
+  };
+  auto work = [&](int st, Step<D>& x) {
+    float sc[2][4];
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
+    for (int tt = 0; tt < 2; ++tt) {
+      const float unit_k = __uint_as_float(x.ks[tt] << 23);
+      float4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (rb + 16 * tt + i >= rows || x.gone[tt] < 0) {
-              sc[tt][i] = -INFINITY;
-              x.vs[tt] = (x.vs[tt] & ~(0xFFu << (8 * i))) | (127u << (8 * i));     // (no NaN from a row that is not there)
-            }
+      for (int i = 0; i < KW; ++i) {
+        uint32_t kv[4];
+        eight_values(x.k[tt][i], unit_k, kv);
+        const bf16x8 ka = as_bf16x8(kv[0], kv[1], kv[2], kv[3]);
+#pragma unroll
+        for (int t = QTERMS - 1; t >= 0; --t)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, as_bf16x8(q[t][i][0], q[t][i][1], q[t][i][2], q[t][i][3]), acc, 0, 0, 0);
       }
-      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      if (__ballot(mx > limit)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m, mx * a.scale_log2e), alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
-        m = m_new;
-        limit = (m + kSlack) * a.limit_scale;
-        ref = m > -INFINITY ? m : 0.f;
-        ls *= alpha;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float a_i = __shfl(alpha, 4 * g4 + i, 64);
-#pragma unroll
-          for (int t = 0; t < VT; ++t) out[t][i] *= a_i;
-        }
-      }
-      uint32_t hi[4], mid[4], lo[4];
+      for (int i = 0; i < 4; ++i) sc[tt][i] = acc[i];
+    }
+    const int rb = 32 * st + 4 * g4;
+    if (x.missing < 0 || 32 * st + 32 > rows) {              // (the same for the wave)
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          float p0 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i], a.scale_log2e, -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i + 1], a.scale_log2e, -ref));
-          ls += p0;
-          ls += p1;
-          const int w2 = 2 * tt + i / 2;
-          hi[w2] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
-          p0 = less_low(p0, hi[w2]);
-          p1 = less_high(p1, hi[w2]);
-          mid[w2] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
-          lo[w2] = pack_bf16(less_low(p0, mid[w2]), less_high(p1, mid[w2]));
-        }
-      const bf16x8 ph = as_bf16x8(hi[0], hi[1], hi[2], hi[3]), pm = as_bf16x8(mid[0], mid[1], mid[2], mid[3]),
-                   pl = as_bf16x8(lo[0], lo[1], lo[2], lo[3]);
-      float unit_v[2][4];
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        // (the conversion looks at the exponent alone)
-        unit_v[tt][0] = __uint_as_float(x.vs[tt] << 23);
-        unit_v[tt][1] = __uint_as_float(x.vs[tt] << 15);
-        unit_v[tt][2] = __uint_as_float(x.vs[tt] << 7);
-        unit_v[tt][3] = __uint_as_float(x.vs[tt] >> 1);
-      }
-      // byte c of a row's D / 32 bytes has the columns of output tiles 2 c and 2 c + 1
-      auto tiles_of = [&](auto byte) {
-        constexpr int c = decltype(byte)::value;
-        uint32_t r[2][4];
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (D == 128) r[tt][i] = two_values<c>(x.v[tt][i], unit_v[tt][i]);
-            else r[tt][i] = i & 1 ? two_values<c + 2>(x.v[tt][i / 2], unit_v[tt][i]) : two_values<c>(x.v[tt][i / 2], unit_v[tt][i]);
+        for (int i = 0; i < 4; ++i)
+          if (rb + 16 * tt + i >= rows || x.gone[tt] < 0) {
+            sc[tt][i] = -INFINITY;
+            x.vs[tt] = (x.vs[tt] & ~(0xFFu << (8 * i))) | (127u << (8 * i));     // (no NaN from a row that is not there)
           }
+    }
+    float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                     fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+    if (__ballot(mx > limit)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float m_new = fmaxf(m, mx * a.scale_log2e), alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+      m = m_new;
+      limit = (m + kSlack) * a.limit_scale;
+      ref = m > -INFINITY ? m : 0.f;
+      ls *= alpha;
 #pragma unroll
-        for (int o = 0; o < 2; ++o) {
-          const uint32_t sel = o ? 0x07060302u : 0x05040100u;
-          const bf16x8 vb = as_bf16x8(__builtin_amdgcn_perm(r[0][1], r[0][0], sel), __builtin_amdgcn_perm(r[0][3], r[0][2], sel),
-                                      __builtin_amdgcn_perm(r[1][1], r[1][0], sel), __builtin_amdgcn_perm(r[1][3], r[1][2], sel));
-          float4v acc = out[2 * c + o];
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph, vb, acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pm, vb, acc, 0, 0, 0);
-          out[2 * c + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, vb, acc, 0, 0, 0);
-        }
-      };
-      tiles_of(std::integral_constant<int, 0>{});
-      tiles_of(std::integral_constant<int, 1>{});
-      if constexpr (D == 128) {
-        tiles_of(std::integral_constant<int, 2>{});
-        tiles_of(std::integral_constant<int, 3>{});
-      }
-    };
-    // kAhead steps under way; a step's registers are filled again in place.  (Loads without conditions, behind the wave's last step of that
-    // step's last tile again: where a load may or may not have been made the next wait is for all of them.)
-    if (s0 < s1) {
-      Step<D> x[kAhead];
+      for (int i = 0; i < 4; ++i) {
+        const float a_i = __shfl(alpha, 4 * g4 + i, 64);
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) load_step(x[i]);
-      for (int st = s0; st < s1; st += kAhead) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          if (st + i < s1) work(st + i, x[i]);
-          load_step(x[i]);
-        }
+        for (int t = 0; t < VT; ++t) out[t][i] *= a_i;
       }
     }
-
-    // the four lanes of a head add their sums
-    ls += __shfl_xor(ls, 16, 64);
-    ls += __shfl_xor(ls, 32, 64);
-    float* const mine = parts + wave * part_floats;
-    if (g4 == 0 && c16 < G) { mine[G * D + c16] = m; mine[G * D + G + c16] = ls; }
+    uint32_t hi[4], mid[4], lo[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * g4 + i < G)
+    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < VT; t += 4)
-          *reinterpret_cast<float4v*>(mine + (4 * g4 + i) * D + VT * c16 + t) = float4v{out[t][i], out[t + 1][i], out[t + 2][i], out[t + 3][i]};
+      for (int i = 0; i < 4; i += 2) {
+        float p0 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i], a.scale_log2e, -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i + 1], a.scale_log2e, -ref));
+        ls += p0;
+        ls += p1;
+        const int w2 = 2 * tt + i / 2;
+        hi[w2] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+        p0 = less_low(p0, hi[w2]);
+        p1 = less_high(p1, hi[w2]);
+        mid[w2] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+        lo[w2] = pack_bf16(less_low(p0, mid[w2]), less_high(p1, mid[w2]));
+      }
+    const bf16x8 ph = as_bf16x8(hi[0], hi[1], hi[2], hi[3]), pm = as_bf16x8(mid[0], mid[1], mid[2], mid[3]),
+                 pl = as_bf16x8(lo[0], lo[1], lo[2], lo[3]);
+    float unit_v[2][4];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      // (the conversion looks at the exponent alone)
+      unit_v[tt][0] = __uint_as_float(x.vs[tt] << 23);
+      unit_v[tt][1] = __uint_as_float(x.vs[tt] << 15);
+      unit_v[tt][2] = __uint_as_float(x.vs[tt] << 7);
+      unit_v[tt][3] = __uint_as_float(x.vs[tt] >> 1);
+    }
+    // byte c of a row's D / 32 bytes has the columns of output tiles 2 c and 2 c + 1
+    auto tiles_of = [&](auto byte) {
+      constexpr int c = decltype(byte)::value;
+      uint32_t r[2][4];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (D == 128) r[tt][i] = two_values<c>(x.v[tt][i], unit_v[tt][i]);
+          else r[tt][i] = i & 1 ? two_values<c + 2>(x.v[tt][i / 2], unit_v[tt][i]) : two_values<c>(x.v[tt][i / 2], unit_v[tt][i]);
+        }
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const uint32_t sel = o ? 0x07060302u : 0x05040100u;
+        const bf16x8 vb = as_bf16x8(__builtin_amdgcn_perm(r[0][1], r[0][0], sel), __builtin_amdgcn_perm(r[0][3], r[0][2], sel),
+                                    __builtin_amdgcn_perm(r[1][1], r[1][0], sel), __builtin_amdgcn_perm(r[1][3], r[1][2], sel));
+        float4v acc = out[2 * c + o];
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph, vb, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pm, vb, acc, 0, 0, 0);
+        out[2 * c + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, vb, acc, 0, 0, 0);
+      }
+    };
+    tiles_of(std::integral_constant<int, 0>{});
+    tiles_of(std::integral_constant<int, 1>{});
+    if constexpr (D == 128) {
+      tiles_of(std::integral_constant<int, 2>{});
+      tiles_of(std::integral_constant<int, 3>{});
+    }
+  };
+  // kAhead steps under way; a step's registers are filled again in place.  (Loads without conditions, behind the wave's last step of that
+  // step's last tile again: where a load may or may not have been made the next wait is for all of them.)
+  if (s0 < s1) {
+    Step<D> x[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load_step(x[i]);
+    for (int st = s0; st < s1; st += kAhead) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (st + i < s1) work(st + i, x[i]);
+        load_step(x[i]);
+      }
+    }
   }
+
+  // the four lanes of a head add their sums
+  ls += __shfl_xor(ls, 16, 64);
+  ls += __shfl_xor(ls, 32, 64);
+  float* const mine = parts + wave * part_floats;
+  if (g4 == 0 && c16 < G) { mine[G * D + c16] = m; mine[G * D + G + c16] = ls; }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (4 * g4 + i < G)
+#pragma unroll
+      for (int t = 0; t < VT; t += 4)
+        *reinterpret_cast<float4v*>(mine + (4 * g4 + i) * D + VT * c16 + t) = float4v{out[t][i], out[t + 1][i], out[t + 2][i], out[t + 3][i]};
   __syncthreads();
 
   // the waves' parts, in their order
@@ -537,9 +535,10 @@ hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* tab
                             int B, int L, int H, int group, int d, int dtype, const int32_t* rows, float scale, float* out, void* ws,
                             hipStream_t s) {
   const int units = B * L * H;
-  // Tables that reach no further than kWholeSteps, and more units than four rounds of workgroups: one for each unit, and no merge.  (4 units of 115, 460 and 921 rows 12.6, 12.0, 12.0 us with
-  // pieces of four steps, 9.8, 9.5, 10.0 whole; 64 units of 921 13.2 and 10.7, of 1843 15.2 and 15.7; 4 of 1843 12.3 and 15.2; 3584 of 1500 177 and 151,
-  // 1792 of 1500 83 and 80, of which a layer far longer than the others would keep a single workgroup busy.)
+  // Tables that reach no further than kWholeSteps, and more units than four rounds of workgroups: one for each unit, and no merge.  (4 units of
+  // 115, 460 and 921 rows 12.6, 12.0, 12.0 us with pieces of four steps, 9.8, 9.5, 10.0 whole; 64 units of 921 13.2 and 10.7, of 1843 15.2 and
+  // 15.7; 4 of 1843 12.3 and 15.2; 3584 of 1500 177 and 151.  1792 of 1500 are 83 and 80, but a layer far longer than the others would keep a
+  // single workgroup busy.)
   constexpr int64_t kWholeSteps = 32;
   const int64_t reach = ((int64_t)max_pages * page_size + 31) / 32;
   const int groups = groups_held(d, dtype);
