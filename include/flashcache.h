@@ -361,7 +361,7 @@ fc_status flashcache_assign_pages(const int32_t* rows, const int32_t* add, int32
  * whatever the memory holds; they may be read, and no attention reads rows from the given number on. */
 size_t flashcache_mx_page_bytes(int32_t page_size, int32_t head_dim);   /* 0 if unsupported */
 
-/* Rows of K and of V: row r of sequence b begins at base + b*stride_b + r*stride_r elements. */
+/* Rows of K and of V: row r of sequence b begins at base + b*stride_b + r*stride_r elements.  Fewer than 2^29 rows. */
 typedef struct {
   int32_t batch, head_dim, dtype, reserved;
   int64_t rows, stride_b, stride_r;
@@ -377,7 +377,7 @@ fc_status flashcache_mx_load(const int64_t* slots, const void* pages, int32_t pa
                              const fc_rows_desc* desc, void* K, void* V, void* hip_stream);
 
 /* flashcache_select_gather_paged into a 4-bit cache: selection and idx_out as there (shared: as its shared mode), kept row j of a unit goes to
- * slot j % page_size of page block_table[b][l][h][j / page_size]. */
+ * slot j % page_size of page block_table[b][l][h][j / page_size].  Fewer than 2^29 rows a sequence. */
 fc_status flashcache_select_gather_mx(const void* K, const void* V, const fc_kv_desc* desc, const float* scores,
                                       const int32_t* budgets, const int64_t* layer_offsets, int64_t rows_per_seq,
                                       int32_t shared, int32_t* idx_out, const int32_t* block_table, int32_t page_size,

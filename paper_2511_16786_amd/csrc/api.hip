@@ -457,7 +457,8 @@ static fc_status check_mx_rows(const fc_rows_desc* d, const void* K, const void*
   if (st != FC_OK) return st;
   const int64_t e = d->dtype == FC_BF16 ? 2 : 4;
   if (d->stride_b < 0 || d->stride_r < 0 || (d->batch > 1 && (d->stride_b * e) % 16) || (d->rows > 1 && (d->stride_r * e) % 16)) return FC_EINVAL;
-  if (d->batch > 65535 || d->rows > 0x7FFFFFFFll) return FC_EUNSUPPORTED;
+  // (a workgroup of 256 threads has 32 rows, and a launch fewer than 2^32 threads)
+  if (d->batch > 65535 || d->rows >= (1 << 29)) return FC_EUNSUPPORTED;
   if (d->batch == 0 || d->rows == 0) return FC_OK;
   if (!K || !V || !slots || !pages) return FC_EINVAL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(pages) || (reinterpret_cast<uintptr_t>(slots) & 7u)) return FC_EINVAL;
@@ -491,7 +492,7 @@ fc_status flashcache_select_gather_mx(const void* K, const void* V, const fc_kv_
   if (max_pages < 1) return FC_EINVAL;
   st = check_mx_pages(page_size, desc->head_dim, num_pages);
   if (st != FC_OK) return st;
-  if ((int64_t)desc->kv_heads * desc->n_tokens > 0xFFFFFFFFll || desc->batch > 65535) return FC_EUNSUPPORTED;
+  if ((int64_t)desc->kv_heads * desc->n_tokens > 0xFFFFFFFFll || desc->batch > 65535 || rows_per_seq >= (1 << 29)) return FC_EUNSUPPORTED;
   if (!block_table || (reinterpret_cast<uintptr_t>(block_table) & 3u)) return FC_EINVAL;
   if (desc->batch > 0 && rows_per_seq > 0 && (!pages || !aligned16(pages))) return FC_EINVAL;
   st = select_gather_common(K, V, desc, scores, budgets, layer_offsets, rows_per_seq, shared != 0, idx_out, nullptr, nullptr, nullptr, 0, 0,

@@ -144,6 +144,7 @@ def test_mx_store_and_load_refusals():
         for over in (dict(batch=-1), dict(rows=-1), dict(dtype=3), dict(stride_r=132), dict(stride_b=-8), dict(head_dim=0)):
             assert call(desc(**over)) == b.FC_EINVAL, (name, over)
         assert call(ps=24) == b.FC_EUNSUPPORTED and call(desc(head_dim=96)) == b.FC_EUNSUPPORTED
+        assert call(desc(rows=1 << 29)) == b.FC_EUNSUPPORTED
         assert call(desc(batch=65536)) == b.FC_EUNSUPPORTED and call(n=1 << 31) == b.FC_EUNSUPPORTED
         assert call(desc(rows=0), K=None, slots=None) == b.FC_OK and call(desc(batch=0), K=None) == b.FC_OK
     assert call(desc(stride_r=64)) == b.FC_EINVAL                                  # rows of the output on one another
@@ -159,6 +160,7 @@ def test_select_gather_mx_refusals():
     for kw in (dict(K=None), dict(table=None), dict(pages=None), dict(table=33), dict(pages=40), dict(most=0), dict(n=0), dict(rows=-1),
                dict(rows=257), dict(idx=None), dict(d=12)):
         assert call(**kw) == b.FC_EINVAL, kw
+    assert call(rows=1 << 29) == b.FC_EUNSUPPORTED
     assert call(d=96) == b.FC_EUNSUPPORTED and call(ps=20) == b.FC_EUNSUPPORTED
     assert call(rows=0, K=None, pages=None) == b.FC_OK and call(B=0, K=None) == b.FC_OK
 

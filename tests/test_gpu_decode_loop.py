@@ -248,6 +248,57 @@ def test_mx_store_and_load(dtype, d, ps, B, R):
     assert np.array_equal(_f64(Ko).reshape(-1, d), wk, equal_nan=True) and np.array_equal(_f64(Vo).reshape(-1, d), wv, equal_nan=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,B,R", [(64, 1, 66005), (64, 3, 22011), (128, 1, 33003), (128, 2, 17001)])
+def test_mx_store_and_load_of_many_rows_equal_those_of_few(dtype, d, B, R):
+    """Large calls take several rows for each group of lanes, small ones (tested above against the oracle) one."""
+    fc = _fc()
+    g = torch.Generator(device="cuda").manual_seed(R)
+    dt, ps = _dt(dtype), 48
+    n_pages = -(-B * R // ps) + 1
+    K, V = (torch.randn((B, R, d), generator=g, device="cuda").mul_(3.0).to(dt) for _ in range(2))
+    slots = torch.randperm(n_pages * ps, generator=g, device="cuda")[:B * R].view(B, R).contiguous()
+    slots[:, ::97] = -1
+    slots[:, 5::1001] = n_pages * ps
+    pages, want = (torch.full((n_pages, fc.mx_page_bytes(ps, d)), 5, dtype=torch.uint8, device="cuda") for _ in range(2))
+    Ko, Vo, Kw, Vw = (torch.full((B, R + 1, d), 7.0, dtype=dt, device="cuda") for _ in range(4))     # a row behind the last one
+    fc.mx_store(K, V, slots, pages, ps)
+    fc.mx_load(slots, pages, ps, Ko[:, :R], Vo[:, :R])
+    for b in range(B):
+        for r in range(0, R, 3001):
+            part = slots[b:b + 1, r:r + 3001].contiguous()
+            rows = slice(r, r + part.shape[1])
+            fc.mx_store(K[b:b + 1, rows], V[b:b + 1, rows], part, want, ps)
+            fc.mx_load(part, want, ps, Kw[b:b + 1, rows], Vw[b:b + 1, rows])
+    assert torch.equal(pages, want) and torch.equal(Ko, Kw) and torch.equal(Vo, Vw)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+def test_select_gather_mx_of_many_rows_equals_the_packed_rows_stored(dtype, d):
+    fc = _fc()
+    rng = np.random.default_rng(d + 5)
+    B, L, H, N, ps = 1, 3, 3, 9000, 64
+    dt = _dt(dtype)
+    K, V = (torch.from_numpy(rng.standard_normal((B, L, H, N, d), dtype=np.float32)).to(dt).cuda() for _ in range(2))
+    comp = fc.Compressor(K, 600, fc.total_budget(L, N, 0.83))
+    comp.run(K, V)
+    assert comp.rows_per_seq > 2048 * 2048 // d                      # (groups of 16 rows of 128 columns, 32 of 64)
+    most = -(-N // ps)
+    table = torch.full((B, L, H, most), -1, dtype=torch.int32, device="cuda")
+    rows, cursor = torch.zeros((B, L), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    pool = B * L * H * most
+    slots = torch.empty((B, comp.rows_per_seq), dtype=torch.int64, device="cuda")
+    free = torch.from_numpy(rng.permutation(pool).astype(np.int32)).cuda()
+    fc.assign_pages(rows, comp.budgets, ps, table, cursor, free_pages=free, slots=slots)
+    pages, want = (torch.full((pool, fc.mx_page_bytes(ps, d)), 3, dtype=torch.uint8, device="cuda") for _ in range(2))
+    idx = torch.full_like(comp.idx, -5)
+    fc.select_gather_mx(K, V, comp.desc, comp.scores, comp.budgets, comp.layer_offsets, comp.rows_per_seq, idx, table, ps, pages)
+    assert torch.equal(idx, comp.idx)
+    for r in range(0, comp.rows_per_seq, 20011):
+        fc.mx_store(comp.K_out[:, r:r + 20011], comp.V_out[:, r:r + 20011], slots[:, r:r + 20011].contiguous(), want, ps)
+    assert torch.equal(pages, want)
+
+
 def test_mx_blocks_with_values_that_are_not_finite():
     fc = _fc()
     x = torch.ones((1, 4, 128), device="cuda")
