@@ -8,11 +8,14 @@
 // fp32 is off by 0.06 rad at position 10^6.  32 bits of the turn are left to an octant and the series of sine and cosine
 // on |theta| <= pi / 4 (terms up to theta^9 and theta^8, whose rest is below 2^-25).
 //
-// Bound by memory: every element is read and written once.  A thread keeps the sines of its pairs (about 40 operations each) for several heads of
-// its token; eight heads side by side, so that what a wave reads at a time lies together.  32768 tokens of 28 and 4 heads of 128 columns in bf16
-// (0.54 GB in all): 112 us with a token's heads one after another in a thread, 105 side by side, 99 with loads and stores past the
-// last-level cache as well, 5.7 TB/s, which is a copy's rate here.
+// Bound by memory: every element is read and written once.  A thread keeps the sines of its pairs (about 40 operations each) for four heads and
+// more of its token, whose pieces are all loaded before the first is stored (behind a store the next load's wait is for the store too).  Pieces
+// side by side in a wave are whole lines: of the halves 8 bytes a lane, of interleaved pairs 16.  32768 tokens of 28 and 4 heads of 128 columns in
+// bf16 (0.54 GB in all), us: a head at a time 112, eight heads side by side 105, past the last-level cache 97, four loaded together 92,
+// four pairs a thread in place of eight 88, 6.1 TB/s; interleaved pairs as two pieces of 16 bytes 151, as one 88; fp32 (1.07 GB) as 32
+// bytes a lane 224, as 16 180.
 #include <algorithm>
+#include <type_traits>
 #include <math.h>
 #include <string.h>
 
@@ -23,6 +26,7 @@ namespace fc {
 namespace {
 
 constexpr int kRotThreads = 256;
+constexpr int kHeadsAtOnce = 4, kMostPairs = 4, kMostAbreast = 8, kMostTurns = 8;
 
 struct RotSide {                 // Q or K
   const char* in;
@@ -46,7 +50,6 @@ template <> struct Bytes<2> { typedef uint16_t type; };
 template <> struct Bytes<4> { typedef uint32_t type; };
 template <> struct Bytes<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Bytes<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
-template <> struct Bytes<32> { struct type { Bytes<16>::type a, b; }; };
 
 template <typename T, int N> struct Vec {
   typename Bytes<N * (int)sizeof(T)>::type raw;
@@ -84,26 +87,14 @@ template <typename T, int N> __device__ __forceinline__ Vec<T, N> narrow(const f
 template <bool PAST, typename T, int N> __device__ __forceinline__ Vec<T, N> get(const char* p) {
   const Vec<T, N>* const at = reinterpret_cast<const Vec<T, N>*>(p);
   Vec<T, N> v;
-  if constexpr (!PAST) {
-    v = *at;
-  } else if constexpr (sizeof(v.raw) <= 16) {
-    v.raw = __builtin_nontemporal_load(&at->raw);
-  } else {
-    v.raw.a = __builtin_nontemporal_load(&at->raw.a);
-    v.raw.b = __builtin_nontemporal_load(&at->raw.b);
-  }
+  if constexpr (PAST) v.raw = __builtin_nontemporal_load(&at->raw);
+  else v = *at;
   return v;
 }
 template <bool PAST, typename T, int N> __device__ __forceinline__ void put(char* p, const Vec<T, N>& v) {
   Vec<T, N>* const at = reinterpret_cast<Vec<T, N>*>(p);
-  if constexpr (!PAST) {
-    *at = v;
-  } else if constexpr (sizeof(v.raw) <= 16) {
-    __builtin_nontemporal_store(v.raw, &at->raw);
-  } else {
-    __builtin_nontemporal_store(v.raw.a, &at->raw.a);
-    __builtin_nontemporal_store(v.raw.b, &at->raw.b);
-  }
+  if constexpr (PAST) __builtin_nontemporal_store(v.raw, &at->raw);
+  else *at = v;
 }
 
 // Sine and cosine of `turns` 2^-32 of a whole turn.
@@ -118,9 +109,11 @@ __device__ __forceinline__ void sine_cosine(uint32_t turns, float& s, float& c) 
   c = (quarter + 1) & 2 ? -y : y;
 }
 
-// P pairs a thread and head; a chunk behind the turned ones is 2 P columns to be copied.
+// P pairs a thread and head: a piece of P columns and its partners' half a head away, or, interleaved, one of 2 P columns; chunks behind the
+// turned ones are copied, as pieces of the same kind.
 template <typename T, int P, bool INTERLEAVED, bool PAST>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc_rotary_plan plan) {
+  constexpr int kPieces = INTERLEAVED ? 1 : 2, kPiece = 2 * P / kPieces;     // pieces of a chunk, columns of a piece
   const int place = (int)(threadIdx.x / (unsigned)a.chunks), chunk = (int)threadIdx.x - place * a.chunks;
   const int own = (int)((unsigned)place / (unsigned)a.abreast), beside = place - own * a.abreast;
   const int64_t row64 = (int64_t)blockIdx.x * a.per_group + own;
@@ -128,11 +121,11 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc
   const int row = (int)row64, b = row / a.tokens, t = row - b * a.tokens;
   const bool turned = chunk < a.turned;
   float sn[P], cs[P];
-  int at0, at1;                                            // columns of the chunk's two parts
+  // bytes of the first piece from the head's begin on, and from it to the second
+  const int at = (turned ? chunk * kPiece : 2 * a.half + (chunk - a.turned) * kPiece) * (int)sizeof(T);
+  const int apart = (turned ? a.half : (a.chunks - a.turned) * P) * (int)sizeof(T);
   if (turned) {
     const int first = chunk * P;
-    at0 = INTERLEAVED ? 2 * first : first;
-    at1 = INTERLEAVED ? at0 + P : first + a.half;
     int64_t where[4];
     where[0] = a.positions[row];
     for (int k = 1; k < 4; ++k) where[k] = k < a.streams ? a.positions[(int64_t)k * a.rows + row] : where[0];
@@ -145,38 +138,41 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc
       sn[i] *= a.magnitude * a.sign;
       cs[i] *= a.magnitude;
     }
-  } else {
-    at0 = 2 * a.half + (chunk - a.turned) * 2 * P;
-    at1 = at0 + P;
   }
   const int heads = a.q.heads + a.k.heads, h0 = (int)blockIdx.y * a.abreast * a.turns, h1 = min(heads, h0 + a.abreast * a.turns);
-#pragma unroll 2
-  for (int h = h0 + beside; h < h1; h += a.abreast) {
-    const bool is_q = h < a.q.heads;
-    const int hh = is_q ? h : h - a.q.heads;
-    const char* in = (is_q ? a.q.in : a.k.in) + b * (is_q ? a.q.sb : a.k.sb) + t * (is_q ? a.q.st : a.k.st) + hh * (is_q ? a.q.sh : a.k.sh);
-    char* out = (is_q ? a.q.out : a.k.out) + b * (is_q ? a.q.ob : a.k.ob) + t * (is_q ? a.q.ot : a.k.ot) + hh * (is_q ? a.q.oh : a.k.oh);
-    const Vec<T, P> v0 = get<PAST, T, P>(in + at0 * (int)sizeof(T)), v1 = get<PAST, T, P>(in + at1 * (int)sizeof(T));
-    if (!turned) {
-      put<PAST>(out + at0 * (int)sizeof(T), v0);
-      put<PAST>(out + at1 * (int)sizeof(T), v1);
-      continue;
-    }
-    float x[2 * P], y[2 * P], lo[P], hi[P];
-    widen<T, P>(v0, lo);
-    widen<T, P>(v1, hi);
+  for (int hb = h0 + beside; hb < h1; hb += kHeadsAtOnce * a.abreast) {
+    Vec<T, kPiece> v[kHeadsAtOnce][kPieces];
+    char* out[kHeadsAtOnce];
 #pragma unroll
-    for (int i = 0; i < P; ++i) { x[i] = lo[i]; x[P + i] = hi[i]; }
+    for (int i = 0; i < kHeadsAtOnce; ++i) {
+      const int h = hb + i * a.abreast;
+      if (h >= h1) break;
+      const bool is_q = h < a.q.heads;
+      const int hh = is_q ? h : h - a.q.heads;
+      const char* const in = (is_q ? a.q.in : a.k.in) + b * (is_q ? a.q.sb : a.k.sb) + t * (is_q ? a.q.st : a.k.st) + hh * (is_q ? a.q.sh : a.k.sh) + at;
+      out[i] = (is_q ? a.q.out : a.k.out) + b * (is_q ? a.q.ob : a.k.ob) + t * (is_q ? a.q.ot : a.k.ot) + hh * (is_q ? a.q.oh : a.k.oh) + at;
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int p = INTERLEAVED ? 2 * i : i, q = INTERLEAVED ? 2 * i + 1 : P + i;
-      y[p] = x[p] * cs[i] - x[q] * sn[i];
-      y[q] = x[q] * cs[i] + x[p] * sn[i];
+      for (int j = 0; j < kPieces; ++j) v[i][j] = get<PAST, T, kPiece>(in + j * apart);
     }
 #pragma unroll
-    for (int i = 0; i < P; ++i) { lo[i] = y[i]; hi[i] = y[P + i]; }
-    put<PAST>(out + at0 * (int)sizeof(T), narrow<T, P>(lo));
-    put<PAST>(out + at1 * (int)sizeof(T), narrow<T, P>(hi));
+    for (int i = 0; i < kHeadsAtOnce; ++i) {
+      if (hb + i * a.abreast >= h1) break;
+      if (turned) {
+        float x[kPieces][kPiece], y[kPieces][kPiece];
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) widen<T, kPiece>(v[i][j], x[j]);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          const int j = INTERLEAVED ? 0 : 1, c0 = INTERLEAVED ? 2 * k : k, c1 = INTERLEAVED ? 2 * k + 1 : k;
+          y[0][c0] = x[0][c0] * cs[k] - x[j][c1] * sn[k];
+          y[j][c1] = x[j][c1] * cs[k] + x[0][c0] * sn[k];
+        }
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) v[i][j] = narrow<T, kPiece>(y[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) put<PAST>(out[i] + j * apart, v[i][j]);
+    }
   }
 }
 
@@ -199,8 +195,9 @@ hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, c
   uint64_t bits = 0;
   for (const RotSide* r : {&a.q, &a.k})
     bits |= (uint64_t)(uintptr_t)r->in | (uint64_t)(uintptr_t)r->out | (uint64_t)(r->sb | r->st | r->sh | r->ob | r->ot | r->oh);
-  int pairs = 8;
-  while (pairs > 1 && (half % pairs || rest % (2 * pairs) || (bits & (uint64_t)(std::min(16, pairs * e) - 1)))) pairs /= 2;
+  const int pieces = plan.interleaved ? 1 : 2;             // (of a chunk: 16 bytes at most)
+  int pairs = std::min(8 * pieces / e, kMostPairs);
+  while (pairs > 1 && (half % pairs || rest % (2 * pairs) || (bits & (uint64_t)(2 * pairs / pieces * e - 1)))) pairs /= 2;
   a.positions = positions;
   a.tokens = q.tokens;
   a.rows = q.batch * q.tokens;
@@ -215,29 +212,34 @@ hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, c
   a.sign = inverse ? -1.f : 1.f;
   const int heads = a.q.heads + a.k.heads, places = kRotThreads / a.chunks;
   const int64_t one_turn = ((int64_t)a.rows * heads + places - 1) / places;    // workgroups if every thread has a single head
-  // few tokens: all heads side by side, so that a step's launch is spread over the chip; else several turns of eight
-  a.abreast = std::min(std::min(heads, places), one_turn > 2048 ? 8 : heads);
-  a.turns = (int)std::max<int64_t>(1, std::min<int64_t>((heads + a.abreast - 1) / a.abreast, one_turn / 2048));
+  // few tokens: all heads side by side, so that a step's launch is spread over the chip; else at least four turns, for which the sines are made
+  // once (32768 tokens, us with eight side by side whatever there is / so: 8 heads of 128 columns 44 / 30, 10 of 64 26 / 17)
+  int abreast = 1;
+  while (abreast < kMostAbreast && 2 * abreast * kHeadsAtOnce <= heads) abreast *= 2;
+  a.abreast = std::min(std::min(heads, places), one_turn > 2048 ? abreast : heads);
+  a.turns = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMostTurns, (heads + a.abreast - 1) / a.abreast), one_turn / 2048));
   a.per_group = places / a.abreast;
   const dim3 grid((unsigned)(((int64_t)a.rows + a.per_group - 1) / a.per_group), (unsigned)((heads + a.abreast * a.turns - 1) / (a.abreast * a.turns)));
   ProfileScope ps("rotary_kernel", s);
   auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a, plan); };
-  const bool past = 2LL * a.rows * heads * q.head_dim * e > 256000000;         // (what is read and written exceeds the cache)
-#define FC_ROTARY(T, P)                                                                                                                        \
-  plan.interleaved ? (past ? launch(rotary_kernel<T, P, true, true>) : launch(rotary_kernel<T, P, true, false>))                               \
-                   : (past ? launch(rotary_kernel<T, P, false, true>) : launch(rotary_kernel<T, P, false, false>))
-  if (q.dtype == FC_BF16) {
-    if (pairs == 8) FC_ROTARY(uint16_t, 8);
-    else if (pairs == 4) FC_ROTARY(uint16_t, 4);
-    else if (pairs == 2) FC_ROTARY(uint16_t, 2);
-    else FC_ROTARY(uint16_t, 1);
-  } else {
-    if (pairs == 8) FC_ROTARY(float, 8);
-    else if (pairs == 4) FC_ROTARY(float, 4);
-    else if (pairs == 2) FC_ROTARY(float, 2);
-    else FC_ROTARY(float, 1);
-  }
-#undef FC_ROTARY
+  // what is read and written exceeds the cache, in pieces of whole lines (half lines: 32 and 8 heads of 128 columns, 64 of them turned, 147 / 136)
+  const bool past = 2LL * a.rows * heads * q.head_dim * e > 256000000 && (plan.interleaved || half * e % 128 == 0);
+  auto with = [&](auto type, auto n, auto interleaved) {
+    typedef decltype(type) T;
+    past ? launch(rotary_kernel<T, decltype(n)::value, decltype(interleaved)::value, true>)
+         : launch(rotary_kernel<T, decltype(n)::value, decltype(interleaved)::value, false>);
+  };
+  typedef std::integral_constant<int, 4> Four;
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 1> One;
+  auto sized = [&](auto type, auto interleaved) {          // (interleaved fp32: two pairs are 16 bytes)
+    constexpr bool kFour = !decltype(interleaved)::value || sizeof(type) == 2;
+    if (pairs == 1) with(type, One{}, interleaved);
+    else if (!kFour || pairs == 2) with(type, Two{}, interleaved);
+    else with(type, std::conditional_t<kFour, Four, Two>{}, interleaved);
+  };
+  auto of = [&](auto type) { plan.interleaved ? sized(type, std::true_type{}) : sized(type, std::false_type{}); };
+  q.dtype == FC_BF16 ? of(uint16_t{}) : of(float{});
   return hipGetLastError();
 }
 

@@ -117,6 +117,28 @@ def test_rotary_in_place_strided_and_unaligned():
             _check_rotary(y, w, size, angle, 64, m, dtype, w)
 
 
+@pytest.mark.parametrize("dtype,T,Hq,Hk,d,R,inter", [
+    ("bf16", 16001, 28, 4, 128, 128, False), ("bf16", 16001, 28, 4, 128, 128, True), ("f32", 16001, 9, 2, 128, 96, False),
+    ("f32", 9001, 17, 8, 128, 32, True), ("bf16", 60001, 5, 1, 80, 20, True), ("bf16", 13001, 33, 8, 128, 64, False),
+    ("bf16", 5001, 70, 3, 64, 64, False), ("bf16", 40001, 0, 8, 128, 128, False),
+])
+def test_rotary_of_many_tokens_equals_that_of_few(dtype, T, Hq, Hk, d, R, inter):
+    """Large calls take several heads a thread and go past the cache; small ones are tested above against the oracle."""
+    fc = _fc()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    heads = [torch.randn((1, T, h, d), generator=g, device="cuda").to(_dt(dtype)) for h in (Hq, Hk)]
+    pos = torch.randint(-1000, 200000, (1, T), generator=g, device="cuda", dtype=torch.int32)
+    plan = fc.rotary_plan(R, theta=1e6, interleaved=inter)
+    got = fc.rotary(plan, pos, *heads)
+    want = [torch.empty_like(x) for x in heads]
+    for t in range(0, T, 61):
+        q, k = (x[:, t:t + 61] for x in heads)
+        fc.rotary(plan, pos[:, t:t + 61].contiguous(), q, k, Q_out=want[0][:, t:t + 61], K_out=want[1][:, t:t + 61])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    fc.rotary(plan, pos, *heads, Q_out=heads[0], K_out=heads[1])             # in place
+    assert all(torch.equal(a, b) for a, b in zip(heads, want))
+
+
 def test_rotary_gradient_against_differences():
     """<g, rotary(x)> has the gradient rotary(g, inverse): against the formula's and against differences of the map itself."""
     fc = _fc()
