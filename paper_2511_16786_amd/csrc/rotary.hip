@@ -8,12 +8,13 @@
 // fp32 is off by 0.06 rad at position 10^6.  32 bits of the turn are left to an octant and the series of sine and cosine
 // on |theta| <= pi / 4 (terms up to theta^9 and theta^8, whose rest is below 2^-25).
 //
-// Bound by memory: every element is read and written once.  A thread keeps the sines of its pairs (about 40 operations each) for four heads and
+// Bound by memory: every element is read and written once.  A thread keeps the sines of its pairs (about 35 operations each) for four heads and
 // more of its token, whose pieces are all loaded before the first is stored (behind a store the next load's wait is for the store too).  Pieces
 // side by side in a wave are whole lines: of the halves 8 bytes a lane, of interleaved pairs 16.  32768 tokens of 28 and 4 heads of 128 columns in
 // bf16 (0.54 GB in all), us: a head at a time 112, eight heads side by side 105, past the last-level cache 97, four loaded together 92,
-// four pairs a thread in place of eight 88, 6.1 TB/s; interleaved pairs as two pieces of 16 bytes 151, as one 88; fp32 (1.07 GB) as 32
-// bytes a lane 224, as 16 180.
+// four pairs a thread in place of eight 88, 6.1 TB/s; interleaved pairs as two pieces of 16 bytes 151, as one 87; fp32 (1.07 GB) as 32
+// bytes a lane 224, as 16 180.  Integer products of 64 bits take four times as long as others: heads' places by the wave and sequences that
+// follow each other as one made 8192 tokens of 5 and 1 heads 9.1 / 7.9 us, 2048 of 28 and 4 10.5 / 9.5.
 #include <algorithm>
 #include <type_traits>
 #include <math.h>
@@ -40,10 +41,16 @@ struct RotArgs {
   int tokens, rows;              // tokens of a sequence, of all sequences
   int half, chunks, turned;      // pairs; chunks of a head; those that are turned
   int per_group;                 // tokens of a workgroup
+  uint32_t chunks_inverse, abreast_inverse;
+  bool flat;                     // the sequences follow each other as tokens do
   int abreast, turns;            // heads of a token side by side; how many of them a thread has, one after another
   int streams, end0, end1, end2; // first pair behind the first, second and third stream
   float magnitude, sign;
 };
+
+// n / d for n and d up to 256, with d's inverse in 16 bits, rounded up
+__host__ __device__ __forceinline__ uint32_t inverse_of(int d) { return (65536u + (uint32_t)d - 1u) / (uint32_t)d; }
+__device__ __forceinline__ int quotient(uint32_t n, uint32_t inverse) { return (int)(n * inverse >> 16); }
 
 template <int BYTES> struct Bytes;
 template <> struct Bytes<2> { typedef uint16_t type; };
@@ -114,11 +121,11 @@ __device__ __forceinline__ void sine_cosine(uint32_t turns, float& s, float& c) 
 template <typename T, int P, bool INTERLEAVED, bool PAST>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc_rotary_plan plan) {
   constexpr int kPieces = INTERLEAVED ? 1 : 2, kPiece = 2 * P / kPieces;     // pieces of a chunk, columns of a piece
-  const int place = (int)(threadIdx.x / (unsigned)a.chunks), chunk = (int)threadIdx.x - place * a.chunks;
-  const int own = (int)((unsigned)place / (unsigned)a.abreast), beside = place - own * a.abreast;
+  const int place = quotient(threadIdx.x, a.chunks_inverse), chunk = (int)threadIdx.x - place * a.chunks;
+  const int own = quotient(place, a.abreast_inverse), beside = place - own * a.abreast;
   const int64_t row64 = (int64_t)blockIdx.x * a.per_group + own;
   if (own >= a.per_group || row64 >= a.rows) return;
-  const int row = (int)row64, b = row / a.tokens, t = row - b * a.tokens;
+  const int row = (int)row64;
   const bool turned = chunk < a.turned;
   float sn[P], cs[P];
   // bytes of the first piece from the head's begin on, and from it to the second
@@ -126,37 +133,62 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotArgs a, const fc
   const int apart = (turned ? a.half : (a.chunks - a.turned) * P) * (int)sizeof(T);
   if (turned) {
     const int first = chunk * P;
-    int64_t where[4];
+    int32_t where[P];
     where[0] = a.positions[row];
-    for (int k = 1; k < 4; ++k) where[k] = k < a.streams ? a.positions[(int64_t)k * a.rows + row] : where[0];
+#pragma unroll
+    for (int i = 1; i < P; ++i) where[i] = where[0];
+    if (a.streams > 1) {
+      int32_t other[3];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) other[k] = k + 1 < a.streams ? a.positions[(int64_t)(k + 1) * a.rows + row] : 0;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const int pair = first + i;
+        where[i] = pair < a.end0 ? where[i] : pair < a.end1 ? other[0] : pair < a.end2 ? other[1] : other[2];
+      }
+    }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int pair = first + i;
-      const int64_t pos = pair < a.end0 ? where[0] : pair < a.end1 ? where[1] : pair < a.end2 ? where[2] : where[3];
-      const uint64_t whole = (uint64_t)pos * plan.turns[pair];
-      sine_cosine((uint32_t)((whole + 0x80000000ull) >> 32), sn[i], cs[i]);
+      // the upper half of position * turns, rounded: what the lower halves' product carries, and less 2^32 times the turns for a negative one
+      const uint64_t turns = plan.turns[first + i];
+      const uint32_t low = (uint32_t)turns, high = (uint32_t)(turns >> 32), pos = (uint32_t)where[i];
+      const uint64_t carried = (uint64_t)pos * low + 0x80000000ull;
+      sine_cosine(pos * high + (uint32_t)(carried >> 32) - (where[i] < 0 ? low : 0u), sn[i], cs[i]);
       sn[i] *= a.magnitude * a.sign;
       cs[i] *= a.magnitude;
     }
   }
   const int heads = a.q.heads + a.k.heads, h0 = (int)blockIdx.y * a.abreast * a.turns, h1 = min(heads, h0 + a.abreast * a.turns);
-  for (int hb = h0 + beside; hb < h1; hb += kHeadsAtOnce * a.abreast) {
+  // head `beside` of Q, and what would be that of Q and K as one
+  int b = 0, t = row;
+  if (!a.flat) {
+    b = row / a.tokens;
+    t = row - b * a.tokens;
+  }
+  int64_t q_in = t * a.q.st + beside * a.q.sh + at, q_out = t * a.q.ot + beside * a.q.oh + at;
+  int64_t k_in = t * a.k.st + (beside - a.q.heads) * a.k.sh + at, k_out = t * a.k.ot + (beside - a.q.heads) * a.k.oh + at;
+  if (!a.flat) {
+    q_in += b * a.q.sb;
+    q_out += b * a.q.ob;
+    k_in += b * a.k.sb;
+    k_out += b * a.k.ob;
+  }
+  for (int hw = h0; hw < h1; hw += kHeadsAtOnce * a.abreast) {
     Vec<T, kPiece> v[kHeadsAtOnce][kPieces];
     char* out[kHeadsAtOnce];
 #pragma unroll
     for (int i = 0; i < kHeadsAtOnce; ++i) {
-      const int h = hb + i * a.abreast;
+      const int hu = hw + i * a.abreast, h = hu + beside;  // (the first is the same for the wave)
       if (h >= h1) break;
       const bool is_q = h < a.q.heads;
-      const int hh = is_q ? h : h - a.q.heads;
-      const char* const in = (is_q ? a.q.in : a.k.in) + b * (is_q ? a.q.sb : a.k.sb) + t * (is_q ? a.q.st : a.k.st) + hh * (is_q ? a.q.sh : a.k.sh) + at;
-      out[i] = (is_q ? a.q.out : a.k.out) + b * (is_q ? a.q.ob : a.k.ob) + t * (is_q ? a.q.ot : a.k.ot) + hh * (is_q ? a.q.oh : a.k.oh) + at;
+      const char* const in = is_q ? a.q.in + hu * a.q.sh + q_in : a.k.in + hu * a.k.sh + k_in;
+      out[i] = is_q ? a.q.out + hu * a.q.oh + q_out : a.k.out + hu * a.k.oh + k_out;
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) v[i][j] = get<PAST, T, kPiece>(in + j * apart);
     }
 #pragma unroll
     for (int i = 0; i < kHeadsAtOnce; ++i) {
-      if (hb + i * a.abreast >= h1) break;
+      if (hw + i * a.abreast + beside >= h1) break;
       if (turned) {
         float x[kPieces][kPiece], y[kPieces][kPiece];
 #pragma unroll
@@ -201,6 +233,15 @@ hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, c
   a.positions = positions;
   a.tokens = q.tokens;
   a.rows = q.batch * q.tokens;
+  a.flat = true;
+  for (RotSide* r : {&a.q, &a.k}) {
+    if (q.tokens == 1) {
+      r->st = r->sb;
+      r->ot = r->ob;
+    } else if (q.batch > 1 && r->heads) {
+      a.flat = a.flat && r->sb == q.tokens * r->st && r->ob == q.tokens * r->ot;
+    }
+  }
   a.half = half;
   a.turned = half / pairs;
   a.chunks = a.turned + rest / (2 * pairs);
@@ -219,6 +260,8 @@ hipError_t rotary_launch(const fc_rotary_plan& plan, const int32_t* positions, c
   a.abreast = std::min(std::min(heads, places), one_turn > 2048 ? abreast : heads);
   a.turns = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMostTurns, (heads + a.abreast - 1) / a.abreast), one_turn / 2048));
   a.per_group = places / a.abreast;
+  a.chunks_inverse = inverse_of(a.chunks);
+  a.abreast_inverse = inverse_of(a.abreast);
   const dim3 grid((unsigned)(((int64_t)a.rows + a.per_group - 1) / a.per_group), (unsigned)((heads + a.abreast * a.turns - 1) / (a.abreast * a.turns)));
   ProfileScope ps("rotary_kernel", s);
   auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kRotThreads), 0, s, a, plan); };
