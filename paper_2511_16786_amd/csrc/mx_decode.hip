@@ -7,6 +7,10 @@
 //            columns; fp32 queries as three bf16 terms, 24 bits), so that a lane has the scores of rows 4 g4 + i and head c16
 //   output:  A = probabilities (head c16, rows 4 g4 + i of both tiles of a step: as the scores come out), B = V (the same rows, column
 //            D / 16 c16 + t for output tile t).  Probabilities are three bf16 terms, 24 bits: with two the result is off by 1e-6.
+// Up to eight heads leave half of the sixteen lanes, columns and rows of these products idle (FOLD): lanes 8 .. 15 then have the second tile's
+// scores, half the exponentials and splits each; rows 8 .. 15 of A are the probabilities' second term, two products in place of three, added up
+// once at the end; and columns 8 .. 15 of B an fp32 query's second term.  (28 layers that keep 29 500 of 32 768 rows, 7 heads: bf16 88.5 us / 84.5
+// so, the second tile's scores alone 87; 6554 rows fp32 30.5 / 28.6, 64 columns 21.4 / 20.5.)
 //
 // A workgroup has a piece of one unit, in steps of 32 rows of which each of its waves takes a quarter; the waves merge in LDS, the pieces of a
 // unit in a second kernel.  Budgets are on the device, so that every wave finds out by itself how many pieces the layers make and which of
@@ -76,6 +80,14 @@ __device__ __forceinline__ void eight_values(uint32_t code, float unit, uint32_t
   o[2] = two_values<2>(code, unit);
   o[3] = two_values<3>(code, unit);
 }
+// Of each sixteen lanes the upper eight, or the lower eight, take b's from the lane eight below, or above; the others keep a.
+__device__ __forceinline__ uint32_t upper_half(uint32_t a, uint32_t b) { return (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x118, 0xF, 0xC, false); }
+__device__ __forceinline__ uint32_t lower_half(uint32_t a, uint32_t b) { return (uint32_t)__builtin_amdgcn_update_dpp((int)a, (int)b, 0x108, 0xF, 0x3, false); }
+// the lower eight's own, and zeros
+__device__ __forceinline__ uint32_t lower_half_alone(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xE4, 0xF, 0x3, false); }
+__device__ __forceinline__ float other_half(float v) {     // eight lanes further round
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x128, 0xF, 0xF, false));
+}
 // in a scalar register
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v) {     // 0 where there is no source lane
@@ -128,7 +140,7 @@ template <int D> struct Step {
   int gone[2], missing;          // negative: the tile, either tile has no page
 };
 
-template <int D, int QTERMS>
+template <int D, int QTERMS, bool FOLD>
 __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_partial_kernel(MxdArgs a) {
   typedef MxTile<D> Tile;
   constexpr int KW = D / 32;             // dwords of K and of V a lane and tile; 32-column products of a score
@@ -190,15 +202,17 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
   const int s0 = first + n * wave / kMxdWaves, s1 = first + n * (wave + 1) / kMxdWaves;
   if (!a.whole && piece == 0 && tid == 0) a.span[unit] = int2{w, pieces};
   // queries: head c16 (zeros beyond G), columns D / 4 g4 + 8 i .. + 7
-  uint32_t q[QTERMS][KW][4];
+  constexpr int kQ = FOLD && QTERMS == 3 ? 2 : QTERMS;
+  const int head = FOLD && QTERMS == 3 ? c16 & 7 : c16;
+  uint32_t q[kQ][KW][4];
 #pragma unroll
-  for (int t = 0; t < QTERMS; ++t)
+  for (int t = 0; t < kQ; ++t)
 #pragma unroll
     for (int i = 0; i < KW; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) q[t][i][j] = 0u;
-  if (c16 < G && s0 < s1) {
-    const size_t at_q = ((size_t)unit * G + c16) * D + g4 * (D / 4);
+  if (head < G && s0 < s1) {
+    const size_t at_q = ((size_t)unit * G + head) * D + g4 * (D / 4);
     if constexpr (QTERMS == 1) {
       const uint32_t flip = a.negate ? 0x80008000u : 0u;
 #pragma unroll
@@ -214,17 +228,25 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
         for (int j = 0; j < 4; ++j) {
           const float2v x = *reinterpret_cast<const float2v*>(static_cast<const float*>(a.Q) + at_q + 8 * i + 2 * j);
           float x0 = a.negate ? -x[0] : x[0], x1 = a.negate ? -x[1] : x[1];
+          uint32_t term[QTERMS];
 #pragma unroll
           for (int t = 0; t < QTERMS; ++t) {
             // (the first two cut off, so that nothing overflows to infinity; the last to nearest)
             const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
             if (t == QTERMS - 1) {
-              q[t][i][j] = pack_bf16(x0, x1);
+              term[t] = pack_bf16(x0, x1);
             } else {
-              q[t][i][j] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+              term[t] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
               x0 -= __uint_as_float(u0 & 0xFFFF0000u);
               x1 -= __uint_as_float(u1 & 0xFFFF0000u);
             }
+          }
+          if constexpr (FOLD) {
+            q[0][i][j] = c16 < 8 ? term[0] : term[1];
+            q[1][i][j] = c16 < 8 ? term[2] : 0u;
+          } else {
+#pragma unroll
+            for (int t = 0; t < QTERMS; ++t) q[t][i][j] = term[t];
           }
         }
     }
@@ -297,11 +319,11 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
         eight_values(x.k[tt][i], unit_k, kv);
         const bf16x8 ka = as_bf16x8(kv[0], kv[1], kv[2], kv[3]);
 #pragma unroll
-        for (int t = QTERMS - 1; t >= 0; --t)
+        for (int t = kQ - 1; t >= 0; --t)
           acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, as_bf16x8(q[t][i][0], q[t][i][1], q[t][i][2], q[t][i][3]), acc, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sc[tt][i] = acc[i];
+      for (int i = 0; i < 4; ++i) sc[tt][i] = kQ < QTERMS ? acc[i] + other_half(acc[i]) : acc[i];
     }
     const int rb = 32 * st + 4 * g4;
     if (x.missing < 0 || 32 * st + 32 > rows) {              // (the same for the wave)
@@ -314,9 +336,15 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
             x.vs[tt] = (x.vs[tt] & ~(0xFFu << (8 * i))) | (127u << (8 * i));     // (no NaN from a row that is not there)
           }
     }
-    float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                     fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+    constexpr int kTiles = FOLD ? 1 : 2;
+    if constexpr (FOLD) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[0][i] = __uint_as_float(upper_half(__float_as_uint(sc[0][i]), __float_as_uint(sc[1][i])));
+    }
+    float mx = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3]));
+    if constexpr (!FOLD) mx = fmaxf(mx, fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
     if (__ballot(mx > limit)) {
+      if constexpr (FOLD) mx = fmaxf(mx, __shfl_xor(mx, 8, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       const float m_new = fmaxf(m, mx * a.scale_log2e), alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
@@ -333,7 +361,7 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
     }
     uint32_t hi[4], mid[4], lo[4];
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
+    for (int tt = 0; tt < kTiles; ++tt)
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
         float p0 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i], a.scale_log2e, -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[tt][i + 1], a.scale_log2e, -ref));
@@ -346,8 +374,16 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
         mid[w2] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
         lo[w2] = pack_bf16(less_low(p0, mid[w2]), less_high(p1, mid[w2]));
       }
-    const bf16x8 ph = as_bf16x8(hi[0], hi[1], hi[2], hi[3]), pm = as_bf16x8(mid[0], mid[1], mid[2], mid[3]),
-                 pl = as_bf16x8(lo[0], lo[1], lo[2], lo[3]);
+    constexpr int kP = FOLD ? 2 : 3;
+    bf16x8 terms[kP];
+    if constexpr (FOLD) {
+      terms[0] = as_bf16x8(upper_half(hi[0], mid[0]), upper_half(hi[1], mid[1]), lower_half(mid[0], hi[0]), lower_half(mid[1], hi[1]));
+      terms[1] = as_bf16x8(lower_half_alone(lo[0]), lower_half_alone(lo[1]), lower_half(0u, lo[0]), lower_half(0u, lo[1]));
+    } else {
+      terms[0] = as_bf16x8(hi[0], hi[1], hi[2], hi[3]);
+      terms[1] = as_bf16x8(mid[0], mid[1], mid[2], mid[3]);
+      terms[kP - 1] = as_bf16x8(lo[0], lo[1], lo[2], lo[3]);
+    }
     float unit_v[2][4];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -374,9 +410,9 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
         const bf16x8 vb = as_bf16x8(__builtin_amdgcn_perm(r[0][1], r[0][0], sel), __builtin_amdgcn_perm(r[0][3], r[0][2], sel),
                                     __builtin_amdgcn_perm(r[1][1], r[1][0], sel), __builtin_amdgcn_perm(r[1][3], r[1][2], sel));
         float4v acc = out[2 * c + o];
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph, vb, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pm, vb, acc, 0, 0, 0);
-        out[2 * c + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, vb, acc, 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < kP; ++t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(terms[t], vb, acc, 0, 0, 0);
+        out[2 * c + o] = acc;
       }
     };
     tiles_of(std::integral_constant<int, 0>{});
@@ -401,7 +437,18 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
     }
   }
 
-  // the four lanes of a head add their sums
+  if constexpr (FOLD) {                                    // heads' second terms, eight rows below
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t u = __float_as_uint(out[t][i]);
+        const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        out[t][i] = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+      }
+  }
+  // the lanes of a head add their sums
+  if constexpr (FOLD) ls += __shfl_xor(ls, 8, 64);
   ls += __shfl_xor(ls, 16, 64);
   ls += __shfl_xor(ls, 32, 64);
   float* const mine = parts + wave * part_floats;
@@ -554,8 +601,12 @@ hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* tab
     const int grid = whole ? units : (int)std::min<int64_t>(most_pieces(groups, units), units * ((reach + kLeastSteps - 1) / kLeastSteps));
     const size_t lds = kMxdWaves * piece_floats(group, d) * sizeof(float);
     auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(grid), dim3(kMxdThreads), lds, s, a); };
-    if (dtype == FC_BF16) d == 128 ? launch(mx_decode_partial_kernel<128, 1>) : launch(mx_decode_partial_kernel<64, 1>);
-    else d == 128 ? launch(mx_decode_partial_kernel<128, 3>) : launch(mx_decode_partial_kernel<64, 3>);
+    auto folded = [&](auto fold) {
+      constexpr bool kFold = decltype(fold)::value;
+      if (dtype == FC_BF16) d == 128 ? launch(mx_decode_partial_kernel<128, 1, kFold>) : launch(mx_decode_partial_kernel<64, 1, kFold>);
+      else d == 128 ? launch(mx_decode_partial_kernel<128, 3, kFold>) : launch(mx_decode_partial_kernel<64, 3, kFold>);
+    };
+    group <= 8 ? folded(std::true_type{}) : folded(std::false_type{});
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || whole) return e;

@@ -481,6 +481,23 @@ def test_mx_decode_attention(dtype, B, L, H, G, d, ps, rows):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", range(1, 17))
+def test_mx_decode_attention_of_every_group(dtype, d, G):
+    fc = _fc()
+    rng = np.random.default_rng(100 * G + d)
+    B, L, H, ps = 1, 2, 2, 16
+    rows = np.array([[1500, 40 + G]], np.int32)
+    pages, table, Ks, Vs = _cache(fc, rng, B, L, H, d, ps, rows)
+    Q = _rand(rng, (B, L, H * G, d), _dt(dtype))
+    guarded = torch.full((L * H * G + 1, d), 5.0, device="cuda")
+    got = fc.mx_decode_attention(Q, pages, ps, H, torch.from_numpy(rows).cuda(), torch.from_numpy(table).cuda(), -0.2,
+                                 out=guarded[:-1].view(B, L, H * G, d))
+    _check_attend(got, Q, Ks, Vs, B, L, H, G, -0.2)
+    assert bool((guarded[-1] == 5).all())
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_mx_decode_attention_missing_pages_and_rows_beyond_the_table(d):
     fc = _fc()
