@@ -119,9 +119,10 @@ __device__ __forceinline__ float less_high(float x, uint32_t two) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, c), x, false);
 }
 
-__device__ __forceinline__ int rows_at(const MxdArgs& a, int bl) {
-  return min(min(max(a.rows[bl], 0), kMostRows), (int)min((int64_t)kMostRows, (int64_t)a.max_pages * a.page_tiles * 16));
+__device__ __forceinline__ int rows_within(const MxdArgs& a, int rows) {
+  return min(min(max(rows, 0), kMostRows), (int)min((int64_t)kMostRows, (int64_t)a.max_pages * a.page_tiles * 16));
 }
+__device__ __forceinline__ int rows_at(const MxdArgs& a, int bl) { return rows_within(a, a.rows[bl]); }
 __device__ __forceinline__ int steps_of(int rows) { return (rows + 31) >> 5; }
 
 // Steps of a piece, for a launch of `all` steps: as many pieces as stay resident together, a part of one more for each unit among them; where
@@ -159,9 +160,13 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
     int held[kChunks];
     auto load_rows = [&](int base) {
 #pragma unroll
-      for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j < a.layers ? rows_at(a, min(base + 64 * j + lane, a.layers - 1)) : 0;
+      for (int j = 0; j < kChunks; ++j) held[j] = 0;
+      auto load = [&](int j) { held[j] = a.rows[min(base + 64 * j + lane, a.layers - 1)]; };
+      load(0);
+      if (a.layers > base + 64) { load(1); load(2); load(3); }                 // (no use of one before the next)
+      if (a.layers > base + 256) { load(4); load(5); load(6); load(7); }
 #pragma unroll
-      for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j + lane < a.layers ? held[j] : 0;
+      for (int j = 0; j < kChunks; ++j) held[j] = base + 64 * j + lane < a.layers ? rows_within(a, held[j]) : 0;
     };
     int total = 0;
     for (int base = 0; base < a.layers; base += 64 * kChunks) {
@@ -201,63 +206,6 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
   const int share = steps / pieces, over = steps - share * pieces, first = piece * share + min(piece, over), n = share + (piece < over ? 1 : 0);
   const int s0 = first + n * wave / kMxdWaves, s1 = first + n * (wave + 1) / kMxdWaves;
   if (!a.whole && piece == 0 && tid == 0) a.span[unit] = int2{w, pieces};
-  // queries: head c16 (zeros beyond G), columns D / 4 g4 + 8 i .. + 7
-  constexpr int kQ = FOLD && QTERMS == 3 ? 2 : QTERMS;
-  const int head = FOLD && QTERMS == 3 ? c16 & 7 : c16;
-  uint32_t q[kQ][KW][4];
-#pragma unroll
-  for (int t = 0; t < kQ; ++t)
-#pragma unroll
-    for (int i = 0; i < KW; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) q[t][i][j] = 0u;
-  if (head < G && s0 < s1) {
-    const size_t at_q = ((size_t)unit * G + head) * D + g4 * (D / 4);
-    if constexpr (QTERMS == 1) {
-      const uint32_t flip = a.negate ? 0x80008000u : 0u;
-#pragma unroll
-      for (int i = 0; i < KW; ++i) {
-        const u32x4 u = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.Q) + at_q + 8 * i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) q[0][i][j] = u[j] ^ flip;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < KW; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2v x = *reinterpret_cast<const float2v*>(static_cast<const float*>(a.Q) + at_q + 8 * i + 2 * j);
-          float x0 = a.negate ? -x[0] : x[0], x1 = a.negate ? -x[1] : x[1];
-          uint32_t term[QTERMS];
-#pragma unroll
-          for (int t = 0; t < QTERMS; ++t) {
-            // (the first two cut off, so that nothing overflows to infinity; the last to nearest)
-            const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
-            if (t == QTERMS - 1) {
-              term[t] = pack_bf16(x0, x1);
-            } else {
-              term[t] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
-              x0 -= __uint_as_float(u0 & 0xFFFF0000u);
-              x1 -= __uint_as_float(u1 & 0xFFFF0000u);
-            }
-          }
-          if constexpr (FOLD) {
-            q[0][i][j] = c16 < 8 ? term[0] : term[1];
-            q[1][i][j] = c16 < 8 ? term[2] : 0u;
-          } else {
-#pragma unroll
-            for (int t = 0; t < QTERMS; ++t) q[t][i][j] = term[t];
-          }
-        }
-    }
-  }
-
-  // reference of head c16 (the same in its four lanes), in log2 units, and this lane's sum; the product from which on the reference is moved
-  float m = -INFINITY, ref = 0.f, ls = 0.f, limit = -INFINITY;
-  float4v out[VT];
-#pragma unroll
-  for (int t = 0; t < VT; ++t) out[t] = float4v{0.f, 0.f, 0.f, 0.f};
-
   const int32_t* const entries = a.table + (int64_t)unit * a.max_pages;
   const int last_tile = min((rows + 15) >> 4, 2 * s1);
   const uint32_t k_off = Tile::k_code(c16, g4 * (D / 8)), v_off = Tile::v_code(4 * g4, c16);
@@ -272,7 +220,26 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
     const int32_t id = entries[min(page0 + lane, a.max_pages - 1)];
     return id >= 0 && id < a.num_pages ? id * a.page_tiles : -1;
   };
-  int32_t entry = s0 < s1 ? lookup() : -1;
+  int32_t entry = lookup();
+  // queries: head c16 (zeros beyond G), columns D / 4 g4 + 8 i .. + 7; on the way as the page numbers are, and made operands of behind the first tiles
+  constexpr int kQ = FOLD && QTERMS == 3 ? 2 : QTERMS;
+  typedef std::conditional_t<QTERMS == 1, uint16_t, float> Query;
+  const int head = FOLD && QTERMS == 3 ? c16 & 7 : c16;
+  u32x4 raw[KW][sizeof(Query) / 2];
+  {
+    const Query* const from = static_cast<const Query*>(a.Q) + ((size_t)unit * G + min(head, G - 1)) * D + g4 * (D / 4);
+#pragma unroll
+    for (int i = 0; i < KW; ++i)
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(Query) / 2; ++j) raw[i][j] = reinterpret_cast<const u32x4*>(from + 8 * i)[j];
+  }
+
+  // reference of head c16 (the same in its four lanes), in log2 units, and this lane's sum; the product from which on the reference is moved
+  float m = -INFINITY, ref = 0.f, ls = 0.f, limit = -INFINITY;
+  float4v out[VT];
+#pragma unroll
+  for (int t = 0; t < VT; ++t) out[t] = float4v{0.f, 0.f, 0.f, 0.f};
+
   auto load_step = [&](Step<D>& x) {
     x.missing = 0;
 #pragma unroll
@@ -307,6 +274,43 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
       x.vs[tt] = load_past<uint32_t>(at_tile + vs_off);
     }
   };
+  Step<D> x[kAhead];                   // (of a wave without steps: what is at that place, or the cache's first tile)
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load_step(x[i]);
+  uint32_t q[kQ][KW][4];
+#pragma unroll
+  for (int i = 0; i < KW; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t there = head < G ? ~0u : 0u;
+      if constexpr (QTERMS == 1) {
+        q[0][i][j] = (raw[i][0][j] ^ (a.negate ? 0x80008000u : 0u)) & there;
+      } else {
+        const uint32_t flip = a.negate ? 0x80000000u : 0u;
+        const uint32_t pair0 = raw[i][j / 2][2 * (j % 2)], pair1 = raw[i][j / 2][2 * (j % 2) + 1];
+        float x0 = __uint_as_float((pair0 ^ flip) & there), x1 = __uint_as_float((pair1 ^ flip) & there);
+        uint32_t term[QTERMS];
+#pragma unroll
+        for (int t = 0; t < QTERMS; ++t) {
+          // (the first two cut off, so that nothing overflows to infinity; the last to nearest)
+          const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+          if (t == QTERMS - 1) {
+            term[t] = pack_bf16(x0, x1);
+          } else {
+            term[t] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+            x0 -= __uint_as_float(u0 & 0xFFFF0000u);
+            x1 -= __uint_as_float(u1 & 0xFFFF0000u);
+          }
+        }
+        if constexpr (FOLD) {
+          q[0][i][j] = c16 < 8 ? term[0] : term[1];
+          q[1][i][j] = c16 < 8 ? term[2] : 0u;
+        } else {
+#pragma unroll
+          for (int t = 0; t < QTERMS; ++t) q[t][i][j] = term[t];
+        }
+      }
+    }
   auto work = [&](int st, Step<D>& x) {
     float sc[2][4];
 #pragma unroll
@@ -424,16 +428,11 @@ __global__ __launch_bounds__(kMxdThreads, waves_held(D, QTERMS)) void mx_decode_
   };
   // kAhead steps under way; a step's registers are filled again in place.  (Loads without conditions, behind the wave's last step of that
   // step's last tile again: where a load may or may not have been made the next wait is for all of them.)
-  if (s0 < s1) {
-    Step<D> x[kAhead];
+  for (int st = s0; st < s1; st += kAhead) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) load_step(x[i]);
-    for (int st = s0; st < s1; st += kAhead) {
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        if (st + i < s1) work(st + i, x[i]);
-        load_step(x[i]);
-      }
+    for (int i = 0; i < kAhead; ++i) {
+      if (st + i < s1) work(st + i, x[i]);
+      load_step(x[i]);
     }
   }
 
