@@ -356,12 +356,16 @@ def decode_attention_paged(Q: torch.Tensor, K_pages: torch.Tensor, V_pages: torc
 
 
 # ---- the decode loop around a compacted cache --------------------------------------------------
-def _dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
+def _type(dtype: torch.dtype) -> int:
+    if dtype == torch.bfloat16:
         return FC_BF16
-    if t.dtype == torch.float32:
+    if dtype == torch.float32:
         return FC_F32
-    raise ValueError(f"unsupported dtype {t.dtype}")
+    raise ValueError(f"unsupported dtype {dtype}")
+
+
+def _dtype(t: torch.Tensor) -> int:
+    return _type(t.dtype)
 
 
 def _want(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape: Tuple[int, ...], index: int) -> None:
@@ -407,14 +411,22 @@ def rotary_plan(rotary_dim: int, theta: float = 10000.0, interleaved: bool = Fal
     return plan
 
 
-def _heads(x: torch.Tensor, out: torch.Tensor, what: str, index: int) -> FcHeadsDesc:
-    if out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != index or x.get_device() != index:
-        raise ValueError(f"{what} and its output must agree in shape and dtype and be on GPU {index}")
-    B, T, H, d = x.shape
-    (sb, st, sh, sd), (ob, ot, oh, od) = x.stride(), out.stride()
+@functools.lru_cache(maxsize=1024)
+def _heads_of(shape, out_shape, strides, out_strides, dtype) -> FcHeadsDesc:
+    """(By what it says alone: a descriptor takes as long to make as all checks of a call; the library reads it only.)"""
+    if out_shape != shape:
+        raise ValueError("Q, K and their outputs must agree in shape")
+    B, T, H, d = shape
+    (sb, st, sh, sd), (ob, ot, oh, od) = strides, out_strides
     if (sd != 1 or od != 1) and d > 1:
         raise ValueError("the head dimension must be contiguous")
-    return FcHeadsDesc(B, T, H, d, _dtype(x), 0, sb, st, sh, ob, ot, oh)
+    return FcHeadsDesc(B, T, H, d, _type(dtype), 0, sb, st, sh, ob, ot, oh)
+
+
+def _heads(x: torch.Tensor, out: torch.Tensor, what: str, index: int) -> FcHeadsDesc:
+    if out.dtype is not x.dtype or out.get_device() != index or x.get_device() != index:
+        raise ValueError(f"{what} and its output must agree in shape and dtype and be on GPU {index}")
+    return _heads_of(x.shape, out.shape, x.stride(), out.stride(), x.dtype)
 
 
 def rotary(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K: Optional[torch.Tensor] = None,
@@ -501,17 +513,24 @@ def _mx_pages(pages: torch.Tensor, page_size: int, head_dim: int, index: int) ->
     return n
 
 
-def _mx_rows(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, index: int) -> FcRowsDesc:
-    if K.dim() != 3 or K.shape != V.shape or K.dtype is not V.dtype or V.get_device() != index:
-        raise ValueError("K and V must have shape [B, R, d], the same strides, dtype and device")
-    B, R, d = K.shape
-    strides, others = K.stride(), V.stride()
-    if strides != others and any(n > 1 and s != o for n, s, o in zip(K.shape, strides, others)):
+@functools.lru_cache(maxsize=1024)
+def _rows_of(shape, v_shape, strides, v_strides, dtype) -> FcRowsDesc:
+    if len(shape) != 3 or shape != v_shape:
+        raise ValueError("K and V must have shape [B, R, d]")
+    B, R, d = shape
+    if strides != v_strides and any(n > 1 and s != o for n, s, o in zip(shape, strides, v_strides)):
         raise ValueError("K and V must have the same strides")
     if strides[2] != 1 and d > 1:
         raise ValueError("the head dimension must be contiguous")
-    _want(slots, "slots", torch.int64, (B, R), index)
-    return FcRowsDesc(B, d, _dtype(K), 0, R, strides[0], strides[1])
+    return FcRowsDesc(B, d, _type(dtype), 0, R, strides[0], strides[1])
+
+
+def _mx_rows(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, index: int) -> FcRowsDesc:
+    if K.dtype is not V.dtype or V.get_device() != index:
+        raise ValueError("K and V must have the same dtype and device")
+    desc = _rows_of(K.shape, V.shape, K.stride(), V.stride(), K.dtype)
+    _want(slots, "slots", torch.int64, (desc.batch, desc.rows), index)
+    return desc
 
 
 def mx_store(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, page_size: int) -> None:
