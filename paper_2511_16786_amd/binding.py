@@ -555,8 +555,9 @@ def _described(K: torch.Tensor, V: torch.Tensor, desc: FcKvDesc, index: int) -> 
     shape = (desc.batch, desc.layers, desc.kv_heads, desc.n_tokens, desc.head_dim)
     strides = (desc.stride_b, desc.stride_l, desc.stride_h, desc.stride_n, 1)
     for t in (K, V):
-        if t.shape != shape or _dtype(t) != desc.dtype or t.get_device() != index or any(
-                n > 1 and s != o for n, s, o in zip(shape, strides, t.stride())):
+        given = t.stride()
+        if t.shape != shape or _dtype(t) != desc.dtype or t.get_device() != index or (given != strides and any(
+                n > 1 and s != o for n, s, o in zip(shape, strides, given))):
             raise ValueError("K and V must be what the descriptor describes")
 
 
