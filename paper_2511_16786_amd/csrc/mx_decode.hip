@@ -33,7 +33,8 @@ constexpr int kMxdThreads = 256, kMxdWaves = 4;
 constexpr int kAhead = 2;              // steps of rows under way in a wave
 constexpr int kLeastSteps = 4;         // of a piece
 // Waves that a SIMD holds by the registers of each form, and as many workgroups a compute unit, which all are resident together.  (With one step
-// under way and four workgroups in place of three: 28 layers of 4 heads that keep 6554 rows 29.2 us, 28.2 so.)
+// under way and four workgroups in place of three: 28 layers of 4 heads that keep 6554 rows 29.2 us, 28.2 so; four of the folded form 32.6 and 27.4,
+// three of fp32's in place of two 30.9 and 28.6.)
 constexpr int waves_held(int d, int terms) { return d == 64 ? 4 : terms > 1 ? 2 : 3; }
 constexpr int kMostRows = (1 << 25) - 1;
 constexpr float kSlack = 16.f;         // how far scores (in log2) may exceed the running reference before it is moved
