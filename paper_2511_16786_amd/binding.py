@@ -686,7 +686,8 @@ class MxCache:
     """A 4-bit paged cache and its block tables: filled from a compression, then extended and attended to step by step.
 
     Pure plumbing, as `Compressor`: buffers through torch, calls on the current stream, nothing read back.  Of `num_pages`
-    pages the first ones are taken as rows come; `missing()` (synchronising) says how many were asked for beyond them.
+    pages the first ones are taken as rows come, `max_pages` by a unit at most.  Rows without a page are counted in `rows`, but neither
+    stored nor attended to; `missing()` (synchronising) says how many pages they lack.
     A step is rotary (outside), append(k, v), attend(q), and may be captured into a graph (after one eager attend, which
     makes the workspace).  Calls of one cache have to follow each other: on one stream, or ordered by events."""
 
@@ -753,5 +754,8 @@ class MxCache:
                                    workspace=workspace)
 
     def missing(self) -> int:
-        """Pages that were asked for and not there (their rows are not stored): reads the cursor back."""
-        return max(0, int(self.cursor.item()) - self.num_pages)
+        """Pages that the counted rows lack (those rows are not stored): beyond `num_pages` of the pool, and beyond `max_pages`
+        of each unit's table, which the cursor does not count.  Reads rows and cursor back."""
+        heads, most = self.block_table.shape[2:]
+        pages = (self.rows.long() + (self.page_size - 1)) // self.page_size
+        return max(0, int(self.cursor.item()) - self.num_pages) + heads * int((pages - most).clamp_(min=0).sum().item())
