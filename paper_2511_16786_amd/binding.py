@@ -721,10 +721,16 @@ class MxCache:
         if not self._empty:
             raise ValueError("fill takes an empty cache: reset() first")
         _described(K, V, comp.desc, _here(K, "K"))
-        self._empty = False
+        if (K.data_ptr() | V.data_ptr()) % 16:
+            raise ValueError("K and V must be aligned to 16 bytes")
         assign_pages(self.rows, comp.budgets, self.page_size, self.block_table, self.cursor, num_free=self.num_pages)
-        select_gather_mx(K, V, comp.desc, comp.scores, comp.budgets, comp.layer_offsets, comp.rows_per_seq, comp.idx,
-                         self.block_table, self.page_size, self.pages, shared=comp.shared)
+        self._empty = False
+        try:
+            select_gather_mx(K, V, comp.desc, comp.scores, comp.budgets, comp.layer_offsets, comp.rows_per_seq, comp.idx,
+                             self.block_table, self.page_size, self.pages, shared=comp.shared)
+        except (ValueError, FlashCacheError):    # (too many rows for one launch, for instance: nothing of them is stored)
+            self.reset()
+            raise
 
     def append(self, k: torch.Tensor, v: torch.Tensor) -> None:
         """One row more for every unit: k, v [B, L, H, d] contiguous."""

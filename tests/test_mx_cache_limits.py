@@ -53,3 +53,51 @@ def test_rows_beyond_a_units_table_are_reported_as_missing():
     cache.reset()
     cache.fill(comp, K, V)
     assert cache.missing() == H * int((-(-comp.budgets // ps) - 2).clamp(min=0).sum()) > 0
+
+
+# ---- refused calls --------------------------------------------------------------------------------
+def _filled_state(cache):
+    return cache.rows.clone(), cache.cursor.clone(), cache.block_table.clone()
+
+
+def _compression(B, L, H, N, d, seed):
+    import paper_2511_16786_amd as fc
+    K, V = _rows((B, L, H, N, d), seed), _rows((B, L, H, N, d), seed + 1)
+    comp = fc.Compressor(K, 30, fc.total_budget(L, N, 0.3))
+    comp.run(K, V)
+    return comp, K, V
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", ["K", "V", "in the call"])
+def test_a_refused_fill_leaves_the_cache_empty(which, monkeypatch):
+    """Rows at addresses off by 8 bytes have the descriptor's strides, and what the library refuses of its own comes after the pages."""
+    import paper_2511_16786_amd as fc
+    from paper_2511_16786_amd import binding
+    B, L, H, N, d, ps = 1, 2, 2, 200, 64, 16
+    comp, K, V = _compression(B, L, H, N, d, 40)
+    cache = fc.MxCache(B, L, H, d, ps, -(-N // ps), 64)
+    held = _filled_state(cache)
+    if which == "in the call":
+        def refuse(*args, **kwargs):
+            raise fc.FlashCacheError(binding.FC_EUNSUPPORTED, "flashcache_select_gather_mx")
+        with monkeypatch.context() as m:
+            m.setattr(binding, "select_gather_mx", refuse)
+            with pytest.raises(fc.FlashCacheError):
+                cache.fill(comp, K, V)
+    else:
+        odd = torch.zeros(K.numel() + 4, dtype=K.dtype, device="cuda")[4:].view(K.shape)
+        with pytest.raises(ValueError):
+            cache.fill(comp, odd if which == "K" else K, odd if which == "V" else V)
+    for t, s in zip((cache.rows, cache.cursor, cache.block_table), held):
+        assert torch.equal(t, s)
+    cache.fill(comp, K, V)                               # (refused too, if the cache took itself for filled)
+    assert torch.equal(cache.rows, comp.budgets) and cache.missing() == 0
+    # row 0 of the first unit, as the packed copy has it in four bits
+    Ko, Vo = (torch.empty((1, 1, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    same, Kw, Vw = torch.zeros_like(cache.pages[:1]), torch.empty_like(Ko), torch.empty_like(Vo)
+    fc.mx_load(cache.block_table[:1, 0, 0, :1].long() * ps, cache.pages, ps, Ko, Vo)
+    first = torch.zeros((1, 1), dtype=torch.int64, device="cuda")
+    fc.mx_store(comp.K_out[:1, :1].contiguous(), comp.V_out[:1, :1].contiguous(), first, same, ps)
+    fc.mx_load(first, same, ps, Kw, Vw)
+    assert torch.equal(Ko, Kw) and torch.equal(Vo, Vw)
