@@ -754,7 +754,7 @@ class MxCache:
         heads = q.shape[2]
         workspace = self._workspaces.get(heads)
         if workspace is None:
-            workspace = torch.empty(max(_mx_decode_workspace(B, L, H, heads, d), 16), dtype=torch.uint8, device=q.device)
+            workspace = torch.empty(max(_mx_decode_workspace(B, L, H, heads, d), 16), dtype=torch.uint8, device=self.pages.device)
             self._workspaces[heads] = workspace
         return mx_decode_attention(q, self.pages, self.page_size, H, self.rows, self.block_table, scale, out=out,
                                    workspace=workspace)

@@ -101,3 +101,17 @@ def test_a_refused_fill_leaves_the_cache_empty(which, monkeypatch):
     fc.mx_store(comp.K_out[:1, :1].contiguous(), comp.V_out[:1, :1].contiguous(), first, same, ps)
     fc.mx_load(first, same, ps, Kw, Vw)
     assert torch.equal(Ko, Kw) and torch.equal(Vo, Vw)
+
+
+@pytest.mark.gpu
+def test_a_query_on_the_host_is_refused_and_no_more_than_that():
+    """The workspace is the cache's: a refused query of other whereabouts does not leave one behind that the next call cannot use."""
+    import paper_2511_16786_amd as fc
+    B, L, H, d, ps = 1, 2, 1, 64, 16
+    cache = fc.MxCache(B, L, H, d, ps, 2, 4)
+    k, v, q = _rows((B, L, H, d), 50), _rows((B, L, H, d), 51), _rows((B, L, 4 * H, d), 52)
+    cache.append(k, v)
+    with pytest.raises(ValueError):
+        cache.attend(q.cpu(), 0.1)
+    out = cache.attend(q, 0.1)
+    assert torch.equal(out, cache.attend(q, 0.1)) and bool(out.isfinite().all()) and bool(out.any())
