@@ -696,6 +696,8 @@ class MxCache:
         nbytes = mx_page_bytes(page_size, head_dim)
         if nbytes == 0:
             raise FlashCacheError(FC_EUNSUPPORTED, "flashcache_mx_page_bytes")
+        if max_pages < 1 or num_pages < 1:
+            raise ValueError("a cache has at least one page, and room for one in each table")
         self.page_size, self.num_pages = int(page_size), int(num_pages)
         self.shape = (int(batch), int(layers), int(kv_heads), int(head_dim))
         self.pages = torch.empty((num_pages, nbytes), dtype=torch.uint8, device=device)

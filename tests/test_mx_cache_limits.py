@@ -115,3 +115,11 @@ def test_a_query_on_the_host_is_refused_and_no_more_than_that():
         cache.attend(q.cpu(), 0.1)
     out = cache.attend(q, 0.1)
     assert torch.equal(out, cache.attend(q, 0.1)) and bool(out.isfinite().all()) and bool(out.any())
+
+
+@pytest.mark.parametrize("max_pages,num_pages", [(1, 0), (0, 1), (1, -1), (-1, 1)])
+def test_a_cache_without_pages_or_tables_is_refused(max_pages, num_pages):
+    """(It would count the first row and only then find that the store refuses a cache without pages.)"""
+    import paper_2511_16786_amd as fc
+    with pytest.raises(ValueError):
+        fc.MxCache(1, 1, 1, 64, 16, max_pages, num_pages, device="cpu")
