@@ -361,7 +361,7 @@ fc_status flashcache_assign_pages(const int32_t* rows, const int32_t* add, int32
  * whatever the memory holds; they may be read, and no attention reads rows from the given number on. */
 size_t flashcache_mx_page_bytes(int32_t page_size, int32_t head_dim);   /* 0 if unsupported */
 
-/* Rows of K and of V: row r of sequence b begins at base + b*stride_b + r*stride_r elements.  Fewer than 2^29 rows. */
+/* Rows of K and of V: row r of sequence b begins at base + b*stride_b + r*stride_r elements.  Up to 2^29 - 32 rows. */
 typedef struct {
   int32_t batch, head_dim, dtype, reserved;
   int64_t rows, stride_b, stride_r;

@@ -457,8 +457,8 @@ static fc_status check_mx_rows(const fc_rows_desc* d, const void* K, const void*
   if (st != FC_OK) return st;
   const int64_t e = d->dtype == FC_BF16 ? 2 : 4;
   if (d->stride_b < 0 || d->stride_r < 0 || (d->batch > 1 && (d->stride_b * e) % 16) || (d->rows > 1 && (d->stride_r * e) % 16)) return FC_EINVAL;
-  // (a workgroup of 256 threads has 32 rows, and a launch fewer than 2^32 threads)
-  if (d->batch > 65535 || d->rows >= (1 << 29)) return FC_EUNSUPPORTED;
+  // (a workgroup of 256 threads has 32 rows, the last one fewer, and a launch fewer than 2^32 threads)
+  if (d->batch > 65535 || d->rows > (1 << 29) - 32) return FC_EUNSUPPORTED;
   if (d->batch == 0 || d->rows == 0) return FC_OK;
   if (!K || !V || !slots || !pages) return FC_EINVAL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(pages) || (reinterpret_cast<uintptr_t>(slots) & 7u)) return FC_EINVAL;

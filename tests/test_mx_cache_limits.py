@@ -123,3 +123,13 @@ def test_a_cache_without_pages_or_tables_is_refused(max_pages, num_pages):
     import paper_2511_16786_amd as fc
     with pytest.raises(ValueError):
         fc.MxCache(1, 1, 1, 64, 16, max_pages, num_pages, device="cpu")
+
+
+@pytest.mark.parametrize("rows", [(1 << 29) - 31, (1 << 29) - 1])
+def test_rows_whose_launch_would_have_two_to_the_32_threads_are_refused(rows):
+    """256 threads for each 32 rows, begun ones too: nothing is launched, on no machine."""
+    from paper_2511_16786_amd import binding as b
+    for d in (64, 128):
+        desc = b.FcRowsDesc(1, d, b.FC_BF16, 0, rows, rows * d, d)
+        assert b._lib.flashcache_mx_store(32, 32, ctypes.byref(desc), 32, 16, 4, 32, None) == b.FC_EUNSUPPORTED
+        assert b._lib.flashcache_mx_load(32, 32, 16, 4, ctypes.byref(desc), 32, 32, None) == b.FC_EUNSUPPORTED
