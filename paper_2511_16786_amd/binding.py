@@ -434,8 +434,12 @@ def rotary(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K: Opti
            inverse: bool = False) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Rotary positions of Q [B, T, Hq, d] and K [B, T, Hk, d] (any strides, innermost contiguous); positions int32
     [B, T], or [streams, B, T].  Q_out / K_out may be Q and K themselves; without them new tensors are returned.
-    inverse: the transposed map, which takes gradients of the outputs to gradients of the inputs."""
+    inverse: the transposed map, which takes gradients of the outputs to gradients of the inputs.  The call records nothing for
+    autograd: tensors that want gradients are refused unless recording is off, as in an autograd.Function's forward and backward."""
     index = _here(Q, "Q")
+    if torch.is_grad_enabled() and (Q.requires_grad or K is not None and K.requires_grad or Q_out is not None and
+                                    Q_out.requires_grad or K_out is not None and K_out.requires_grad):
+        raise ValueError("rotary records no gradients: call it under torch.no_grad() or in an autograd.Function (backward: inverse=True)")
     if Q.dim() != 4 or (K is not None and (K.dim() != 4 or K.shape[:2] != Q.shape[:2])):
         raise ValueError("Q and K must have shape [B, T, H, d], with B and T in common")
     if plan.streams == 1 and positions.dim() == 2:
