@@ -494,7 +494,7 @@ def assign_pages(rows: torch.Tensor, add, page_size: int, block_table: torch.Ten
             raise ValueError("num_free exceeds the list")
     per_seq = 0
     if slots is not None:
-        per_seq = slots.numel() // max(B, 1)
+        per_seq = slots.shape[-1] if slots.dim() else 0
         _want(slots, "slots", torch.int64, (B, per_seq), index)
     _check(_lib.flashcache_assign_pages(
         rows.data_ptr(), add_ptr, each, B, L, H, page_size, most, _ptr(free_pages), num_free, cursor.data_ptr(),

@@ -133,3 +133,17 @@ def test_rows_whose_launch_would_have_two_to_the_32_threads_are_refused(rows):
         desc = b.FcRowsDesc(1, d, b.FC_BF16, 0, rows, rows * d, d)
         assert b._lib.flashcache_mx_store(32, 32, ctypes.byref(desc), 32, 16, 4, 32, None) == b.FC_EUNSUPPORTED
         assert b._lib.flashcache_mx_load(32, 32, 16, 4, ctypes.byref(desc), 32, 32, None) == b.FC_EUNSUPPORTED
+
+
+@pytest.mark.gpu
+def test_a_batch_of_no_sequences_is_appended_and_attended_to():
+    import paper_2511_16786_amd as fc
+    L, H, d, ps = 2, 2, 64, 16
+    cache = fc.MxCache(0, L, H, d, ps, 2, 4)
+    none = torch.empty((0, L, H, d), dtype=torch.bfloat16, device="cuda")
+    cache.append(none, none)
+    assert cache.attend(torch.empty((0, L, 3 * H, d), dtype=torch.bfloat16, device="cuda"), 0.1).shape == (0, L, 3 * H, d)
+    assert cache.missing() == 0
+    with pytest.raises(ValueError):                      # a map of another batch
+        fc.assign_pages(cache.rows, 1, ps, cache.block_table, cache.cursor, num_free=4,
+                        slots=torch.empty((1, 4), dtype=torch.int64, device="cuda"))
