@@ -478,6 +478,8 @@ def assign_pages(rows: torch.Tensor, add, page_size: int, block_table: torch.Ten
         add_ptr = add.data_ptr()
     else:
         each = int(add)
+        if not -2 ** 31 <= each < 2 ** 31:
+            raise ValueError("a number of rows has 32 bits")
     rows_out = rows if rows_out is None else rows_out
     cursor_out = cursor if cursor_out is None else cursor_out
     _want(rows, "rows", torch.int32, (B, L), index)

@@ -147,3 +147,17 @@ def test_a_batch_of_no_sequences_is_appended_and_attended_to():
     with pytest.raises(ValueError):                      # a map of another batch
         fc.assign_pages(cache.rows, 1, ps, cache.block_table, cache.cursor, num_free=4,
                         slots=torch.empty((1, 4), dtype=torch.int64, device="cuda"))
+
+
+@pytest.mark.gpu
+def test_a_number_of_rows_beyond_32_bits_is_refused():
+    """(It was cut to its lower half: 2^32 + 1 rows were one.)  What 32 bits hold is cut to the most rows that are counted."""
+    import paper_2511_16786_amd as fc
+    rows, cursor = torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    table = torch.full((1, 2, 1, 3), -1, dtype=torch.int32, device="cuda")
+    for add in (2 ** 32 + 1, 2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(ValueError):
+            fc.assign_pages(rows, add, 16, table, cursor, num_free=9)
+    assert not bool(rows.any()) and int(cursor) == 0
+    fc.assign_pages(rows, 2 ** 31 - 1, 16, table, cursor, num_free=9)
+    assert bool((rows == 2 ** 25 - 1).all()) and int(cursor) == 6 and table.view(-1).tolist() == list(range(6))
