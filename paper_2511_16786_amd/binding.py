@@ -388,8 +388,9 @@ def rotary_plan(rotary_dim: int, theta: float = 10000.0, interleaved: bool = Fal
                 frequencies: Optional[Sequence[float]] = None) -> FcRotaryPlan:
     """What `rotary` needs (host memory; may be kept and used by any number of calls and threads).
 
-    scaling: "none", "linear", "base" or "parts" (flashcache.h has the formulas); sections: pairs that each of 2 to 4 streams
-    of positions turns; frequencies: radians per position of each pair, instead of theta and the scaling."""
+    scaling: "none", "linear", "base" or "parts" (flashcache.h has the formulas; "parts" mixes by the turns of a pair, not by its
+    number); sections: pairs that each of 2 to 4 streams of positions turns; frequencies: radians per position of each pair,
+    instead of theta and the scaling (a magnitude other than 1 has to be given then)."""
     spec = FcRotarySpec(rotary_dim=rotary_dim, interleaved=1 if interleaved else 0, scaling=ROTARY_SCALINGS[scaling],
                         original_tokens=original_tokens, streams=1, theta=theta, factor=factor, beta_fast=beta_fast,
                         beta_slow=beta_slow, magnitude=magnitude)
@@ -595,7 +596,7 @@ def mx_decode_attention(Q: torch.Tensor, pages: torch.Tensor, page_size: int, kv
                         block_table: torch.Tensor, scale: float, out: Optional[torch.Tensor] = None,
                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Q [B, L, Hq, d]; pages uint8 [num_pages, mx_page_bytes]; rows int32 [B, L]; block_table int32
-    [B, L, H, max_pages]; returns float32 [B, L, Hq, d]."""
+    [B, L, H, max_pages]; returns float32 [B, L, Hq, d].  An operator of inference: no gradients."""
     shape = Q.shape
     B, L, Hq, d = shape
     index = _here(Q, "Q")
@@ -695,7 +696,10 @@ class MxCache:
     pages the first ones are taken as rows come, `max_pages` by a unit at most.  Rows without a page are counted in `rows`, but neither
     stored nor attended to; `missing()` (synchronising) says how many pages they lack.
     A step is rotary (outside), append(k, v), attend(q), and may be captured into a graph (after one eager attend, which
-    makes the workspace).  Calls of one cache have to follow each other: on one stream, or ordered by events."""
+    makes the workspace).  Both take all layers at once; layer by layer, as a model runs, a step is assign_pages over the cache's
+    tensors (all layers), then for layer l mx_store into slots[:, l*H:(l+1)*H] and mx_decode_attention over rows[:, l:l+1] and
+    block_table[:, l:l+1], of which several sequences need contiguous copies.
+    Calls of one cache have to follow each other: on one stream, or ordered by events."""
 
     def __init__(self, batch: int, layers: int, kv_heads: int, head_dim: int, page_size: int, max_pages: int,
                  num_pages: int, device="cuda"):
