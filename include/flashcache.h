@@ -288,7 +288,8 @@ fc_status flashcache_decode_attention_paged(const void* Q, const void* K_pages, 
  *   FC_ROTARY_BASE    theta * s^(rotary_dim / (rotary_dim - 2)) in place of theta
  *   FC_ROTARY_PARTS   by the turns n_i = original_tokens * f_i / (2 pi) that a pair makes over the original context: f_i from beta_fast turns
  *                     on, f_i / s up to beta_slow, and between them f_i g + (f_i / s) (1 - g) with g = (n_i - beta_slow) / (beta_fast -
- *                     beta_slow); m = 0.1 ln s + 1
+ *                     beta_slow); m = 0.1 ln s + 1.  g is linear in the turns, as the method defines it; model code often takes it linear in i,
+ *                     between the two pairs (rounded) that make beta_fast and beta_slow turns: pass such frequencies in `frequencies`
  * `streams` (1 to 4) sequences of positions share out the pairs: the first stream_pairs[0] pairs turn by the first one, the next
  * stream_pairs[1] by the second (time, height and width of images, for instance); with one stream stream_pairs is not read.
  * `magnitude` m, 0: as above, 1 without FC_ROTARY_PARTS. */

@@ -16,7 +16,6 @@ namespace fc {
 // Codes: two a byte, the lower nibble the even column.  Scales: E of 2^(E - 127) for 32 columns.
 template <int D> struct MxTile {
   static constexpr int kBytes = 17 * D, kV = 8 * D, kScales = 16 * D, kVScales = 16 * D + D / 2;
-  static constexpr int kBlocks = D / 32;
   __host__ __device__ static constexpr int k_code(int row, int byte) { return row * (D / 2) + byte; }
   __host__ __device__ static constexpr int v_code(int row, int n) { return kV + row / 4 * (2 * D) + n * (D / 8) + row % 4 * (D / 32); }
   __host__ __device__ static constexpr int k_scale(int row, int block) { return kScales + block * 16 + row; }
