@@ -398,6 +398,81 @@ fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const
                                          const int32_t* rows, float scale, float* out, void* workspace,
                                          size_t workspace_bytes, void* hip_stream);
 
+/* ---- decode steps over the paged cache of bf16 or fp32 rows ------------------------------------------------------------------------ */
+
+/* A paged cache as flashcache_select_gather_paged writes it: row j of unit (b,l,h) is in slot j % page_size of page block_table[b][l][h][j /
+ * page_size] of K and V [num_pages][page_size][head_dim], all pointers device.  rows [batch][layers] are the rows that every head of a layer
+ * holds (negative values count as 0, what the table does not reach is not there), block_table [batch][layers][kv_heads][max_pages]; both may be a layer's
+ * slice of a larger one, with `rows_stride_b` and `table_stride_b` elements from a sequence to the next.  Pages that are negative or from num_pages on
+ * are not there, and neither are their rows.  Fewer than 2^32 - 1 rows in all pages; K and V aligned to 16 bytes, rows multiples of 16 bytes. */
+typedef struct {
+  int32_t batch, layers, kv_heads, head_dim;
+  int32_t dtype, page_size, max_pages, reserved;             /* fc_dtype */
+  int64_t num_pages, rows_stride_b, table_stride_b;
+  const void *K, *V;
+  const int32_t *rows, *block_table;
+} fc_paged_kv;
+
+/* New tokens into a paged cache, in one launch: Q and K turned by their positions as flashcache_rotary does, Q to Q_out, K and V to their slots.
+ *   plan, positions  as for flashcache_rotary
+ *   Q, Q_out   device in / out, [batch][tokens][heads][head_dim] by q_desc; Q_out may be Q itself (same strides)
+ *   K, V       device in, by k_desc and v_desc (as many heads in both; the out_ strides are not read)
+ *   slots      device in, int64: of token t of head h of sequence b at b*slots_stride_b + h*slots_stride_h + t, page * page_size + place, as
+ *              flashcache_assign_pages makes them; rows whose slot is negative or beyond the pages are left out.  No slot may come twice in a call
+ *   K_pages, V_pages  device out, [num_pages][page_size][head_dim]; other slots stay as they are
+ *   bounds     device in/out or NULL, [num_pages][2][head_dim] in the input dtype: the lowest and the largest key of every column in each page.  Those of a
+ *              page whose first row (place 0) is among the new ones are made from the new rows, those of other touched pages are
+ *              widened.  The rows of a page are to follow each other as tokens of one head of one sequence (else what a page's bounds hold is
+ *              unspecified); a NaN does not change bounds, a column of NaNs alone has +infinity and -infinity
+ * Any even head_dim from rotary_dim to 512, fewer than 2^24 tokens of all sequences, launches below 2^24 workgroups; no output may overlap another
+ * or an input, other than Q_out. */
+fc_status flashcache_append_paged(const fc_rotary_plan* plan, const int32_t* positions, const void* Q, void* Q_out, const fc_heads_desc* q_desc,
+                                  const void* K, const fc_heads_desc* k_desc, const void* V, const fc_heads_desc* v_desc, const int64_t* slots,
+                                  int64_t slots_stride_b, int64_t slots_stride_h, int32_t page_size, int64_t num_pages, void* K_pages,
+                                  void* V_pages, void* bounds, void* hip_stream);
+
+/* Bounds (as above) of all pages that hold rows, from the cache; those of other pages stay as they are.  kv->V is not read.  Rows up to 1024 bytes. */
+fc_status flashcache_page_bounds(const fc_paged_kv* kv, void* bounds, void* hip_stream);
+
+/* The pages of each unit that its q_heads / kv_heads = G queries can score highest in: `count` places in its table, rising, -1 behind the last.  A page's
+ * score is the sum over the G queries of the largest dot product that a key within its bounds can have, sum_g sum_c max(q_gc low_c, q_gc high_c), in 64
+ * bits, rounded to 32.  The first `first` and the last `last` of the pages that hold a unit's rows are taken whatever their scores (first + last <=
+ * count), then those of largest score, the earlier one of two alike; pages that are not there never, those whose score is not a number last.
+ *   Q       device in, [B][L][q_heads][d] in the cache's dtype, of kv's batch, layers and head_dim;  bounds  as above;  kv's K and V are not read
+ *   chosen  device out, int32 [B][L][kv_heads][count]
+ *   workspace  device, 16-byte aligned, flashcache_choose_pages_workspace_bytes() bytes; calls that may run at the same time need one each
+ * d in {64, 128}, G from 1 to 16. */
+size_t flashcache_choose_pages_workspace_bytes(const fc_paged_kv* kv);
+fc_status flashcache_choose_pages(const void* Q, int32_t q_heads, const fc_paged_kv* kv, const void* bounds, int32_t count, int32_t first,
+                                  int32_t last, int32_t* chosen, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* flashcache_decode_attention_paged over the rows of the chosen pages alone: one new token a sequence attends to the rows that each unit holds in the pages
+ * at places chosen[b][l][h][0 .. count) of its table.  Places that are negative, beyond the table or without a page are left out, a place that comes
+ * twice counts twice; a unit without attended rows gives zeros.
+ *   Q    device in, [B][L][q_heads][d] in the cache's dtype; out  device out, float [B][L][q_heads][d]
+ *   workspace  device, 16-byte aligned, flashcache_decode_chosen_workspace_bytes() bytes (may be 0); one for each call that may run at the same time
+ * d in {64, 128}, 1 to 16 query heads a KV head for both dtypes, count * page_size below 2^30.  Products on the matrix cores: of bf16 exact in fp32, with
+ * probabilities of 17 bits; of fp32 in fp32.  Sums and softmax in fp32. */
+size_t flashcache_decode_chosen_workspace_bytes(const fc_paged_kv* kv, int32_t q_heads, int32_t count);
+fc_status flashcache_decode_attention_chosen(const void* Q, int32_t q_heads, const fc_paged_kv* kv, const int32_t* chosen, int32_t count, float scale,
+                                             float* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Decode-step attention of sequences that share the rows of a prompt (several answers to it, for instance): sequence b attends to the rows that
+ * common holds for prompt p, where starts[p] <= b < starts[p + 1], and then to its own.  A prompt's rows are read once for up to 16 query heads of its
+ * sequences together.
+ *   Q       device in, [B][L][q_heads][d] in the caches' dtype
+ *   common  the prompts' cache, batch = P of them (0 or more); own  the sequences', batch = B; layers, kv_heads, head_dim and dtype are the same in both,
+ *           pages may be of different sizes, and the pages' memory the same
+ *   starts  device in, int32 [P + 1], not falling; values outside [0, B] count as its ends.  Sequences before the first start and from the last on have rows
+ *           of their own alone.  (Starts that fall give unspecified values)
+ *   out     device out, float [B][L][q_heads][d]; a unit without attended rows gives zeros
+ *   workspace  device, 16-byte aligned, flashcache_decode_shared_workspace_bytes() bytes; calls that may run at the same time need one each
+ * d in {64, 128}, 1 to 16 query heads a KV head; precision as for flashcache_decode_attention_chosen. */
+size_t flashcache_decode_shared_workspace_bytes(int32_t prompts, int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads, int32_t head_dim,
+                                                int32_t dtype);
+fc_status flashcache_decode_attention_shared(const void* Q, int32_t q_heads, const fc_paged_kv* common, const int32_t* starts, const fc_paged_kv* own,
+                                             float scale, float* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Measurement aid (off by default; not part of the method).  While enabled, every kernel the
  * library launches is bracketed by a pair of HIP events on its launch stream.
  * flashcache_profile_enable(on) clears the records and switches recording on or off.

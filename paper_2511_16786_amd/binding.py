@@ -36,6 +36,9 @@ EXPORTED_SYMBOLS = (
     "flashcache_rotary_prepare", "flashcache_rotary", "flashcache_assign_pages", "flashcache_mx_page_bytes",
     "flashcache_mx_store", "flashcache_mx_load", "flashcache_select_gather_mx", "flashcache_mx_decode_workspace_bytes",
     "flashcache_mx_decode_attention",
+    "flashcache_append_paged", "flashcache_page_bounds", "flashcache_choose_pages_workspace_bytes", "flashcache_choose_pages",
+    "flashcache_decode_chosen_workspace_bytes", "flashcache_decode_attention_chosen", "flashcache_decode_shared_workspace_bytes",
+    "flashcache_decode_attention_shared",
     "flashcache_profile_enable", "flashcache_profile_read",
 )
 
@@ -84,6 +87,15 @@ class FcRowsDesc(ctypes.Structure):
     _fields_ = [
         ("batch", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
         ("rows", ctypes.c_int64), ("stride_b", ctypes.c_int64), ("stride_r", ctypes.c_int64),
+    ]
+
+
+class FcPagedKv(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("layers", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("num_pages", ctypes.c_int64), ("rows_stride_b", ctypes.c_int64), ("table_stride_b", ctypes.c_int64),
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("rows", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
     ]
 
 
@@ -155,7 +167,20 @@ def _load() -> ctypes.CDLL:
     lib.flashcache_mx_decode_workspace_bytes.restype = sz
     lib.flashcache_mx_decode_attention.argtypes = [vp, vp, vp, i32, i32, i64, i32, i32, i32, i32, i32, i32, vp,
                                                    ctypes.c_float, vp, vp, sz, vp]
-    for name in ("rotary_prepare", "rotary", "assign_pages", "mx_store", "mx_load", "select_gather_mx", "mx_decode_attention"):
+    heads_p, paged_p, f32 = ctypes.POINTER(FcHeadsDesc), ctypes.POINTER(FcPagedKv), ctypes.c_float
+    lib.flashcache_append_paged.argtypes = [ctypes.POINTER(FcRotaryPlan), vp, vp, vp, heads_p, vp, heads_p, vp, heads_p, vp, i64, i64,
+                                            i32, i64, vp, vp, vp, vp]
+    lib.flashcache_page_bounds.argtypes = [paged_p, vp, vp]
+    lib.flashcache_choose_pages_workspace_bytes.argtypes, lib.flashcache_choose_pages_workspace_bytes.restype = [paged_p], sz
+    lib.flashcache_choose_pages.argtypes = [vp, i32, paged_p, vp, i32, i32, i32, vp, vp, sz, vp]
+    lib.flashcache_decode_chosen_workspace_bytes.argtypes = [paged_p, i32, i32]
+    lib.flashcache_decode_chosen_workspace_bytes.restype = sz
+    lib.flashcache_decode_attention_chosen.argtypes = [vp, i32, paged_p, vp, i32, f32, vp, vp, sz, vp]
+    lib.flashcache_decode_shared_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32]
+    lib.flashcache_decode_shared_workspace_bytes.restype = sz
+    lib.flashcache_decode_attention_shared.argtypes = [vp, i32, paged_p, vp, paged_p, f32, vp, vp, sz, vp]
+    for name in ("rotary_prepare", "rotary", "assign_pages", "mx_store", "mx_load", "select_gather_mx", "mx_decode_attention", "append_paged",
+                 "page_bounds", "choose_pages", "decode_attention_chosen", "decode_attention_shared"):
         getattr(lib, "flashcache_" + name).restype = i32
     lib.flashcache_status_string.argtypes, lib.flashcache_status_string.restype = [i32], ctypes.c_char_p
     return lib
@@ -617,6 +642,204 @@ def mx_decode_attention(Q: torch.Tensor, pages: torch.Tensor, page_size: int, kv
         Q.data_ptr(), pages.data_ptr(), block_table.data_ptr(), page_size, most, n, B, L, kv_heads, Hq, d, _dtype(Q),
         rows.data_ptr(), scale, out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()),
         "flashcache_mx_decode_attention")
+    return out
+
+
+# ---- decode steps over the paged cache of bf16 or fp32 rows ------------------------------------
+class PagedKV:
+    """A paged cache as `select_gather_paged` fills it and the calls below take it: K, V [num_pages, page_size, d]; rows int32 [B, L] that
+    every head of a layer holds; block_table int32 [B, L, H, max_pages].  rows and block_table may be a layer's slices, rows[:, l:l+1] and
+    block_table[:, l:l+1].
+
+    A view that reads nothing: it keeps the four tensors, whose contents may change between calls, and where they are."""
+
+    __slots__ = ("K", "V", "rows", "block_table", "shape", "dtype", "index", "_desc", "_ref")
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, rows: torch.Tensor, block_table: torch.Tensor):
+        if K.dim() != 3 or block_table.dim() != 4:
+            raise ValueError("K and V must have shape [num_pages, page_size, d], block_table [B, L, H, max_pages]")
+        pages, page_size, d = K.shape
+        B, L, H, most = block_table.shape
+        index = K.get_device()
+        if index < 0:
+            raise ValueError("K must be on a GPU")
+        _want(K, "K", K.dtype, K.shape, index)
+        _want(V, "V", K.dtype, K.shape, index)
+        if rows.dtype is not torch.int32 or rows.shape != (B, L) or rows.get_device() != index or (L > 1 and rows.stride(1) != 1):
+            raise ValueError(f"rows must be a torch.int32 tensor of shape {(B, L)} on GPU {index}, its layers side by side")
+        if block_table.dtype is not torch.int32 or block_table.get_device() != index or any(
+                n > 1 and s != t for n, s, t in zip((L, H, most), block_table.stride()[1:], (H * most, most, 1))):
+            raise ValueError(f"block_table must be a torch.int32 tensor on GPU {index}, what is a sequence's contiguous")
+        if K.requires_grad or V.requires_grad:
+            raise ValueError("the cache's attention records no gradients")
+        self.K, self.V, self.rows, self.block_table = K, V, rows, block_table
+        self.shape, self.dtype, self.index = (B, L, H, d), K.dtype, index
+        self._desc = FcPagedKv(B, L, H, d, _dtype(K), page_size, most, 0, pages, rows.stride(0) if B > 1 else 0,
+                               block_table.stride(0) if B > 1 else 0, K.data_ptr(), V.data_ptr(), rows.data_ptr(), block_table.data_ptr())
+        self._ref = ctypes.byref(self._desc)
+
+
+@functools.lru_cache(maxsize=1024)
+def _new_rows_of(shape, strides, dtype) -> FcHeadsDesc:
+    B, T, H, d = shape
+    sb, st, sh, sd = strides
+    if sd != 1 and d > 1:
+        raise ValueError("the head dimension must be contiguous")
+    return FcHeadsDesc(B, T, H, d, _type(dtype), 0, sb, st, sh, 0, 0, 0)
+
+
+def append_paged(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor,
+                 K_pages: torch.Tensor, V_pages: torch.Tensor, Q_out: Optional[torch.Tensor] = None,
+                 bounds: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """New tokens into a paged cache: Q [B, T, Hq, d] turned by `positions` (as `rotary` takes them) into Q_out, which is returned (a new tensor
+    unless given, or Q itself); K and V [B, T, H, d], K turned, into the slots int64 [B, H, T] (negative: left out; a layer's slice of the map
+    that `assign_pages` makes) of K_pages, V_pages [num_pages, page_size, d].  bounds [num_pages, 2, d]: lowest and largest key of each page
+    and column, brought up to date.  Any strides of Q, K and V, innermost contiguous.  Records no gradients."""
+    index = _here(Q, "Q")
+    if torch.is_grad_enabled() and (Q.requires_grad or K.requires_grad or V.requires_grad or K_pages.requires_grad or V_pages.requires_grad or
+                                    Q_out is not None and Q_out.requires_grad or bounds is not None and bounds.requires_grad):
+        raise ValueError("append_paged records no gradients: call it under torch.no_grad()")
+    shape, kv_shape = Q.shape, K.shape
+    if len(shape) != 4 or len(kv_shape) != 4 or kv_shape[:2] != shape[:2] or kv_shape[3] != shape[3] or V.shape != kv_shape:
+        raise ValueError("Q, K and V must have shape [B, T, H, d], K and V as many heads, all with B, T and d in common")
+    B, T, H, d = kv_shape
+    dtype = Q.dtype
+    if K.dtype is not dtype or V.dtype is not dtype or K.get_device() != index or V.get_device() != index:
+        raise ValueError(f"Q, K and V must have the same dtype and be on GPU {index}")
+    if plan.streams == 1 and positions.dim() == 2:
+        _want(positions, "positions", torch.int32, (B, T), index)
+    else:
+        _want(positions, "positions", torch.int32, (plan.streams, B, T), index)
+    if K_pages.dim() != 3:
+        raise ValueError("K_pages and V_pages must have shape [num_pages, page_size, d]")
+    pages, page_size = K_pages.shape[:2]
+    _want(K_pages, "K_pages", dtype, (pages, page_size, d), index)
+    _want(V_pages, "V_pages", dtype, (pages, page_size, d), index)
+    _want(bounds, "bounds", dtype, (pages, 2, d), index)
+    if slots.dtype is not torch.int64 or slots.shape != (B, H, T) or slots.get_device() != index or (T > 1 and slots.stride(2) != 1):
+        raise ValueError(f"slots must be a torch.int64 tensor of shape {(B, H, T)} on GPU {index}, a head's tokens side by side")
+    if Q_out is None:
+        Q_out = torch.empty(shape, dtype=dtype, device=Q.device)
+    qd = _heads(Q, Q_out, "Q", index)
+    _check(_lib.flashcache_append_paged(
+        ctypes.byref(plan), positions.data_ptr(), Q.data_ptr(), Q_out.data_ptr(), ctypes.byref(qd), K.data_ptr(),
+        ctypes.byref(_new_rows_of(kv_shape, K.stride(), dtype)), V.data_ptr(), ctypes.byref(_new_rows_of(kv_shape, V.stride(), dtype)),
+        slots.data_ptr(), slots.stride(0), slots.stride(1), page_size, pages, K_pages.data_ptr(), V_pages.data_ptr(), _ptr(bounds), _stream()),
+        "flashcache_append_paged")
+    return Q_out
+
+
+def _bounds(kv: PagedKV, bounds: torch.Tensor) -> None:
+    _want(bounds, "bounds", kv.dtype, (kv.K.shape[0], 2, kv.shape[3]), kv.index)
+
+
+def page_bounds(kv: PagedKV, bounds: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Lowest and largest key of every column of each page that holds rows, into bounds [num_pages, 2, d], which is returned (a new tensor
+    unless given); what it has for other pages stays as it is (0 in a new one)."""
+    _here(kv.K, "the cache")
+    if bounds is None:
+        bounds = torch.zeros((kv.K.shape[0], 2, kv.shape[3]), dtype=kv.dtype, device=kv.K.device)
+    _bounds(kv, bounds)
+    _check(_lib.flashcache_page_bounds(kv._ref, bounds.data_ptr(), _stream()), "flashcache_page_bounds")
+    return bounds
+
+
+def _queries(Q: torch.Tensor, kv: PagedKV) -> int:
+    """Queries of the cache's shape on the current GPU."""
+    index = _here(Q, "Q")
+    if torch.is_grad_enabled() and Q.requires_grad:
+        raise ValueError("the cache's attention records no gradients: call it under torch.no_grad()")
+    B, L, H, d = kv.shape
+    if Q.dim() != 4:
+        raise ValueError("Q must have shape [B, L, Hq, d]")
+    _want(Q, "Q", kv.dtype, (B, L, Q.shape[2], d), index)
+    if kv.index != index:
+        raise ValueError(f"the cache must be on GPU {index}")
+    return index
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor, index: int) -> torch.Tensor:
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=like.device)
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on GPU {index}")
+    return workspace
+
+
+def _chosen_bytes(kv: PagedKV, q_heads: int, count: int) -> int:
+    return max(int(_lib.flashcache_choose_pages_workspace_bytes(kv._ref)), int(_lib.flashcache_decode_chosen_workspace_bytes(kv._ref, q_heads, count)))
+
+
+def chosen_workspace(Q: torch.Tensor, kv: PagedKV, count: int) -> torch.Tensor:
+    """A workspace for `choose_pages` and `decode_attention_chosen` of this shape, one after the other."""
+    return torch.empty(max(_chosen_bytes(kv, Q.shape[2], count), 16), dtype=torch.uint8, device=Q.device)
+
+
+def choose_pages(Q: torch.Tensor, kv: PagedKV, bounds: torch.Tensor, count: int, first: int = 1, last: int = 1,
+                 chosen: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The `count` pages of each unit that Q [B, L, Hq, d] can score highest in by the pages' bounds, the first `first` and the last `last`
+    among them whatever their scores: places in its block table int32 [B, L, H, count], rising, -1 behind the last."""
+    index = _queries(Q, kv)
+    _bounds(kv, bounds)
+    shape = (*kv.shape[:3], count)
+    if chosen is None:
+        chosen = torch.empty(shape, dtype=torch.int32, device=Q.device)
+    else:
+        _want(chosen, "chosen", torch.int32, shape, index)
+    workspace = _scratch(workspace, 0 if workspace is not None else _chosen_bytes(kv, Q.shape[2], count), Q, index)
+    _check(_lib.flashcache_choose_pages(Q.data_ptr(), Q.shape[2], kv._ref, bounds.data_ptr(), count, first, last, chosen.data_ptr(),
+                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "flashcache_choose_pages")
+    return chosen
+
+
+def decode_attention_chosen(Q: torch.Tensor, kv: PagedKV, chosen: torch.Tensor, scale: float, out: Optional[torch.Tensor] = None,
+                            workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of one new token a sequence, Q [B, L, Hq, d], over the rows in the pages at the places chosen int32 [B, L, H, count] of
+    each unit's block table (negative: none); returns float32 [B, L, Hq, d].  An operator of inference: no gradients."""
+    index = _queries(Q, kv)
+    count = chosen.shape[-1] if chosen.dim() else 0
+    _want(chosen, "chosen", torch.int32, (*kv.shape[:3], count), index)
+    workspace = _scratch(workspace, 0 if workspace is not None else _chosen_bytes(kv, Q.shape[2], count), Q, index)
+    if out is None:
+        out = torch.empty(Q.shape, dtype=torch.float32, device=Q.device)
+    else:
+        _want(out, "out", torch.float32, Q.shape, index)
+    _check(_lib.flashcache_decode_attention_chosen(
+        Q.data_ptr(), Q.shape[2], kv._ref, chosen.data_ptr(), count, scale, out.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream()), "flashcache_decode_attention_chosen")
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def _shared_bytes(prompts: int, batch: int, layers: int, kv_heads: int, q_heads: int, head_dim: int, dtype: int) -> int:
+    return int(_lib.flashcache_decode_shared_workspace_bytes(prompts, batch, layers, kv_heads, q_heads, head_dim, dtype))
+
+
+def shared_workspace(Q: torch.Tensor, kv_heads: int, prompts: int) -> torch.Tensor:
+    """A workspace for `decode_attention_shared` of this shape."""
+    B, L, Hq, d = Q.shape
+    return torch.empty(max(_shared_bytes(prompts, B, L, kv_heads, Hq, d, _dtype(Q)), 16), dtype=torch.uint8, device=Q.device)
+
+
+def decode_attention_shared(Q: torch.Tensor, common: PagedKV, starts: torch.Tensor, own: PagedKV, scale: float,
+                            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of one new token a sequence, Q [B, L, Hq, d], over the rows of a prompt that sequences share and then their own: sequence b
+    reads prompt p of `common` (its batch is the prompts) where starts[p] <= b < starts[p + 1], starts int32 [P + 1] not falling, and sequence
+    b of `own`.  A prompt's rows are read for all of its sequences together.  Returns float32 [B, L, Hq, d].  No gradients."""
+    index = _queries(Q, own)
+    B, L, H, d = own.shape
+    P = common.shape[0]
+    if common.shape[1:] != (L, H, d) or common.dtype is not own.dtype or common.index != index:
+        raise ValueError("both caches must agree in layers, heads, head dimension, dtype and GPU")
+    _want(starts, "starts", torch.int32, (P + 1,), index)
+    workspace = _scratch(workspace, _shared_bytes(P, B, L, H, Q.shape[2], d, own._desc.dtype), Q, index)
+    if out is None:
+        out = torch.empty(Q.shape, dtype=torch.float32, device=Q.device)
+    else:
+        _want(out, "out", torch.float32, Q.shape, index)
+    _check(_lib.flashcache_decode_attention_shared(
+        Q.data_ptr(), Q.shape[2], common._ref, starts.data_ptr(), own._ref, scale, out.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream()), "flashcache_decode_attention_shared")
     return out
 
 

@@ -25,6 +25,9 @@ UNITS = [
     ("mx_cache.hip", "mx_cache.o", []),
     ("pages.hip", "pages.o", []),
     ("rotary.hip", "rotary.o", []),
+    ("append.hip", "append.o", []),
+    ("choose.hip", "choose.o", []),
+    ("attend.hip", "attend.o", []),
     ("select_gather.hip", "select_gather.o", []),
     ("allocate.hip", "allocate.o", []),
     ("api.hip", "api.o", []),

@@ -537,6 +537,140 @@ fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const
   return e == hipSuccess ? FC_OK : FC_EHIP;
 }
 
+// A paged cache's shape; what is of a sequence has to fit between one and the next unless it is the same for all.
+static fc_status check_paged(const fc_paged_kv* kv) {
+  if (!kv || kv->batch < 0 || kv->layers < 1 || kv->kv_heads < 1 || kv->head_dim < 1 || kv->page_size < 1 || kv->max_pages < 1 || kv->num_pages < 1) return FC_EINVAL;
+  if (kv->dtype != FC_F32 && kv->dtype != FC_BF16) return FC_EINVAL;
+  if (kv->batch > 1 && (kv->rows_stride_b < 0 || kv->table_stride_b < 0)) return FC_EINVAL;
+  if (((int64_t)kv->head_dim * (kv->dtype == FC_BF16 ? 2 : 4)) % 16) return FC_EINVAL;
+  if (kv->head_dim > 512) return FC_EUNSUPPORTED;
+  if ((int64_t)kv->batch * kv->layers * kv->kv_heads > kMaxUnits) return FC_EUNSUPPORTED;
+  if (kv->page_size > (1 << 25) || kv->num_pages > 0x7FFFFFFFll || kv->num_pages * kv->page_size >= 0xFFFFFFFFll) return FC_EUNSUPPORTED;
+  return FC_OK;
+}
+
+static fc_status check_paged_pointers(const fc_paged_kv* kv, bool rows_alone) {
+  if (!kv->rows || !kv->block_table || (reinterpret_cast<uintptr_t>(kv->rows) & 3u) || (reinterpret_cast<uintptr_t>(kv->block_table) & 3u)) return FC_EINVAL;
+  if (!rows_alone && (!kv->K || !kv->V || !aligned16(kv->K) || !aligned16(kv->V))) return FC_EINVAL;
+  return FC_OK;
+}
+
+fc_status flashcache_append_paged(const fc_rotary_plan* plan, const int32_t* positions, const void* Q, void* Q_out, const fc_heads_desc* q_desc,
+                                  const void* K, const fc_heads_desc* k_desc, const void* V, const fc_heads_desc* v_desc, const int64_t* slots,
+                                  int64_t slots_stride_b, int64_t slots_stride_h, int32_t page_size, int64_t num_pages, void* K_pages,
+                                  void* V_pages, void* bounds, void* hip_stream) {
+  if (!plan || !q_desc || !k_desc || !v_desc || plan->magic != kWsMagic) return FC_EINVAL;
+  if (plan->rotary_dim < 2 || plan->rotary_dim % 2 || plan->rotary_dim > 2 * FC_ROTARY_MAX_PAIRS || plan->streams < 1 || plan->streams > 4) return FC_EINVAL;
+  fc_status st = check_heads(*plan, *q_desc, Q, Q_out);
+  if (st != FC_OK) return st;
+  // (rows of K and V go to slots: of their descriptors the input's part counts)
+  for (int i = 0; i < 2; ++i) {
+    fc_heads_desc d = i ? *v_desc : *k_desc;
+    const void* const in = i ? V : K;
+    void* const to = i ? V_pages : K_pages;
+    d.out_stride_b = d.out_stride_t = d.out_stride_h = d.head_dim;
+    st = check_heads(*plan, d, in, to);
+    if (st != FC_OK) return st;
+    if (d.batch != q_desc->batch || d.tokens != q_desc->tokens || d.head_dim != q_desc->head_dim || d.dtype != q_desc->dtype || in == to) return FC_EINVAL;
+  }
+  if (k_desc->heads != v_desc->heads) return FC_EINVAL;
+  if (page_size < 1 || num_pages < 1) return FC_EINVAL;
+  if (page_size > (1 << 25) || num_pages > 0x7FFFFFFFll || num_pages * page_size >= 0xFFFFFFFFll) return FC_EUNSUPPORTED;
+  if ((int64_t)q_desc->heads + 2 * (int64_t)k_desc->heads > 65535) return FC_EUNSUPPORTED;
+  if ((int64_t)q_desc->batch * q_desc->tokens == 0 || q_desc->heads + k_desc->heads == 0) return FC_OK;
+  if (!positions || (reinterpret_cast<uintptr_t>(positions) & 3u)) return FC_EINVAL;
+  if (reinterpret_cast<uintptr_t>(bounds) % (q_desc->dtype == FC_BF16 ? 2 : 4)) return FC_EINVAL;
+  if (k_desc->heads > 0 && (!slots || (reinterpret_cast<uintptr_t>(slots) & 7u) || K_pages == V_pages || slots_stride_b < 0 || slots_stride_h < 0)) return FC_EINVAL;
+  hipError_t e = append_launch(*plan, positions, Q, Q_out, *q_desc, K, *k_desc, V, *v_desc, slots, slots_stride_b, slots_stride_h, page_size, num_pages, K_pages,
+                               V_pages, bounds, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : e == hipErrorInvalidConfiguration ? FC_EUNSUPPORTED : FC_EHIP;
+}
+
+fc_status flashcache_page_bounds(const fc_paged_kv* kv, void* bounds, void* hip_stream) {
+  fc_status st = check_paged(kv);
+  if (st != FC_OK) return st;
+  if (kv->head_dim * (kv->dtype == FC_BF16 ? 2 : 4) > 1024) return FC_EUNSUPPORTED;
+  if (kv->batch == 0) return FC_OK;
+  st = check_paged_pointers(kv, true);
+  if (st != FC_OK) return st;
+  if (!kv->K || !aligned16(kv->K) || !bounds || !aligned16(bounds)) return FC_EINVAL;
+  hipError_t e = page_bounds_launch(*kv, bounds, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+// What the attention kernels and the choice of pages take.
+static fc_status check_attended(const fc_paged_kv* kv, int32_t q_heads) {
+  fc_status st = check_paged(kv);
+  if (st != FC_OK) return st;
+  if (q_heads < kv->kv_heads || q_heads % kv->kv_heads) return FC_EINVAL;
+  return attend_supported(q_heads / kv->kv_heads, kv->head_dim) ? FC_OK : FC_EUNSUPPORTED;
+}
+
+size_t flashcache_choose_pages_workspace_bytes(const fc_paged_kv* kv) {
+  return check_paged(kv) == FC_OK ? choose_workspace_bytes((int64_t)kv->batch * kv->layers * kv->kv_heads, kv->max_pages) : 0;
+}
+
+fc_status flashcache_choose_pages(const void* Q, int32_t q_heads, const fc_paged_kv* kv, const void* bounds, int32_t count, int32_t first,
+                                  int32_t last, int32_t* chosen, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  fc_status st = check_attended(kv, q_heads);
+  if (st != FC_OK) return st;
+  if (count < 1 || first < 0 || last < 0 || (int64_t)first + last > count) return FC_EINVAL;
+  if (kv->batch == 0) return FC_OK;
+  st = check_paged_pointers(kv, true);
+  if (st != FC_OK) return st;
+  if (!Q || !bounds || !chosen || !aligned16(Q) || !aligned16(bounds) || (reinterpret_cast<uintptr_t>(chosen) & 3u)) return FC_EINVAL;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < flashcache_choose_pages_workspace_bytes(kv)) return FC_EWORKSPACE;
+  hipError_t e = choose_launch(Q, q_heads / kv->kv_heads, *kv, bounds, count, first, last, chosen, workspace, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+size_t flashcache_decode_chosen_workspace_bytes(const fc_paged_kv* kv, int32_t q_heads, int32_t count) {
+  if (check_attended(kv, q_heads) != FC_OK || kv->batch == 0 || count < 1 || (int64_t)count * kv->page_size >= (1 << 30)) return 0;
+  return attend_chosen_workspace_bytes(kv->batch * kv->layers * kv->kv_heads, q_heads / kv->kv_heads, kv->head_dim, kv->dtype, kv->page_size, count);
+}
+
+fc_status flashcache_decode_attention_chosen(const void* Q, int32_t q_heads, const fc_paged_kv* kv, const int32_t* chosen, int32_t count, float scale,
+                                             float* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  fc_status st = check_attended(kv, q_heads);
+  if (st != FC_OK) return st;
+  if (count < 1 || !(scale == scale)) return FC_EINVAL;
+  if ((int64_t)count * kv->page_size >= (1 << 30)) return FC_EUNSUPPORTED;
+  if (kv->batch == 0) return FC_OK;
+  st = check_paged_pointers(kv, false);
+  if (st != FC_OK) return st;
+  if (!Q || !out || !chosen || !aligned16(Q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(chosen) & 3u)) return FC_EINVAL;
+  const size_t need = flashcache_decode_chosen_workspace_bytes(kv, q_heads, count);
+  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return FC_EWORKSPACE;
+  hipError_t e = attend_chosen_launch(Q, q_heads / kv->kv_heads, *kv, chosen, count, scale, out, workspace, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
+size_t flashcache_decode_shared_workspace_bytes(int32_t prompts, int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads, int32_t head_dim,
+                                                int32_t dtype) {
+  if (prompts < 0 || batch < 1 || layers < 1 || kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads || (dtype != FC_F32 && dtype != FC_BF16)) return 0;
+  if (!attend_supported(q_heads / kv_heads, head_dim) || (int64_t)batch * layers * kv_heads > kMaxUnits || (int64_t)prompts * layers * kv_heads > kMaxUnits)
+    return 0;
+  return attend_shared_workspace_bytes(prompts, batch, layers, kv_heads, q_heads / kv_heads, head_dim, dtype);
+}
+
+fc_status flashcache_decode_attention_shared(const void* Q, int32_t q_heads, const fc_paged_kv* common, const int32_t* starts, const fc_paged_kv* own,
+                                             float scale, float* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  fc_status st = check_attended(own, q_heads);
+  if (st == FC_OK) st = check_attended(common, q_heads);
+  if (st != FC_OK) return st;
+  if (common->layers != own->layers || common->kv_heads != own->kv_heads || common->head_dim != own->head_dim || common->dtype != own->dtype) return FC_EINVAL;
+  if (!(scale == scale)) return FC_EINVAL;
+  if (own->batch == 0) return FC_OK;
+  st = check_paged_pointers(own, false);
+  if (st == FC_OK && common->batch > 0) st = check_paged_pointers(common, false);
+  if (st != FC_OK) return st;
+  if (!Q || !out || !starts || !aligned16(Q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(starts) & 3u)) return FC_EINVAL;
+  const size_t need = flashcache_decode_shared_workspace_bytes(common->batch, own->batch, own->layers, own->kv_heads, q_heads, own->head_dim, own->dtype);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < need) return FC_EWORKSPACE;
+  hipError_t e = attend_shared_launch(Q, q_heads / own->kv_heads, *common, starts, *own, scale, out, workspace, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? FC_OK : FC_EHIP;
+}
+
 const char* flashcache_status_string(int32_t status) {
   switch (status) {
     case FC_OK: return "FC_OK";

@@ -1,0 +1,377 @@
+// New tokens' rows into a paged cache: queries and keys turned by their positions (the rotation of rotary.hip), keys and values into the slots of
+// their pages, and, where a program ranks pages by their keys' bounds, each touched page's lowest and largest key of every column.
+//
+// Bound by memory: every element is read and written once, in one launch.  Without bounds, queries, keys and values of a token are heads in a row of
+// which the last are copied, as in rotary.hip.  With bounds a wave has a stretch of one KV head's tokens: it stores their keys and keeps the
+// least and largest of what it stores (rounded values: rounding keeps the order) until the page changes, so that no page has two writers and no
+// row is read back.
+#include <algorithm>
+#include <type_traits>
+#include <math.h>
+
+#include "fc_common.h"
+#include "rotary.h"
+
+namespace fc {
+
+namespace {
+
+constexpr int kAppThreads = 256, kAppWaves = kAppThreads / 64;
+constexpr int kHeadsAtOnce = 4, kMostPairs = 4, kMostAbreast = 8, kMostTurns = 8;
+constexpr int kTokensAtOnce = 4;       // of a lane, with bounds
+
+struct NewRows {                 // strides in bytes
+  const char* in;
+  int64_t sb, st, sh;
+  int heads;
+};
+struct AppendArgs {
+  NewRows q, k, v;
+  char* q_out;
+  int64_t ob, ot, oh;
+  char* k_pages;
+  char* v_pages;
+  char* bounds;
+  const int64_t* slots;
+  int64_t slots_b, slots_h;      // strides of the slot map
+  int64_t num_slots;
+  const int32_t* positions;      // [streams][batch * tokens]
+  int tokens, rows;              // tokens of a sequence, of all sequences
+  int half, chunks, turned;      // pairs; chunks of a head; those that are turned
+  int row_bytes;                 // of a head
+  int page_size;
+  // rows of tokens
+  int per_group;                 // tokens of a workgroup
+  uint32_t chunks_inverse, abreast_inverse;
+  int abreast, turns, across;    // heads of a token side by side; how many of them a thread has; workgroups side by side
+  int turning;                   // heads of the first part that are turned; the keys among them unless there are bounds
+  // keys with bounds
+  int stretches, stretch;        // of a head; tokens of one
+  int bound_groups;              // workgroups, the launch's first
+  int streams, end0, end1, end2; // first pair behind the first, second and third stream
+  float magnitude;
+};
+
+template <int P> __device__ __forceinline__ void sines_of(const AppendArgs& a, const fc_rotary_plan& plan, int row, int first, float (&sn)[P], float (&cs)[P]) {
+  int32_t where[P];
+  where[0] = a.positions[row];
+#pragma unroll
+  for (int i = 1; i < P; ++i) where[i] = where[0];
+  if (a.streams > 1) {
+    int32_t other[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) other[k] = k + 1 < a.streams ? a.positions[(int64_t)(k + 1) * a.rows + row] : 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int pair = first + i;
+      where[i] = pair < a.end0 ? where[i] : pair < a.end1 ? other[0] : pair < a.end2 ? other[1] : other[2];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    sine_cosine(turned_by(where[i], plan.turns[first + i]), sn[i], cs[i]);
+    sn[i] *= a.magnitude;
+    cs[i] *= a.magnitude;
+  }
+}
+
+// A chunk's pieces, turned.
+template <typename T, int P, bool INTERLEAVED, int PIECES, int PIECE>
+__device__ __forceinline__ void turn(Vec<T, PIECE> (&v)[PIECES], const float (&sn)[P], const float (&cs)[P]) {
+  float x[PIECES][PIECE], y[PIECES][PIECE];
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j) widen<T, PIECE>(v[j], x[j]);
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    constexpr int j = INTERLEAVED ? 0 : 1;
+    const int c0 = INTERLEAVED ? 2 * k : k, c1 = INTERLEAVED ? 2 * k + 1 : k;
+    y[0][c0] = fmaf(x[0][c0], cs[k], -(x[j][c1] * sn[k]));  // (fused by hand: the same roundings in all forms of the kernel)
+    y[j][c1] = fmaf(x[0][c0], sn[k], x[j][c1] * cs[k]);
+  }
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j) v[j] = narrow<T, PIECE>(y[j]);
+}
+
+// Bytes of a chunk's first piece from the head's begin on, and from it to the second.
+template <typename T, int P, int PIECE> __device__ __forceinline__ void place_of_chunk(const AppendArgs& a, int chunk, int& at, int& apart) {
+  const bool turned = chunk < a.turned;
+  at = (turned ? chunk * PIECE : 2 * a.half + (chunk - a.turned) * PIECE) * (int)sizeof(T);
+  apart = (turned ? a.half : (a.chunks - a.turned) * P) * (int)sizeof(T);
+}
+
+// Tokens' heads side by side.
+template <typename T, int P, bool INTERLEAVED, bool PAST>
+__device__ __forceinline__ void append_rows(const AppendArgs& a, const fc_rotary_plan& plan, int group) {
+  constexpr int kPieces = INTERLEAVED ? 1 : 2, kPiece = 2 * P / kPieces;     // pieces of a chunk, columns of a piece
+  const int along = group / a.across, part = group - along * a.across;
+  const int place = quotient(threadIdx.x, a.chunks_inverse), chunk = (int)threadIdx.x - place * a.chunks;
+  const int own = quotient(place, a.abreast_inverse), beside = place - own * a.abreast;
+  const int64_t row64 = (int64_t)along * a.per_group + own;
+  if (own >= a.per_group || row64 >= a.rows) return;
+  const int row = (int)row64, b = a.tokens == 1 ? row : row / a.tokens, t = row - b * a.tokens;
+  const int heads = a.turning + a.v.heads;
+  const int h0 = part * a.abreast * a.turns, h1 = min(heads, h0 + a.abreast * a.turns);
+  int at, apart;
+  place_of_chunk<T, P, kPiece>(a, chunk, at, apart);
+  const bool turned = chunk < a.turned && h0 + beside < a.turning;
+  float sn[P], cs[P];
+  if (turned) sines_of<P>(a, plan, row, chunk * P, sn, cs);
+  for (int hw = h0; hw < h1; hw += kHeadsAtOnce * a.abreast) {
+    Vec<T, kPiece> v[kHeadsAtOnce][kPieces];
+    char* out[kHeadsAtOnce];
+#pragma unroll
+    for (int i = 0; i < kHeadsAtOnce; ++i) {
+      const int h = hw + i * a.abreast + beside;
+      if (h >= h1) break;
+      const char* in;
+      if (h < a.q.heads) {
+        in = a.q.in + b * a.q.sb + t * a.q.st + h * a.q.sh;
+        out[i] = a.q_out + b * a.ob + t * a.ot + h * a.oh;
+      } else {
+        const bool key = h < a.turning;
+        const int kv = h - (key ? a.q.heads : a.turning);
+        const int64_t slot = a.slots[b * a.slots_b + kv * a.slots_h + t];
+        in = key ? a.k.in + b * a.k.sb + t * a.k.st + kv * a.k.sh : a.v.in + b * a.v.sb + t * a.v.st + kv * a.v.sh;
+        out[i] = slot >= 0 && slot < a.num_slots ? (key ? a.k_pages : a.v_pages) + slot * a.row_bytes : nullptr;
+      }
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) v[i][j] = get<PAST, T, kPiece>(in + at + j * apart);
+    }
+#pragma unroll
+    for (int i = 0; i < kHeadsAtOnce; ++i) {
+      const int h = hw + i * a.abreast + beside;
+      if (h >= h1) break;
+      if (turned && h < a.turning) turn<T, P, INTERLEAVED>(v[i], sn, cs);
+      if (!out[i]) continue;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) put<PAST>(out[i] + at + j * apart, v[i][j]);
+    }
+  }
+}
+
+// A stretch of a KV head's tokens: the runs of tokens with a page in common that begin in it, up to their ends.
+template <typename T, int P, bool INTERLEAVED>
+__device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary_plan& plan, int group) {
+  constexpr int kPieces = INTERLEAVED ? 1 : 2, kPiece = 2 * P / kPieces;
+  const int lane = threadIdx.x & 63, item = __builtin_amdgcn_readfirstlane(group * kAppWaves + (int)(threadIdx.x >> 6));
+  const int head = item / a.stretches, b = head / a.k.heads, h = head - b * a.k.heads;
+  if (b * a.tokens >= a.rows) return;
+  const int t0 = (item - head * a.stretches) * a.stretch, t1 = min(a.tokens, t0 + a.stretch);
+  const int64_t* const slots = a.slots + b * a.slots_b + h * a.slots_h;
+  const char* const in = a.k.in + b * a.k.sb + h * a.k.sh;
+  const int lanes = min(64, a.chunks), rows_abreast = 64 / lanes, mine = lane / lanes;
+  // the page of a token, -1 without one
+  auto page_of = [&](int64_t slot) -> int64_t { return slot >= 0 && slot < a.num_slots ? (int64_t)((uint32_t)slot / (uint32_t)a.page_size) : -1; };
+  for (int first = 0; first < a.chunks; first += lanes) {  // (one turn: a head's chunks but those of narrow pieces fit a wave)
+    const int chunk = first + lane - mine * lanes;
+    const bool has = mine < rows_abreast && chunk < a.chunks;
+    int at, apart;
+    place_of_chunk<T, P, kPiece>(a, has ? chunk : 0, at, apart);
+    float low[kPieces][kPiece], high[kPieces][kPiece];
+    int64_t run = t0 > 0 ? page_of(slots[t0 - 1]) : -1;    // page that the tokens before have
+    bool open = false, begun = false;                      // whether the run is this wave's; whether it has the page's first row
+    auto flush = [&]() {
+      if (!open) return;
+      // rows side by side, one after another: the order does not matter to least and largest
+      for (int r = 1; r < rows_abreast; ++r) {
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+          for (int c = 0; c < kPiece; ++c) {
+            const float l = __shfl(low[j][c], (lane + r * lanes) & 63, 64), g = __shfl(high[j][c], (lane + r * lanes) & 63, 64);
+            if (mine == 0) {
+              low[j][c] = fminf(low[j][c], l);
+              high[j][c] = fmaxf(high[j][c], g);
+            }
+          }
+      }
+      if (has && mine == 0) {
+        char* const to = a.bounds + 2 * run * a.row_bytes + at;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+          if (!begun) {
+            float l[kPiece], g[kPiece];
+            widen<T, kPiece>(get<false, T, kPiece>(to + j * apart), l);
+            widen<T, kPiece>(get<false, T, kPiece>(to + a.row_bytes + j * apart), g);
+#pragma unroll
+            for (int c = 0; c < kPiece; ++c) {
+              low[j][c] = fminf(low[j][c], l[c]);
+              high[j][c] = fmaxf(high[j][c], g[c]);
+            }
+          }
+          put<false>(to + j * apart, narrow<T, kPiece>(low[j]));
+          put<false>(to + a.row_bytes + j * apart, narrow<T, kPiece>(high[j]));
+        }
+      }
+      open = false;
+    };
+    int cur = t0;
+    while (cur < a.tokens) {
+      // the next tokens' slots, a lane each, and how many of them are of the same page
+      const int64_t slot = slots[min(cur + lane, a.tokens - 1)];
+      const int page_mine = (int)page_of(slot);
+      const int page = __builtin_amdgcn_readfirstlane(page_mine);
+      const uint64_t other = __ballot(page_mine != page || cur + lane >= a.tokens);
+      const int n = other ? __builtin_ctzll(other) : 64;
+      if (page != run || page < 0) {                       // a new run
+        flush();
+        if (cur >= t1) break;
+        run = page;
+        open = page >= 0;
+        begun = false;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+          for (int c = 0; c < kPiece; ++c) { low[j][c] = INFINITY; high[j][c] = -INFINITY; }
+      } else if (!open && cur >= t1) {
+        break;
+      }
+      if (open) {
+        const int offset = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)a.page_size);
+        begun = begun || __ballot(lane < n && offset == 0) != 0;
+        for (int i = 0; i < n; i += kTokensAtOnce * rows_abreast) {
+          Vec<T, kPiece> v[kTokensAtOnce][kPieces];
+#pragma unroll
+          for (int u = 0; u < kTokensAtOnce; ++u) {
+            const int t = i + u * rows_abreast + mine;
+            if (has && t < n)
+#pragma unroll
+              for (int j = 0; j < kPieces; ++j) v[u][j] = get<false, T, kPiece>(in + (int64_t)(cur + t) * a.k.st + at + j * apart);
+          }
+#pragma unroll
+          for (int u = 0; u < kTokensAtOnce; ++u) {
+            const int t = i + u * rows_abreast + mine;
+            const int off = __shfl(offset, min(t, 63), 64);
+            if (has && t < n) {
+              if (chunk < a.turned) {
+                float sn[P], cs[P];
+                sines_of<P>(a, plan, b * a.tokens + cur + t, chunk * P, sn, cs);
+                turn<T, P, INTERLEAVED>(v[u], sn, cs);
+              }
+              char* const to = a.k_pages + ((int64_t)page * a.page_size + off) * a.row_bytes + at;
+#pragma unroll
+              for (int j = 0; j < kPieces; ++j) {
+                put<false>(to + j * apart, v[u][j]);
+                float x[kPiece];
+                widen<T, kPiece>(v[u][j], x);
+#pragma unroll
+                for (int c = 0; c < kPiece; ++c) {
+                  low[j][c] = fminf(low[j][c], x[c]);
+                  high[j][c] = fmaxf(high[j][c], x[c]);
+                }
+              }
+            }
+          }
+        }
+      }
+      cur += n;
+    }
+    flush();
+  }
+}
+
+template <typename T, int P, bool INTERLEAVED, bool PAST>
+__global__ __launch_bounds__(kAppThreads) void append_kernel(AppendArgs a, const fc_rotary_plan plan) {
+  if ((int)blockIdx.x < a.bound_groups) append_keys<T, P, INTERLEAVED>(a, plan, blockIdx.x);
+  else append_rows<T, P, INTERLEAVED, PAST>(a, plan, (int)blockIdx.x - a.bound_groups);
+}
+
+}  // namespace
+
+hipError_t append_launch(const fc_rotary_plan& plan, const int32_t* positions, const void* Q, void* Q_out, const fc_heads_desc& q, const void* K,
+                         const fc_heads_desc& k, const void* V, const fc_heads_desc& v, const int64_t* slots, int64_t slots_b, int64_t slots_h,
+                         int page_size, int64_t num_pages, void* K_pages, void* V_pages, void* bounds, hipStream_t s) {
+  const int e = q.dtype == FC_BF16 ? 2 : 4, half = plan.rotary_dim / 2, rest = q.head_dim - plan.rotary_dim;
+  // (the step of an axis of one says nothing: left out, as it would count in what addresses are multiples of)
+  auto step = [&](int n, int64_t stride) { return n > 1 ? stride * e : 0; };
+  auto side = [&](const void* in, const fc_heads_desc& d) {
+    return NewRows{static_cast<const char*>(in), step(d.batch, d.stride_b), step(d.tokens, d.stride_t), step(d.heads, d.stride_h), d.heads};
+  };
+  AppendArgs a{};
+  a.q = side(Q, q);
+  a.k = side(K, k);
+  a.v = side(V, v);
+  a.q_out = static_cast<char*>(Q_out);
+  a.ob = step(q.batch, q.out_stride_b);
+  a.ot = step(q.tokens, q.out_stride_t);
+  a.oh = step(q.heads, q.out_stride_h);
+  a.k_pages = static_cast<char*>(K_pages);
+  a.v_pages = static_cast<char*>(V_pages);
+  a.bounds = static_cast<char*>(bounds);
+  a.slots = slots;
+  a.slots_b = slots_b;
+  a.slots_h = slots_h;
+  a.num_slots = num_pages * page_size;
+  a.page_size = page_size;
+  a.row_bytes = q.head_dim * e;
+  // the widest parts that every address is a multiple of
+  uint64_t bits = (uint64_t)(uintptr_t)K_pages | (uint64_t)(uintptr_t)V_pages | (uint64_t)(uintptr_t)bounds | (uint64_t)a.row_bytes;
+  if (q.heads) bits |= (uint64_t)(uintptr_t)a.q_out | (uint64_t)(a.ob | a.ot | a.oh);
+  for (const NewRows* r : {&a.q, &a.k, &a.v})
+    if (r->heads) bits |= (uint64_t)(uintptr_t)r->in | (uint64_t)(r->sb | r->st | r->sh);
+  const int pieces = plan.interleaved ? 1 : 2;             // (of a chunk: 16 bytes at most)
+  int pairs = std::min(8 * pieces / e, kMostPairs);
+  while (pairs > 1 && (half % pairs || rest % (2 * pairs) || (bits & (uint64_t)(2 * pairs / pieces * e - 1)))) pairs /= 2;
+  a.positions = positions;
+  a.tokens = q.tokens;
+  a.rows = q.batch * q.tokens;
+  a.half = half;
+  a.turned = half / pairs;
+  a.chunks = a.turned + rest / (2 * pairs);
+  a.streams = plan.streams;
+  a.end0 = plan.stream_end[0];
+  a.end1 = plan.stream_end[1];
+  a.end2 = plan.stream_end[2];
+  a.magnitude = plan.magnitude;
+  a.turning = q.heads + (bounds ? 0 : k.heads);
+  const int heads = a.turning + v.heads, places = kAppThreads / a.chunks;
+  int64_t row_groups = 0;
+  if (heads) {
+    const int64_t one_turn = ((int64_t)a.rows * heads + places - 1) / places;  // workgroups if every thread has a single head
+    // few tokens: all heads side by side; else at least four turns, for which the sines are made once (see rotary.hip)
+    int abreast = 1;
+    while (abreast < kMostAbreast && 2 * abreast * kHeadsAtOnce <= heads) abreast *= 2;
+    a.abreast = std::min(std::min(heads, places), one_turn > 2048 ? abreast : heads);
+    a.turns = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMostTurns, (heads + a.abreast - 1) / a.abreast), one_turn / 2048));
+    a.per_group = places / a.abreast;
+    a.chunks_inverse = inverse_of(a.chunks);
+    a.abreast_inverse = inverse_of(a.abreast);
+    a.across = (heads + a.abreast * a.turns - 1) / (a.abreast * a.turns);
+    row_groups = (((int64_t)a.rows + a.per_group - 1) / a.per_group) * a.across;
+  } else {
+    a.across = 1;
+  }
+  if (bounds && k.heads) {
+    a.stretch = a.tokens == 1 ? 1 : std::min(64, std::max(16, page_size));
+    a.stretches = (a.tokens + a.stretch - 1) / a.stretch;
+    const int64_t waves = (int64_t)k.batch * k.heads * a.stretches;
+    if (waves >= 1 << 26) return hipErrorInvalidConfiguration;
+    a.bound_groups = (int)((waves + kAppWaves - 1) / kAppWaves);
+  }
+  const int64_t groups = a.bound_groups + row_groups;
+  if (groups == 0) return hipSuccess;
+  if (groups >= 1 << 24) return hipErrorInvalidConfiguration;                // (2^32 threads)
+  ProfileScope ps("append_kernel", s);
+  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAppThreads), 0, s, a, plan); };
+  // what is read and written exceeds the cache, in pieces of whole lines (see rotary.hip)
+  const bool past = 2LL * a.rows * (q.heads + k.heads + v.heads) * a.row_bytes > 256000000 && (plan.interleaved || half * e % 128 == 0);
+  auto with = [&](auto type, auto n, auto interleaved) {
+    typedef decltype(type) T;
+    past ? launch(append_kernel<T, decltype(n)::value, decltype(interleaved)::value, true>)
+         : launch(append_kernel<T, decltype(n)::value, decltype(interleaved)::value, false>);
+  };
+  typedef std::integral_constant<int, 4> Four;
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 1> One;
+  auto sized = [&](auto type, auto interleaved) {          // (interleaved fp32: two pairs are 16 bytes)
+    constexpr bool kFour = !decltype(interleaved)::value || sizeof(type) == 2;
+    if (pairs == 1) with(type, One{}, interleaved);
+    else if (!kFour || pairs == 2) with(type, Two{}, interleaved);
+    else with(type, std::conditional_t<kFour, Four, Two>{}, interleaved);
+  };
+  auto of = [&](auto type) { plan.interleaved ? sized(type, std::true_type{}) : sized(type, std::false_type{}); };
+  q.dtype == FC_BF16 ? of(uint16_t{}) : of(float{});
+  return hipGetLastError();
+}
+
+}  // namespace fc

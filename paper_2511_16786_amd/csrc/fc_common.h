@@ -129,6 +129,22 @@ hipError_t mx_decode_launch(const void* Q, const void* pages, const int32_t* tab
                             int B, int L, int H, int group, int d, int dtype, const int32_t* rows, float scale, float* out, void* ws,
                             hipStream_t s);
 
+// (hipErrorInvalidConfiguration, and nothing is enqueued: too many workgroups)
+hipError_t append_launch(const fc_rotary_plan& plan, const int32_t* positions, const void* Q, void* Q_out, const fc_heads_desc& q, const void* K,
+                         const fc_heads_desc& k, const void* V, const fc_heads_desc& v, const int64_t* slots, int64_t slots_b, int64_t slots_h,
+                         int page_size, int64_t num_pages, void* K_pages, void* V_pages, void* bounds, hipStream_t s);
+hipError_t page_bounds_launch(const fc_paged_kv& kv, void* bounds, hipStream_t s);
+size_t choose_workspace_bytes(int64_t units, int max_pages);
+hipError_t choose_launch(const void* Q, int group, const fc_paged_kv& kv, const void* bounds, int count, int first, int last, int32_t* chosen, void* ws,
+                         hipStream_t s);
+bool attend_supported(int group, int d);
+size_t attend_chosen_workspace_bytes(int units, int group, int d, int dtype, int page_size, int count);
+hipError_t attend_chosen_launch(const void* Q, int group, const fc_paged_kv& kv, const int32_t* chosen, int count, float scale, float* out, void* ws,
+                                hipStream_t s);
+size_t attend_shared_workspace_bytes(int P, int B, int L, int H, int group, int d, int dtype);
+hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& common, const int32_t* starts, const fc_paged_kv& own, float scale, float* out,
+                                void* ws, hipStream_t s);
+
 // Per-kernel event timing (see profile.hip): brackets the launches made while it is alive.
 bool profiling_on();
 class ProfileScope {

@@ -1,0 +1,37 @@
+// A paged cache as the kernels take it.
+#ifndef FC_PAGED_H_
+#define FC_PAGED_H_
+
+#include "fc_common.h"
+
+namespace fc {
+
+namespace {
+
+constexpr int kMostPagedRows = (1 << 25) - 1;
+
+struct PagedArgs {
+  const void* K;
+  const void* V;
+  const int32_t* rows;           // [B][L], rows_b between sequences
+  const int32_t* table;          // [B][L][H][max_pages], table_b between sequences
+  int64_t rows_b, table_b, num_pages;
+  int B, L, H, page_size, max_pages;
+};
+
+inline PagedArgs paged_args(const fc_paged_kv& kv) {
+  return PagedArgs{kv.K, kv.V, kv.rows, kv.block_table, kv.rows_stride_b, kv.table_stride_b, kv.num_pages,
+                   kv.batch, kv.layers, kv.kv_heads, kv.page_size, kv.max_pages};
+}
+
+// Rows of a layer that its table can reach.
+__device__ __forceinline__ int rows_within(const PagedArgs& a, int rows) {
+  return (int)min((int64_t)min(max(rows, 0), kMostPagedRows), (int64_t)a.max_pages * a.page_size);
+}
+__device__ __forceinline__ int rows_of(const PagedArgs& a, int b, int l) { return rows_within(a, a.rows[b * a.rows_b + l]); }
+__device__ __forceinline__ int pages_of(const PagedArgs& a, int b, int l) { return (rows_of(a, b, l) + a.page_size - 1) / a.page_size; }
+
+}  // namespace
+
+}  // namespace fc
+#endif
