@@ -5,11 +5,16 @@
 //            all of these sequences together: their m * G queries are the rows of one product.
 //   chosen   the rows of the pages that a list names for each unit (sequence, layer, KV head).
 //
-// Both products are on the matrix cores.  bf16 rows: 16x16x32, products exact in fp32; probabilities are two bf16 terms, each rounded to nearest
-// (17 bits, off by 7e-7 in the mean; one term would be off by 1e-3).  fp32 rows: 16x16x4 in fp32.  Sums and softmax are in fp32.
+// Both products are on the matrix cores.  bf16 rows: 16x16x32, products exact in fp32, probabilities as three bf16 terms that are exact together (24 bits;
+// two are off by up to 2^-17).  fp32 rows: 16x16x4 in fp32.  Sums and softmax are in fp32.
 // With c16 = lane % 16 and g4 = lane / 16, and 16 rows of K and V a tile:
 //   scores:  A = K rows (row c16), B = queries (query c16), the same columns of both for each g4; a lane has the scores of rows 4 g4 + i, query c16
 //   output:  A = probabilities (query c16, rows 4 g4 + i, as the scores come out), B = V (the same rows, a column for each c16 and output tile)
+//
+// Where 16 queries or fewer read the same rows, each of a workgroup's waves has rows of its own, straight into registers, and the waves' results are
+// merged.  Where more do, the workgroup has up to 128 queries, two tiles of 16 a wave, and reads the rows once for all of them, through LDS.
+#include <math.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -21,9 +26,11 @@ namespace fc {
 namespace {
 
 constexpr int kAttThreads = 256, kAttWaves = kAttThreads / 64;
-constexpr int kTileQueries = 16;       // of a workgroup
+constexpr int kTileQueries = 128;      // of a workgroup
 constexpr int kLeastSteps = 4;         // of a piece
-constexpr int kGroups = 1024;          // pieces that a launch over shared rows aims at
+constexpr int kGroups = 512;           // pieces that a launch over shared rows aims at: as many as are resident together
+constexpr int kStepsLooked = 64;       // steps whose rows' places are looked up together
+constexpr float kSlack = 16.f;         // how far scores (in log2) may exceed the running reference before it is moved
 
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
@@ -51,7 +58,9 @@ template <typename T, int D> struct Form;
 template <int D> struct Form<uint16_t, D> {
   static constexpr int kTiles = 2, kRows = 32, KW = D / 8, VT = D / 16, VW = VT / 2;
   struct Queries { uint32_t w[KW]; };
-  struct Rows { uint32_t k[2][KW], v[2][4][VW]; };
+  struct Keys { uint32_t w[2][KW]; };
+  struct Values { uint32_t w[2][4][VW]; };
+  struct Weights { uint32_t term[3][4]; };
   static __device__ __forceinline__ int column(int c16, int t) { return VT * c16 + t; }   // of output tile t
   static __device__ __forceinline__ void queries(const uint16_t* q, bool has, int g4, Queries& o) {
 #pragma unroll
@@ -63,56 +72,99 @@ template <int D> struct Form<uint16_t, D> {
         o.w[4 * i] = u.x; o.w[4 * i + 1] = u.y; o.w[4 * i + 2] = u.z; o.w[4 * i + 3] = u.w;
       }
   }
-  static __device__ __forceinline__ void load_k(const uint16_t* base, int64_t row, int g4, int tile, Rows& x) {
+  static __device__ __forceinline__ void load_k(const uint16_t* base, int64_t row, int g4, int tile, Keys& x) {
     const uint16_t* const p = base + row * D + 8 * g4;
 #pragma unroll
     for (int i = 0; i < KW / 4; ++i) {
       const u32x4 u = load_past<u32x4>(p + 32 * i);
-      x.k[tile][4 * i] = u.x; x.k[tile][4 * i + 1] = u.y; x.k[tile][4 * i + 2] = u.z; x.k[tile][4 * i + 3] = u.w;
+      x.w[tile][4 * i] = u.x; x.w[tile][4 * i + 1] = u.y; x.w[tile][4 * i + 2] = u.z; x.w[tile][4 * i + 3] = u.w;
     }
   }
-  static __device__ __forceinline__ void load_v(const uint16_t* base, int64_t row, int c16, int tile, int i, Rows& x) {
+  static __device__ __forceinline__ void load_v(const uint16_t* base, int64_t row, int c16, int tile, int i, Values& x) {
     const uint16_t* const p = base + row * D + VT * c16;
     if constexpr (VW == 4) {
       const u32x4 u = load_past<u32x4>(p);
-      x.v[tile][i][0] = u.x; x.v[tile][i][1] = u.y; x.v[tile][i][2] = u.z; x.v[tile][i][3] = u.w;
+      x.w[tile][i][0] = u.x; x.w[tile][i][1] = u.y; x.w[tile][i][2] = u.z; x.w[tile][i][3] = u.w;
     } else {
       const u32x2 u = load_past<u32x2>(p);
-      x.v[tile][i][0] = u.x; x.v[tile][i][1] = u.y;
+      x.w[tile][i][0] = u.x; x.w[tile][i][1] = u.y;
     }
   }
-  static __device__ __forceinline__ float4v scores(const Queries& q, const Rows& x, int tile) {
+  static __device__ __forceinline__ float4v scores(const Queries& q, const Keys& x, int tile) {
     float4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < KW / 4; ++s)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x.k[tile][4 * s], x.k[tile][4 * s + 1], x.k[tile][4 * s + 2], x.k[tile][4 * s + 3]),
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x.w[tile][4 * s], x.w[tile][4 * s + 1], x.w[tile][4 * s + 2], x.w[tile][4 * s + 3]),
                                                     as_bf16x8(q.w[4 * s], q.w[4 * s + 1], q.w[4 * s + 2], q.w[4 * s + 3]), acc, 0, 0, 0);
     return acc;
   }
-  static __device__ __forceinline__ void add(const float (&p)[kTiles][4], const Rows& x, float4v (&out)[VT]) {
-    uint32_t hi[4], lo[4];
+  static __device__ __forceinline__ void weights(const float (&p)[kTiles][4], Weights& w) {
+    // each term is what the one before left, cut off to bf16: the third is exact
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float a = p[j / 2][j % 2 * 2], b = p[j / 2][j % 2 * 2 + 1];
-      hi[j] = pack_bf16(a, b);
-      lo[j] = pack_bf16(a - __uint_as_float(hi[j] << 16), b - __uint_as_float(hi[j] & 0xFFFF0000u));
+      float a = p[j / 2][j % 2 * 2], b = p[j / 2][j % 2 * 2 + 1];
+#pragma unroll
+      for (int n = 0; n < 3; ++n) {
+        const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+        w.term[n][j] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+        a -= __uint_as_float(ua & 0xFFFF0000u);
+        b -= __uint_as_float(ub & 0xFFFF0000u);
+      }
     }
-    const bf16x8 phi = as_bf16x8(hi[0], hi[1], hi[2], hi[3]), plo = as_bf16x8(lo[0], lo[1], lo[2], lo[3]);
+  }
+  // of N tiles of queries that read the same rows
+  template <int N> static __device__ __forceinline__ void add(const Weights (&p)[N], const Values& x, float4v (&out)[N][VT]) {
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       const uint32_t sel = (t & 1) ? 0x07060302u : 0x05040100u;
       const int w = t >> 1;
-      auto two = [&](int tile, int i) { return __builtin_amdgcn_perm(x.v[tile][i + 1][w], x.v[tile][i][w], sel); };
+      auto two = [&](int tile, int i) { return __builtin_amdgcn_perm(x.w[tile][i + 1][w], x.w[tile][i][w], sel); };
       const bf16x8 v = as_bf16x8(two(0, 0), two(0, 2), two(1, 0), two(1, 2));
-      out[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(phi, v, out[t], 0, 0, 0);
-      out[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(plo, v, out[t], 0, 0, 0);
+#pragma unroll
+      for (int n = 0; n < 3; ++n)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          out[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(p[j].term[n][0], p[j].term[n][1], p[j].term[n][2], p[j].term[n][3]), v, out[j][t], 0, 0, 0);
     }
+  }
+  // ... from LDS, 16 bytes of a row a place: K's places are swapped within a row by its number, or the 16 lanes of a read would meet in the same banks
+  static constexpr int kPieces = D / 8;
+  static __device__ __forceinline__ int k_place(int row, int piece) { return row * kPieces + (piece ^ (row & (kPieces - 1))); }
+  static __device__ __forceinline__ void read(const u32x4* k, int c16, int g4, Keys& x) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int i = 0; i < KW / 4; ++i) {
+        const u32x4 u = k[k_place(16 * tt + c16, g4 + 4 * i)];
+        x.w[tt][4 * i] = u.x; x.w[tt][4 * i + 1] = u.y; x.w[tt][4 * i + 2] = u.z; x.w[tt][4 * i + 3] = u.w;
+      }
+  }
+  static __device__ __forceinline__ void read(const u32x4* v, int c16, int g4, Values& x) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t* const p = reinterpret_cast<const uint32_t*>(v) + (16 * tt + 4 * g4 + i) * (D / 2) + VW * c16;
+        if constexpr (VW == 4) {
+          const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+          x.w[tt][i][0] = u.x; x.w[tt][i][1] = u.y; x.w[tt][i][2] = u.z; x.w[tt][i][3] = u.w;
+        } else {
+          const u32x2 u = *reinterpret_cast<const u32x2*>(p);
+          x.w[tt][i][0] = u.x; x.w[tt][i][1] = u.y;
+        }
+      }
+  }
+  static __device__ __forceinline__ void negate(Queries& q) {
+#pragma unroll
+    for (int i = 0; i < KW; ++i) q.w[i] ^= 0x80008000u;
   }
 };
 template <int D> struct Form<float, D> {
   static constexpr int kTiles = 1, kRows = 16, KW = D / 4, VT = D / 16;
   struct Queries { float w[KW]; };
-  struct Rows { float k[1][KW], v[1][4][VT]; };
+  struct Keys { float w[1][KW]; };
+  struct Values { float w[1][4][VT]; };
+  struct Weights { float p[4]; };
   // (a load takes 16 bytes a lane: four neighbouring columns of each half of a row)
   static __device__ __forceinline__ int column(int c16, int t) { return t / 4 * 64 + 4 * c16 + t % 4; }
   static __device__ __forceinline__ void queries(const float* q, bool has, int g4, Queries& o) {
@@ -125,88 +177,147 @@ template <int D> struct Form<float, D> {
         o.w[4 * j] = u.x; o.w[4 * j + 1] = u.y; o.w[4 * j + 2] = u.z; o.w[4 * j + 3] = u.w;
       }
   }
-  static __device__ __forceinline__ void load_k(const float* base, int64_t row, int g4, int tile, Rows& x) {
+  static __device__ __forceinline__ void load_k(const float* base, int64_t row, int g4, int tile, Keys& x) {
     const float* const p = base + row * D + 4 * g4;
 #pragma unroll
     for (int j = 0; j < KW / 4; ++j) {
       const float4v u = load_past<float4v>(p + 16 * j);
-      x.k[tile][4 * j] = u.x; x.k[tile][4 * j + 1] = u.y; x.k[tile][4 * j + 2] = u.z; x.k[tile][4 * j + 3] = u.w;
+      x.w[tile][4 * j] = u.x; x.w[tile][4 * j + 1] = u.y; x.w[tile][4 * j + 2] = u.z; x.w[tile][4 * j + 3] = u.w;
     }
   }
-  static __device__ __forceinline__ void load_v(const float* base, int64_t row, int c16, int tile, int i, Rows& x) {
+  static __device__ __forceinline__ void load_v(const float* base, int64_t row, int c16, int tile, int i, Values& x) {
     const float* const p = base + row * D + 4 * c16;
 #pragma unroll
     for (int j = 0; j < VT / 4; ++j) {
       const float4v u = load_past<float4v>(p + 64 * j);
-      x.v[tile][i][4 * j] = u.x; x.v[tile][i][4 * j + 1] = u.y; x.v[tile][i][4 * j + 2] = u.z; x.v[tile][i][4 * j + 3] = u.w;
+      x.w[tile][i][4 * j] = u.x; x.w[tile][i][4 * j + 1] = u.y; x.w[tile][i][4 * j + 2] = u.z; x.w[tile][i][4 * j + 3] = u.w;
     }
   }
-  static __device__ __forceinline__ float4v scores(const Queries& q, const Rows& x, int tile) {
+  static __device__ __forceinline__ float4v scores(const Queries& q, const Keys& x, int tile) {
     float4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < KW; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[tile][i], q.w[i], acc, 0, 0, 0);
+    for (int i = 0; i < KW; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w[tile][i], q.w[i], acc, 0, 0, 0);
     return acc;
   }
-  static __device__ __forceinline__ void add(const float (&p)[kTiles][4], const Rows& x, float4v (&out)[VT]) {
+  static __device__ __forceinline__ void weights(const float (&p)[kTiles][4], Weights& w) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.p[i] = p[0][i];
+  }
+  template <int N> static __device__ __forceinline__ void add(const Weights (&p)[N], const Values& x, float4v (&out)[N][VT]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int t = 0; t < VT; ++t) out[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[0][i], x.v[0][i][t], out[t], 0, 0, 0);
+      for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int j = 0; j < N; ++j) out[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[j].p[i], x.w[0][i][t], out[j][t], 0, 0, 0);
+  }
+  static constexpr int kPieces = D / 4;
+  static __device__ __forceinline__ int k_place(int row, int piece) { return row * kPieces + (piece ^ row); }      // (16 rows)
+  static __device__ __forceinline__ void read(const u32x4* k, int c16, int g4, Keys& x) {
+#pragma unroll
+    for (int j = 0; j < KW / 4; ++j) {
+      const float4v u = __builtin_bit_cast(float4v, k[k_place(c16, g4 + 4 * j)]);
+      x.w[0][4 * j] = u.x; x.w[0][4 * j + 1] = u.y; x.w[0][4 * j + 2] = u.z; x.w[0][4 * j + 3] = u.w;
+    }
+  }
+  static __device__ __forceinline__ void read(const u32x4* v, int c16, int g4, Values& x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < VT / 4; ++j) {
+        const float4v u = __builtin_bit_cast(float4v, v[(4 * g4 + i) * kPieces + 16 * j + c16]);
+        x.w[0][i][4 * j] = u.x; x.w[0][i][4 * j + 1] = u.y; x.w[0][i][4 * j + 2] = u.z; x.w[0][i][4 * j + 3] = u.w;
+      }
+  }
+  static __device__ __forceinline__ void negate(Queries& q) {
+#pragma unroll
+    for (int i = 0; i < KW; ++i) q.w[i] = -q.w[i];
   }
 };
 
-// A wave's online softmax: running maximum (in log2 units, common to the four lanes of a query), this lane's sum, weighted V of queries 4 g4 + i.
-template <typename T, int D> struct State {
+// The scale of scores in log2 units, above 0 or 0 (queries change their signs for a negative one), and how scores are compared with a reference.
+struct Scale {
+  float log2e, inverse;
+  bool negate;
+};
+
+// A wave's online softmax over N tiles of queries that read the same rows: reference (in log2 units, common to the four lanes of a query), this lane's
+// sum, weighted V of queries 4 g4 + i.  The reference is the largest score at first and is moved only when one exceeds it by 2^kSlack.
+template <typename T, int D, int N> struct State {
   typedef Form<T, D> F;
-  float m = -INFINITY, sum = 0.f;
-  float4v out[F::VT];
+  static constexpr uint32_t kAll = F::kRows == 32 ? 0xFFFFFFFFu : 0xFFFFu;
+  float m[N], shift[N], limit[N], sum[N];                  // shift: the reference, or 0 before there is one; limit: where it is moved, in products
+  float4v out[N][F::VT];
   __device__ __forceinline__ State() {
 #pragma unroll
-    for (int t = 0; t < F::VT; ++t) out[t] = float4v{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < N; ++j) {
+      m[j] = limit[j] = -INFINITY;
+      shift[j] = sum[j] = 0.f;
+#pragma unroll
+      for (int t = 0; t < F::VT; ++t) out[j][t] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
   }
-  // `where`: lane r has the cache row of row r of the step, or kNoRow
-  __device__ __forceinline__ void step(const typename F::Queries& q, const typename F::Rows& x, uint32_t where, float scale_log2e, int g4) {
+  // `there`: the step's rows that there are, a bit each
+  __device__ __forceinline__ void weigh(int j, const typename F::Queries& q, const typename F::Keys& x, uint32_t there, const Scale& scale, int g4,
+                                        typename F::Weights& w) {
     float p[F::kTiles][4];
     float mx = -INFINITY;
 #pragma unroll
     for (int tt = 0; tt < F::kTiles; ++tt) {
       const float4v acc = F::scores(q, x, tt);
 #pragma unroll
+      for (int i = 0; i < 4; ++i) p[tt][i] = acc[i];
+    }
+    if (there != kAll)
+#pragma unroll
+      for (int tt = 0; tt < F::kTiles; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!((there >> (16 * tt + 4 * g4 + i)) & 1u)) p[tt][i] = -INFINITY;
+#pragma unroll
+    for (int tt = 0; tt < F::kTiles; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, p[tt][i]);
+    if (__any(mx > limit[j])) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float m_new = mx == -INFINITY ? m[j] : fmaxf(m[j], mx * scale.log2e);
+      const float alpha = m_new == -INFINITY ? 1.f : exp2f(m[j] - m_new);
+      m[j] = m_new;
+      shift[j] = m_new == -INFINITY ? 0.f : m_new;
+      limit[j] = (m_new + kSlack) * scale.inverse;
+      sum[j] *= alpha;
+#pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool valid = (uint32_t)__shfl((int)where, 16 * tt + 4 * g4 + i, 64) != kNoRow;
-        p[tt][i] = valid ? acc[i] * scale_log2e : -INFINITY;
-        mx = fmaxf(mx, p[tt][i]);
+        const float a = __shfl(alpha, 4 * g4 + i, 64);
+#pragma unroll
+        for (int t = 0; t < F::VT; ++t) out[j][t][i] *= a;
       }
     }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float m_new = fmaxf(m, mx);
-    const bool none = m_new == -INFINITY;                  // (scores of a query with infinities, too)
-    const float alpha = none ? 1.f : exp2f(m - m_new);
-    m = m_new;
+#pragma unroll
+    for (int tt = 0; tt < F::kTiles; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[tt][i] = __builtin_amdgcn_exp2f(fmaf(p[tt][i], scale.log2e, -shift[j]));
+    if (there != kAll)                                     // (a scale of 0 would make a number of what is not there)
+#pragma unroll
+      for (int tt = 0; tt < F::kTiles; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!((there >> (16 * tt + 4 * g4 + i)) & 1u)) p[tt][i] = 0.f;
     float more = 0.f;
 #pragma unroll
     for (int tt = 0; tt < F::kTiles; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[tt][i] = none ? 0.f : exp2f(p[tt][i] - m_new);
-        more += p[tt][i];
-      }
-    sum = fmaf(sum, alpha, more);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float a = __shfl(alpha, 4 * g4 + i, 64);
-#pragma unroll
-      for (int t = 0; t < F::VT; ++t) out[t][i] *= a;
-    }
-    F::add(p, x, out);
+      for (int i = 0; i < 4; ++i) more += p[tt][i];
+    sum[j] += more;
+    F::weights(p, w);
   }
 };
 
 // Requests a step's rows.  Rows that are not there are read as the step's first one that is: what a cache holds in other places may be anything.
 // False, and nothing requested, if there is none.
 template <typename T, int D>
-__device__ __forceinline__ bool request(const T* K, const T* V, uint32_t where, int lane, int c16, int g4, typename Form<T, D>::Rows& x) {
+__device__ __forceinline__ bool request(const T* K, const T* V, uint32_t where, int lane, int c16, int g4, typename Form<T, D>::Keys& k, typename Form<T, D>::Values& v) {
   typedef Form<T, D> F;
   const uint64_t there = __ballot(where != kNoRow);
   if (there == 0) return false;
@@ -214,57 +325,69 @@ __device__ __forceinline__ bool request(const T* K, const T* V, uint32_t where, 
   const uint32_t row = where == kNoRow ? stand_in : where;
 #pragma unroll
   for (int tt = 0; tt < F::kTiles; ++tt) {
-    F::load_k(K, (uint32_t)__shfl((int)row, 16 * tt + c16, 64), g4, tt, x);
+    F::load_k(K, (uint32_t)__shfl((int)row, 16 * tt + c16, 64), g4, tt, k);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) F::load_v(V, (uint32_t)__shfl((int)row, 16 * tt + 4 * g4 + i, 64), c16, tt, i, x);
+    for (int i = 0; i < 4; ++i) F::load_v(V, (uint32_t)__shfl((int)row, 16 * tt + 4 * g4 + i, 64), c16, tt, i, v);
   }
   return true;
 }
 
 // Steps first, first + stride, ... below end of what `lookup` names (the cache row of row lane % kRows of a step), two under way.
 template <typename T, int D, typename Lookup>
-__device__ __forceinline__ void walk(State<T, D>& state, const typename Form<T, D>::Queries& q, const T* K, const T* V, int first, int end, int stride,
-                                     float scale_log2e, int lane, const Lookup& lookup) {
+__device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<T, D>::Queries& q, const T* K, const T* V, int first, int end, int stride,
+                                     const Scale& scale, int lane, const Lookup& lookup) {
+  typedef Form<T, D> F;
   const int c16 = lane & 15, g4 = lane >> 4;
-  typename Form<T, D>::Rows xa, xb;
-  uint32_t wa = kNoRow, wb = kNoRow, next = kNoRow;
-  bool has_a = false, has_b = false;
+  struct Step {
+    typename F::Keys k;
+    typename F::Values v;
+    uint32_t where;
+    bool has;
+  } xa, xb;
+  uint32_t next = kNoRow;
+  auto ask = [&](Step& x) { x.has = request<T, D>(K, V, x.where, lane, c16, g4, x.k, x.v); };
   if (first < end) {
-    wa = lookup(first);
-    if (first + stride < end) wb = lookup(first + stride);
-    has_a = request<T, D>(K, V, wa, lane, c16, g4, xa);
-    has_b = first + stride < end && request<T, D>(K, V, wb, lane, c16, g4, xb);
+    xa.where = lookup(first);
+    xb.where = first + stride < end ? lookup(first + stride) : kNoRow;
+    ask(xa);
+    ask(xb);
     if (first + 2 * stride < end) next = lookup(first + 2 * stride);
   }
-  auto turn = [&](int st, typename Form<T, D>::Rows& x, uint32_t& w, bool& has) {
-    if (has) state.step(q, x, w, scale_log2e, g4);
-    has = false;
+  auto turn = [&](int st, Step& x) {
+    if (x.has) {
+      typename F::Weights w[1];
+      state.weigh(0, q, x.k, (uint32_t)__ballot(x.where != kNoRow) & State<T, D, 1>::kAll, scale, g4, w[0]);
+      F::template add<1>(w, x.v, state.out);
+    }
     if (st + 2 * stride < end) {
-      w = next;
-      has = request<T, D>(K, V, w, lane, c16, g4, x);
+      x.where = next;
+      ask(x);
       if (st + 3 * stride < end) next = lookup(st + 3 * stride);
     }
   };
   for (int st = first; st < end; st += 2 * stride) {
-    turn(st, xa, wa, has_a);
-    if (st + stride < end) turn(st + stride, xb, wb, has_b);
+    turn(st, xa);
+    if (st + stride < end) turn(st + stride, xb);
   }
 }
 
 // The waves' states as one, through LDS in a fixed order: into a record of `rows` queries, or (whole) the result itself.
+constexpr size_t merge_bytes(int d) { return (size_t)kAttWaves * 16 * (d + 2) * sizeof(float); }
 template <typename T, int D>
-__device__ __forceinline__ void merge_waves(State<T, D>& state, int rows, float* record, float* whole) {
+__device__ __forceinline__ void merge_waves(State<T, D, 1>& state, int rows, float* lds, float* record, float* whole) {
   typedef Form<T, D> F;
-  __shared__ float sm_m[kAttWaves][16], sm_l[kAttWaves][16];
-  __shared__ float sm_o[kAttWaves][16][D];
+  float(*const sm_m)[16] = reinterpret_cast<float(*)[16]>(lds);
+  float(*const sm_l)[16] = sm_m + kAttWaves;
+  float(*const sm_o)[16][D] = reinterpret_cast<float(*)[16][D]>(sm_l + kAttWaves);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g4 = lane >> 4;
-  state.sum += __shfl_xor(state.sum, 16, 64);
-  state.sum += __shfl_xor(state.sum, 32, 64);
-  if (g4 == 0) { sm_m[wave][c16] = state.m; sm_l[wave][c16] = state.sum; }
+  float sum = state.sum[0];
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (g4 == 0) { sm_m[wave][c16] = state.m[0]; sm_l[wave][c16] = sum; }
 #pragma unroll
   for (int t = 0; t < F::VT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sm_o[wave][4 * g4 + i][F::column(c16, t)] = state.out[t][i];
+    for (int i = 0; i < 4; ++i) sm_o[wave][4 * g4 + i][F::column(c16, t)] = state.out[0][t][i];
   __syncthreads();
   for (int item = tid; item < rows * D; item += kAttThreads) {
     const int g = item / D, dim = item % D;
@@ -280,7 +403,7 @@ __device__ __forceinline__ void merge_waves(State<T, D>& state, int rows, float*
         lt = fmaf(sm_l[w][g], f, lt);
       }
     if (whole) {
-      whole[(int64_t)g * D + dim] = lt > 0.f ? acc / lt : 0.f;
+      whole[(int64_t)g * D + dim] = acc / (lt == 0.f ? 1.f : lt);
     } else {
       record[2 * rows + item] = acc;
       if (dim == 0) { record[g] = M; record[rows + g] = lt; }
@@ -292,7 +415,7 @@ __device__ __forceinline__ void merge_waves(State<T, D>& state, int rows, float*
 // grid = (parts, units): the waves of a unit's parts take its steps in turn, so that a list that ends early leaves none idle before the others.
 template <typename T, int D>
 __global__ __launch_bounds__(kAttThreads, 2) void attend_chosen_kernel(PagedArgs a, const T* __restrict__ Q, int G, const int32_t* __restrict__ chosen, int count,
-                                                                       float scale_log2e, float* __restrict__ records, float* __restrict__ whole) {
+                                                                       Scale scale, float* __restrict__ records, float* __restrict__ whole) {
   typedef Form<T, D> F;
   const int u = blockIdx.y, b = u / (a.L * a.H), in = u - b * a.L * a.H;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
@@ -301,6 +424,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_chosen_kernel(PagedArgs
   const int32_t* const list = chosen + (int64_t)u * count;
   typename F::Queries q;
   F::queries(Q + ((int64_t)u * G + min(c16, G - 1)) * D, c16 < G, g4, q);
+  if (scale.negate) F::negate(q);
   auto lookup = [&](int st) -> uint32_t {
     const int at = st * F::kRows + (lane & (F::kRows - 1)), entry = at / a.page_size, off = at - entry * a.page_size;
     if (entry >= count) return kNoRow;
@@ -311,26 +435,92 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_chosen_kernel(PagedArgs
   };
   const int waves = gridDim.x * kAttWaves, wave = blockIdx.x * kAttWaves + uniform(threadIdx.x >> 6);
   const int steps = (count * a.page_size + F::kRows - 1) / F::kRows;
-  State<T, D> state;
-  walk<T, D>(state, q, static_cast<const T*>(a.K), static_cast<const T*>(a.V), wave, steps, waves, scale_log2e, lane, lookup);
-  merge_waves<T, D>(state, G, records + ((int64_t)u * gridDim.x + blockIdx.x) * record_floats(G, D), whole ? whole + (int64_t)u * G * D : nullptr);
+  State<T, D, 1> state;
+  walk<T, D>(state, q, static_cast<const T*>(a.K), static_cast<const T*>(a.V), wave, steps, waves, scale, lane, lookup);
+  __shared__ __align__(16) float merged[merge_bytes(D) / sizeof(float)];
+  merge_waves<T, D>(state, G, merged, records + ((int64_t)u * gridDim.x + blockIdx.x) * record_floats(G, D), whole ? whole + (int64_t)u * G * D : nullptr);
 }
 
-// grid = (G, units), a thread per column
-__global__ void chosen_merge_kernel(const float* __restrict__ records, int parts, int G, int D, float* __restrict__ out) {
-  const int g = blockIdx.x, u = blockIdx.y, dim = threadIdx.x;
-  const int64_t size = record_floats(G, D);
-  const float* const base = records + (int64_t)u * parts * size;
-  float M = -INFINITY, acc = 0.f, lt = 0.f;
-  for (int k = 0; k < parts; ++k) M = fmaxf(M, base[k * size + g]);
-  if (M > -INFINITY)
-    for (int k = 0; k < parts; ++k) {
-      const float* const rec = base + k * size;
-      const float w = exp2f(rec[g] - M);
-      acc = fmaf(rec[2 * G + g * D + dim], w, acc);
-      lt = fmaf(rec[G + g], w, lt);
+// What records hold of a query's row: largest score, sum, four columns of the weighted V.
+struct Part {
+  float m = -INFINITY, sum = 0.f;
+  float4v o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void join(float m2, float sum2, const float4v& o2) {
+    const float M = fmaxf(m, m2);
+    if (M == -INFINITY) return;
+    const float w1 = exp2f(m - M), w2 = exp2f(m2 - M);
+    m = M;
+    sum = sum * w1 + sum2 * w2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = o[i] * w1 + o2[i] * w2;
+  }
+  // records from, from + step, ... below end at `base`, each of `queries` rows, `size` floats; kAtOnce of them under way
+  template <int D> __device__ __forceinline__ void join_records(const float* base, int from, int end, int step, int64_t size, int queries, int row, int c4) {
+    constexpr int kAtOnce = 8;
+    for (int k0 = from; k0 < end; k0 += kAtOnce * step) {
+      float ms[kAtOnce], sums[kAtOnce];
+      float4v os[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float* const rec = base + min(k0 + j * step, end - 1) * size;
+        ms[j] = k0 + j * step < end ? rec[row] : -INFINITY;
+        sums[j] = rec[queries + row];
+        // (records' rows lie at multiples of 8 bytes)
+        const float* const o = rec + 2 * queries + (int64_t)row * D + 4 * c4;
+        const float2v a = *reinterpret_cast<const float2v*>(o), b = *reinterpret_cast<const float2v*>(o + 2);
+        os[j] = float4v{a.x, a.y, b.x, b.y};
+      }
+      float M = m;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) M = fmaxf(M, ms[j]);
+      if (M == -INFINITY) continue;
+      const float w = exp2f(m - M);
+      m = M;
+      sum *= w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= w;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float v = exp2f(ms[j] - M);
+        sum = fmaf(sums[j], v, sum);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(os[j][i], v, o[i]);
+      }
     }
-  out[((int64_t)u * G + g) * D + dim] = lt > 0.f ? acc / lt : 0.f;
+  }
+};
+
+// The parts that a workgroup's `slots` threads of each item have, in order, and the result of the first.
+__device__ __forceinline__ void finish_parts(Part& part, int slots, int item, int items, int slot, float* lds, float* out) {
+  if (slots > 1) {
+    float* const mine = lds + ((int64_t)slot * items + item) * 6;
+    if (slot > 0 && item < items) {
+      mine[0] = part.m;
+      mine[1] = part.sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mine[2 + i] = part.o[i];
+    }
+    __syncthreads();
+    if (slot == 0 && item < items)
+      for (int j = 1; j < slots; ++j) {
+        const float* const x = mine + (int64_t)j * items * 6;
+        part.join(x[0], x[1], float4v{x[2], x[3], x[4], x[5]});
+      }
+  }
+  if (slot == 0 && item < items) {
+    const float sum = part.sum == 0.f ? 1.f : part.sum;    // (no rows: zeros)
+    *reinterpret_cast<float4v*>(out + 4 * item) = float4v{part.o[0] / sum, part.o[1] / sum, part.o[2] / sum, part.o[3] / sum};
+  }
+}
+
+// A workgroup a unit; a thread has four columns of one query and every `slots`-th record.
+template <int D> __global__ __launch_bounds__(1024) void chosen_merge_kernel(const float* __restrict__ records, int parts, int G, int slots, float* __restrict__ out) {
+  extern __shared__ float joined[];
+  const int u = blockIdx.x, items = G * (D / 4), per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = threadIdx.x - slot * per_slot;
+  const int64_t size = record_floats(G, D);
+  Part part;
+  if (item < items) part.join_records<D>(records + (int64_t)u * parts * size, slot, parts, slots, size, G, item / (D / 4), item % (D / 4));
+  finish_parts(part, slots, item, items, slot, joined, out + (int64_t)u * G * D);
 }
 
 // ---- rows of a shared prompt, and of each sequence ---------------------------------------------
@@ -339,7 +529,7 @@ struct SharedArgs {
   const int32_t* starts;         // [P + 1]
   int G, groups;
   int64_t most_common, most_own; // records of either kind that the workspace has
-  float scale_log2e;
+  Scale scale;
   float* common_records;
   float* own_records;
   int2* span;                    // of each prompt's layers, then of each sequence's: first record, pieces of a unit
@@ -381,9 +571,119 @@ __device__ __forceinline__ int64_t wave_scan(int64_t v, int lane) {
   return v;
 }
 
+// A step's rows of K and V in LDS, two steps at a time; the places of 64 steps' rows, and which of them there are.
+template <typename T, int D> struct Staged {
+  typedef Form<T, D> F;
+  static constexpr int kVectors = F::kRows * F::kPieces;   // of 16 bytes, of K or V
+  u32x4 k[2][kVectors], v[2][kVectors];
+  uint32_t places[kStepsLooked * F::kRows];
+  uint32_t there[kStepsLooked];
+};
+
+// Steps first .. end of a unit's rows for up to 64 N queries, N tiles a wave (tiles behind the last query are zeros).  Every thread has its part of a step's rows on the way to registers two steps ahead and
+// puts it into LDS, where the waves find the whole step; one barrier a step.
+template <typename T, int D, int N, typename Places, typename LoadQueries>
+__device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, int first, int end, int queries, const Scale& scale, float* record,
+                                           const Places& place_of, const LoadQueries& load_queries) {
+  typedef Form<T, D> F;
+  typedef Staged<T, D> S;
+  constexpr int kMine = S::kVectors / kAttThreads;         // vectors of K, and of V, a thread and step
+  static_assert(S::kVectors % kAttThreads == 0, "a thread has whole vectors");
+  S& s = *static_cast<S*>(lds);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
+  typename F::Queries q[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) load_queries(16 * (wave + j * kAttWaves), q[j]);
+  State<T, D, N> state;
+  struct Part { u32x4 k[kMine], v[kMine]; };
+  auto request = [&](int at, Part& x) {                    // of step `at` of those that were looked up
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int n = i * kAttThreads + tid, row = n / F::kPieces, piece = n % F::kPieces;
+      const uint32_t place = s.places[at * F::kRows + row];
+      x.k[i] = x.v[i] = u32x4{0u, 0u, 0u, 0u};
+      if (place != kNoRow) {
+        const int64_t from = (int64_t)place * (D * (int)sizeof(T)) + piece * 16;
+        x.k[i] = load_past<u32x4>(reinterpret_cast<const char*>(K) + from);
+        x.v[i] = load_past<u32x4>(reinterpret_cast<const char*>(V) + from);
+      }
+    }
+  };
+  for (int base = first; base < end; base += kStepsLooked) {
+    const int n = min(kStepsLooked, end - base);
+    __syncthreads();                                       // (the steps before are done with)
+    for (int r = tid; r < n * F::kRows; r += kAttThreads) {
+      const uint32_t place = place_of(base * F::kRows + r);
+      s.places[r] = place;
+      const uint64_t found = __ballot(place != kNoRow);    // (whole steps a wave, or none)
+      if constexpr (F::kRows == 32) {
+        if ((lane & 31) == 0) s.there[r / 32] = (uint32_t)(found >> lane);
+      } else {
+        if ((lane & 15) == 0) s.there[r / 16] = (uint32_t)(found >> lane) & 0xFFFFu;
+      }
+    }
+    __syncthreads();
+    Part pa, pb;
+    request(0, pa);
+    if (n > 1) request(1, pb);
+    auto turn = [&](int at, Part& x) {
+      const int buffer = at & 1;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int m = i * kAttThreads + tid;
+        s.k[buffer][F::k_place(m / F::kPieces, m % F::kPieces)] = x.k[i];
+        s.v[buffer][m] = x.v[i];
+      }
+      if (at + 2 < n) request(at + 2, x);
+      const uint32_t there = (uint32_t)uniform((int)s.there[at]);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (what is on the way from memory stays there)
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (there) {
+        typename F::Weights w[N];
+        {
+          typename F::Keys k;
+          F::read(s.k[buffer], c16, g4, k);
+#pragma unroll
+          for (int j = 0; j < N; ++j) state.weigh(j, q[j], k, there, scale, g4, w[j]);
+        }
+        typename F::Values v;
+        F::read(s.v[buffer], c16, g4, v);
+        F::template add<N>(w, v, state.out);
+      }
+    };
+    for (int at = 0; at < n; at += 2) {
+      turn(at, pa);
+      if (at + 1 < n) turn(at + 1, pb);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int from = 16 * (wave + j * kAttWaves);
+    if (from >= queries) break;
+    float sum = state.sum[j];
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (g4 == 0 && from + c16 < queries) {
+      record[from + c16] = state.m[j];
+      record[queries + from + c16] = sum;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int query = from + 4 * g4 + i;
+      if (query < queries)
+#pragma unroll
+        for (int t = 0; t < F::VT; ++t) record[2 * queries + (int64_t)query * D + F::column(c16, t)] = state.out[j][t][i];
+    }
+  }
+}
+
+template <typename T, int D> constexpr size_t shared_lds_bytes() { return sizeof(Staged<T, D>) > merge_bytes(D) ? sizeof(Staged<T, D>) : merge_bytes(D); }
+
 template <typename T, int D>
 __global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArgs a, const T* __restrict__ Q) {
   typedef Form<T, D> F;
+  extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4, wave = uniform(threadIdx.x >> 6);
   const int L = a.own.L, H = a.own.H, G = a.G, shared = a.common.B * L, entries = shared + a.own.B * L;
   // every wave finds out which piece is its workgroup's
@@ -436,31 +736,49 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArg
     first = run.first;
     queries = min(kTileQueries, run.n * G - tile * kTileQueries);
   }
-  const int r = tile * kTileQueries + c16, b = first + r / G, g = r % G;
-  typename F::Queries q;
-  F::queries(Q + (((int64_t)(c16 < queries ? b : first) * L + l) * H * G + (int64_t)h * G + (c16 < queries ? g : 0)) * D, c16 < queries, g4, q);
   const PagedArgs& kv = is_own ? a.own : a.common;
   const int32_t* const table = kv.table + seq * kv.table_b + ((int64_t)l * H + h) * kv.max_pages;
   const int page_size = kv.page_size;
   const int64_t num_pages = kv.num_pages;
-  auto lookup = [&](int st) -> uint32_t {
-    const int row = st * F::kRows + (lane & (F::kRows - 1));
+  const T* const K = static_cast<const T*>(kv.K);
+  const T* const V = static_cast<const T*>(kv.V);
+  auto place_of = [&](int row) -> uint32_t {
     if (row >= rows) return kNoRow;
     const int p = row / page_size, page = table[p];
     return page >= 0 && page < num_pages ? (uint32_t)page * (uint32_t)page_size + (uint32_t)(row - p * page_size) : kNoRow;
   };
-  const int steps = steps_in<F::kRows>(rows), share = pieces * kAttWaves, id = piece * kAttWaves + wave;
-  State<T, D> state;
-  walk<T, D>(state, q, static_cast<const T*>(kv.K), static_cast<const T*>(kv.V), (int)((int64_t)steps * id / share), (int)((int64_t)steps * (id + 1) / share),
-             1, a.scale_log2e, lane, lookup);
-  merge_waves<T, D>(state, queries, is_own ? a.own_records + index * record_floats(G, D) : a.common_records + index * record_floats(kTileQueries, D), nullptr);
+  // query c16 of a tile of 16
+  auto load_queries = [&](int from, typename F::Queries& q) {
+    const bool has = from + c16 < queries;
+    const int r = tile * kTileQueries + from + c16, b = has ? first + r / G : first, g = has ? r % G : 0;
+    F::queries(Q + (((int64_t)b * L + l) * H * G + (int64_t)h * G + g) * D, has, g4, q);
+    if (a.scale.negate) F::negate(q);
+  };
+  float* const record = is_own ? a.own_records + index * record_floats(G, D) : a.common_records + index * record_floats(kTileQueries, D);
+  const int steps = steps_in<F::kRows>(rows);
+  if (queries <= 16) {
+    typename F::Queries q;
+    load_queries(0, q);
+    const int share = pieces * kAttWaves, id = piece * kAttWaves + wave;
+    State<T, D, 1> state;
+    walk<T, D>(state, q, K, V, (int)((int64_t)steps * id / share), (int)((int64_t)steps * (id + 1) / share), 1, a.scale, lane,
+               [&](int st) { return place_of(st * F::kRows + (lane & (F::kRows - 1))); });
+    merge_waves<T, D>(state, queries, reinterpret_cast<float*>(lds), record, nullptr);
+    return;
+  }
+  const int s0 = (int)((int64_t)steps * piece / pieces), s1 = (int)((int64_t)steps * (piece + 1) / pieces);
+  if (queries <= 64) wide_piece<T, D, 1>(lds, K, V, s0, s1, queries, a.scale, record, place_of, load_queries);
+  else wide_piece<T, D, 2>(lds, K, V, s0, s1, queries, a.scale, record, place_of, load_queries);
 }
 
-// grid = (G, B * L * H), a thread per column: the records of the prompt's pieces and of the sequence's own, in order
-template <int D>
-__global__ void shared_merge_kernel(SharedArgs a) {
-  const int L = a.own.L, H = a.own.H, G = a.G, g = blockIdx.x, u = blockIdx.y, dim = threadIdx.x, lane = dim & 63;
-  const int b = u / (L * H), l = u / H % L, h = u % H, P = a.common.B;
+// A workgroup a unit of a sequence: the records of the prompt's pieces and of its own, in order; threads as in chosen_merge_kernel.
+template <int D> __global__ __launch_bounds__(1024) void shared_merge_kernel(SharedArgs a, int slots) {
+  extern __shared__ float joined[];
+  const int L = a.own.L, H = a.own.H, G = a.G, u = blockIdx.x, lane = threadIdx.x & 63, P = a.common.B;
+  const int b = u / (L * H), l = u / H % L, h = u % H, items = G * (D / 4);
+  const int per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = threadIdx.x - slot * per_slot, g = item / (D / 4), c4 = item % (D / 4);
+  const int own_rows = rows_of(a.own, b, l);
+  const int2 own_span = a.span[(P + b) * L + l];
   int p = -1;
   for (int p0 = 0; p0 < P && p < 0; p0 += 64) {
     bool mine = false;
@@ -471,41 +789,35 @@ __global__ void shared_merge_kernel(SharedArgs a) {
     const uint64_t found = __ballot(mine);
     if (found) p = p0 + __builtin_ctzll(found);
   }
-  const float* from[2] = {nullptr, nullptr};
-  int count[2] = {0, 0}, queries[2] = {G, G}, row[2] = {g, g};
-  int64_t size[2] = {record_floats(kTileQueries, D), record_floats(G, D)};
-  if (p >= 0 && rows_of(a.common, p, l) > 0) {
+  Part part;
+  if (p >= 0) {
+    const int rows = rows_of(a.common, p, l);
+    const int2 span = a.span[p * L + l];
     const Run run = run_of(a, p);
     const int tiles = tiles_of(a, run.n), at = (b - run.first) * G + g, tile = at / kTileQueries;
-    const int2 span = a.span[p * L + l];
-    const int64_t index = span.x + (int64_t)(h * tiles + tile) * span.y;
-    if (span.x >= 0 && span.y > 0 && index + span.y <= a.most_common) {
-      from[0] = a.common_records + index * size[0];
-      count[0] = span.y;
-      queries[0] = min(kTileQueries, run.n * G - tile * kTileQueries);
-      row[0] = at - tile * kTileQueries;
-    }
+    const int64_t index = span.x + (int64_t)(h * tiles + tile) * span.y, size = record_floats(kTileQueries, D);
+    if (item < items && rows > 0 && span.x >= 0 && span.y > 0 && index + span.y <= a.most_common)
+      part.join_records<D>(a.common_records + index * size, slot, span.y, slots, size, min(kTileQueries, run.n * G - tile * kTileQueries),
+                           at - tile * kTileQueries, c4);
   }
-  if (rows_of(a.own, b, l) > 0) {
-    const int2 span = a.span[(P + b) * L + l];
-    const int64_t index = span.x + (int64_t)h * span.y;
-    if (span.x >= 0 && span.y > 0 && index + span.y <= a.most_own) {
-      from[1] = a.own_records + index * size[1];
-      count[1] = span.y;
-    }
-  }
-  float M = -INFINITY, acc = 0.f, lt = 0.f;
-  for (int k = 0; k < 2; ++k)
-    for (int i = 0; i < count[k]; ++i) M = fmaxf(M, from[k][i * size[k] + row[k]]);
-  if (M > -INFINITY)
-    for (int k = 0; k < 2; ++k)
-      for (int i = 0; i < count[k]; ++i) {
-        const float* const rec = from[k] + i * size[k];
-        const float w = exp2f(rec[row[k]] - M);
-        acc = fmaf(rec[2 * queries[k] + row[k] * D + dim], w, acc);
-        lt = fmaf(rec[queries[k] + row[k]], w, lt);
-      }
-  a.out[((int64_t)u * G + g) * D + dim] = lt > 0.f ? acc / lt : 0.f;
+  const int64_t index = own_span.x + (int64_t)h * own_span.y, size = record_floats(G, D);
+  if (item < items && own_rows > 0 && own_span.x >= 0 && own_span.y > 0 && index + own_span.y <= a.most_own)
+    part.join_records<D>(a.own_records + index * size, slot, own_span.y, slots, size, G, g, c4);
+  finish_parts(part, slots, item, items, slot, joined, a.out + (int64_t)u * G * D);
+}
+
+// Threads of a merge: as many as a unit has items, in whole waves, for each slot; more slots where few units have many records.
+struct MergeShape { int slots, threads; size_t lds; };
+MergeShape merge_shape(int units, int records, int G, int d) {
+  const int items = G * (d / 4), per_slot = (items + 63) / 64 * 64;
+  int slots = 1;
+  while (slots < 8 && records > 8 * slots && units * 2 * slots * per_slot <= 256 * 1024 && 2 * slots * per_slot <= 1024) slots *= 2;
+  return {slots, slots * per_slot, slots > 1 ? (size_t)slots * items * 6 * sizeof(float) : 0};
+}
+
+Scale scale_of(float scale) {
+  const float s = fabsf(scale) * 1.4426950408889634f;
+  return Scale{s, 1.f / s, scale < 0.f};
 }
 
 // Query tiles of all prompts at most
@@ -549,7 +861,7 @@ hipError_t attend_chosen_launch(const void* Q, int group, const fc_paged_kv& kv,
     ProfileScope ps("attend_chosen_kernel", s);
     auto launch = [&](auto kern, auto type) {
       typedef decltype(type) T;
-      hipLaunchKernelGGL(kern, dim3(parts, units), dim3(kAttThreads), 0, s, a, static_cast<const T*>(Q), group, chosen, count, scale * 1.4426950408889634f, records,
+      hipLaunchKernelGGL(kern, dim3(parts, units), dim3(kAttThreads), 0, s, a, static_cast<const T*>(Q), group, chosen, count, scale_of(scale), records,
                          parts == 1 ? out : nullptr);
     };
     if (kv.dtype == FC_BF16) d == 128 ? launch(attend_chosen_kernel<uint16_t, 128>, uint16_t{}) : launch(attend_chosen_kernel<uint16_t, 64>, uint16_t{});
@@ -558,7 +870,9 @@ hipError_t attend_chosen_launch(const void* Q, int group, const fc_paged_kv& kv,
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   ProfileScope ps("chosen_merge_kernel", s);
-  hipLaunchKernelGGL(chosen_merge_kernel, dim3(group, units), dim3(d), 0, s, records, parts, group, d, out);
+  const MergeShape m = merge_shape(units, parts, group, d);
+  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(units), dim3(m.threads), m.lds, s, records, parts, group, m.slots, out); };
+  d == 128 ? launch(chosen_merge_kernel<128>) : launch(chosen_merge_kernel<64>);
   return hipGetLastError();
 }
 
@@ -572,22 +886,27 @@ hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& com
   const SharedSizes z = shared_sizes(P, B, L, H, group, d);
   float* const records = static_cast<float*>(ws);
   float* const own_records = records + z.common * record_floats(kTileQueries, d);
-  SharedArgs a{paged_args(common), paged_args(own), starts, group, kGroups, z.common, z.own, scale * 1.4426950408889634f, records, own_records,
+  SharedArgs a{paged_args(common), paged_args(own), starts, group, kGroups, z.common, z.own, scale_of(scale), records, own_records,
                reinterpret_cast<int2*>(own_records + z.own * record_floats(group, d)), out};
   {
     ProfileScope ps("attend_shared_kernel", s);
     const int64_t groups = kGroups + (int64_t)L * H * (most_tiles(P, B, group) + B);
-    auto launch = [&](auto kern, auto type) {
+    auto launch = [&](auto kern, size_t lds, auto type) {
       typedef decltype(type) T;
-      hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAttThreads), 0, s, a, static_cast<const T*>(Q));
+      hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAttThreads), lds, s, a, static_cast<const T*>(Q));
     };
-    if (own.dtype == FC_BF16) d == 128 ? launch(attend_shared_kernel<uint16_t, 128>, uint16_t{}) : launch(attend_shared_kernel<uint16_t, 64>, uint16_t{});
-    else d == 128 ? launch(attend_shared_kernel<float, 128>, float{}) : launch(attend_shared_kernel<float, 64>, float{});
+    if (own.dtype == FC_BF16)
+      d == 128 ? launch(attend_shared_kernel<uint16_t, 128>, shared_lds_bytes<uint16_t, 128>(), uint16_t{})
+               : launch(attend_shared_kernel<uint16_t, 64>, shared_lds_bytes<uint16_t, 64>(), uint16_t{});
+    else
+      d == 128 ? launch(attend_shared_kernel<float, 128>, shared_lds_bytes<float, 128>(), float{})
+               : launch(attend_shared_kernel<float, 64>, shared_lds_bytes<float, 64>(), float{});
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ProfileScope ps("shared_merge_kernel", s);
-  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(group, B * L * H), dim3(d), 0, s, a); };
+  const MergeShape m = merge_shape(B * L * H, std::max(1, kGroups / (L * H)), group, d);
+  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(B * L * H), dim3(m.threads), m.lds, s, a, m.slots); };
   d == 128 ? launch(shared_merge_kernel<128>) : launch(shared_merge_kernel<64>);
   return hipGetLastError();
 }

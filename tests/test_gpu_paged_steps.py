@@ -6,8 +6,8 @@ Tolerances.  u = 2^-24, half a step of fp32.
              result.  Values, other slots and bounds of what was stored: equal.
   choice     equal (scores are summed in 64 bits).
   attention  a logit is a sum of d products in fp32: off by at most d u sum |q k| scale, its scaling and exponential by 4 u (|logit| + 1), twice
-             (its own and the reference's); bf16 rows take probabilities as two terms, each to nearest: 2^-18; the sums over n rows go at
-             least 16 at a time, then pieces: n / 16 + 64 roundings.  All of it relative to sum p |v|.
+             (its own and the reference's); the sums over n rows go at least 16 at a time, then pieces: n / 16 + 64 roundings.  All of it
+             relative to sum p |v|.
 """
 import math
 
@@ -91,7 +91,7 @@ def _check_attention(got, Q, scale, rows_for, dtype):
                 g = slice(h * rows_for.group, (h + 1) * rows_for.group)
                 K, V = rows_for(b, l, h)
                 want, size, logit, terms = pr.attend(Q[b, l, g], K, V, scale)
-                slip = 2 * (d * U * terms + 4 * U * (logit + 1)) + (K.shape[0] / 16 + 64) * U + (2.0 ** -18 if dtype == "bf16" else 0.0)
+                slip = 2 * (d * U * terms + 4 * U * (logit + 1)) + (K.shape[0] / 16 + 64) * U
                 worst = np.max(np.abs(got[b, l, g] - want) - slip * size)
                 assert worst <= 0, (b, l, h, K.shape[0], worst)
                 h += 1
