@@ -314,60 +314,63 @@ template <typename T, int D, int N> struct State {
   }
 };
 
-// Requests a step's rows.  Rows that are not there are read as the step's first one that is: what a cache holds in other places may be anything.
-// False, and nothing requested, if there is none.
-template <typename T, int D>
-__device__ __forceinline__ bool request(const T* K, const T* V, uint32_t where, int lane, int c16, int g4, typename Form<T, D>::Keys& k, typename Form<T, D>::Values& v) {
+// A wave's steps 0 .. n - 1, two under way.  `begin(step, r)` loads what leads to the place of row r of a step, `finish` takes that and loads the place
+// (the cache row, or kNoRow): both for as many steps together as 64 lanes have rows of, and a turn ahead of their use.
+template <typename T, int D, typename Begin, typename Finish>
+__device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<T, D>::Queries& q, const T* K, const T* V, int n, const Scale& scale, int lane,
+                                     const Begin& begin, const Finish& finish) {
   typedef Form<T, D> F;
-  const uint64_t there = __ballot(where != kNoRow);
-  if (there == 0) return false;
-  const uint32_t stand_in = (uint32_t)__builtin_amdgcn_readlane((int)where, __builtin_ctzll(there));
-  const uint32_t row = where == kNoRow ? stand_in : where;
-#pragma unroll
-  for (int tt = 0; tt < F::kTiles; ++tt) {
-    F::load_k(K, (uint32_t)__shfl((int)row, 16 * tt + c16, 64), g4, tt, k);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) F::load_v(V, (uint32_t)__shfl((int)row, 16 * tt + 4 * g4 + i, 64), c16, tt, i, v);
-  }
-  return true;
-}
-
-// Steps first, first + stride, ... below end of what `lookup` names (the cache row of row lane % kRows of a step), two under way.
-template <typename T, int D, typename Lookup>
-__device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<T, D>::Queries& q, const T* K, const T* V, int first, int end, int stride,
-                                     const Scale& scale, int lane, const Lookup& lookup) {
-  typedef Form<T, D> F;
-  const int c16 = lane & 15, g4 = lane >> 4;
+  constexpr int kTogether = 64 / F::kRows;                 // steps of a look-up
+  const int c16 = lane & 15, g4 = lane >> 4, r = lane % F::kRows, of = lane / F::kRows;
   struct Step {
     typename F::Keys k;
     typename F::Values v;
-    uint32_t where;
-    bool has;
+    uint32_t there;
   } xa, xb;
-  uint32_t next = kNoRow;
-  auto ask = [&](Step& x) { x.has = request<T, D>(K, V, x.where, lane, c16, g4, x.k, x.v); };
-  if (first < end) {
-    xa.where = lookup(first);
-    xb.where = first + stride < end ? lookup(first + stride) : kNoRow;
-    ask(xa);
-    ask(xb);
-    if (first + 2 * stride < end) next = lookup(first + 2 * stride);
-  }
-  auto turn = [&](int st, Step& x) {
-    if (x.has) {
-      typename F::Weights w[1];
-      state.weigh(0, q, x.k, (uint32_t)__ballot(x.where != kNoRow) & State<T, D, 1>::kAll, scale, g4, w[0]);
-      F::template add<1>(w, x.v, state.out);
+  if (n <= 0) return;
+  auto begin_group = [&](int group) { return begin(min(group * kTogether + of, n - 1), r); };
+  auto finish_group = [&](int group, auto token) {
+    const uint32_t place = finish(token, min(group * kTogether + of, n - 1), r);
+    return group * kTogether + of < n ? place : kNoRow;
+  };
+  const auto t0 = begin_group(0), t1 = begin_group(1);
+  auto ahead = begin_group(2);
+  uint32_t now = finish_group(0, t0), next = finish_group(1, t1);
+  int group = 0;
+  // Rows that are not there are read as the step's first one that is: what a cache holds in other places may be anything.
+  auto ask = [&](int st, Step& x) {
+    if (st / kTogether != group) {
+      now = next;
+      next = finish_group(group + 2, ahead);
+      ahead = begin_group(group + 3);
+      ++group;
     }
-    if (st + 2 * stride < end) {
-      x.where = next;
-      ask(x);
-      if (st + 3 * stride < end) next = lookup(st + 3 * stride);
+    const int base = st % kTogether * F::kRows;
+    const uint64_t found = __ballot(now != kNoRow) >> base;
+    x.there = (uint32_t)found & State<T, D, 1>::kAll;
+    if (x.there == 0) return;
+    const uint32_t stand_in = (uint32_t)__builtin_amdgcn_readlane((int)now, base + __builtin_ctz(x.there));
+    const uint32_t row = now == kNoRow ? stand_in : now;
+#pragma unroll
+    for (int tt = 0; tt < F::kTiles; ++tt) {
+      F::load_k(K, (uint32_t)__shfl((int)row, base + 16 * tt + c16, 64), g4, tt, x.k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) F::load_v(V, (uint32_t)__shfl((int)row, base + 16 * tt + 4 * g4 + i, 64), c16, tt, i, x.v);
     }
   };
-  for (int st = first; st < end; st += 2 * stride) {
+  ask(0, xa);
+  if (n > 1) ask(1, xb);
+  auto turn = [&](int st, Step& x) {
+    if (x.there) {
+      typename F::Weights w[1];
+      state.weigh(0, q, x.k, x.there, scale, g4, w[0]);
+      F::template add<1>(w, x.v, state.out);
+    }
+    if (st + 2 < n) ask(st + 2, x);
+  };
+  for (int st = 0; st < n; st += 2) {
     turn(st, xa);
-    if (st + stride < end) turn(st + stride, xb);
+    if (st + 1 < n) turn(st + 1, xb);
   }
 }
 
@@ -425,18 +428,18 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_chosen_kernel(PagedArgs
   typename F::Queries q;
   F::queries(Q + ((int64_t)u * G + min(c16, G - 1)) * D, c16 < G, g4, q);
   if (scale.negate) F::negate(q);
-  auto lookup = [&](int st) -> uint32_t {
-    const int at = st * F::kRows + (lane & (F::kRows - 1)), entry = at / a.page_size, off = at - entry * a.page_size;
-    if (entry >= count) return kNoRow;
-    const int p = list[entry];
-    if (p < 0 || p >= a.max_pages || (int64_t)p * a.page_size + off >= rows) return kNoRow;
-    const int page = table[p];
-    return page >= 0 && page < a.num_pages ? (uint32_t)page * (uint32_t)a.page_size + (uint32_t)off : kNoRow;
-  };
   const int waves = gridDim.x * kAttWaves, wave = blockIdx.x * kAttWaves + uniform(threadIdx.x >> 6);
   const int steps = (count * a.page_size + F::kRows - 1) / F::kRows;
+  // step i of the wave is step wave + i * waves of the unit
+  auto begin = [&](int i, int r) { return list[min(a.pages.of((wave + i * waves) * F::kRows + r), count - 1)]; };
+  auto finish = [&](int p, int i, int r) -> uint32_t {
+    const int at = (wave + i * waves) * F::kRows + r, entry = a.pages.of(at), off = at - entry * a.page_size;
+    const bool held = entry < count && p >= 0 && p < a.max_pages && (int64_t)p * a.page_size + off < rows;
+    const int page = table[held ? p : 0];
+    return held && page >= 0 && page < a.num_pages ? (uint32_t)page * (uint32_t)a.page_size + (uint32_t)off : kNoRow;
+  };
   State<T, D, 1> state;
-  walk<T, D>(state, q, static_cast<const T*>(a.K), static_cast<const T*>(a.V), wave, steps, waves, scale, lane, lookup);
+  walk<T, D>(state, q, static_cast<const T*>(a.K), static_cast<const T*>(a.V), (steps - wave + waves - 1) / waves, scale, lane, begin, finish);
   __shared__ __align__(16) float merged[merge_bytes(D) / sizeof(float)];
   merge_waves<T, D>(state, G, merged, records + ((int64_t)u * gridDim.x + blockIdx.x) * record_floats(G, D), whole ? whole + (int64_t)u * G * D : nullptr);
 }
@@ -744,7 +747,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArg
   const T* const V = static_cast<const T*>(kv.V);
   auto place_of = [&](int row) -> uint32_t {
     if (row >= rows) return kNoRow;
-    const int p = row / page_size, page = table[p];
+    const int p = kv.pages.of(row), page = table[p];
     return page >= 0 && page < num_pages ? (uint32_t)page * (uint32_t)page_size + (uint32_t)(row - p * page_size) : kNoRow;
   };
   // query c16 of a tile of 16
@@ -761,8 +764,12 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArg
     load_queries(0, q);
     const int share = pieces * kAttWaves, id = piece * kAttWaves + wave;
     State<T, D, 1> state;
-    walk<T, D>(state, q, K, V, (int)((int64_t)steps * id / share), (int)((int64_t)steps * (id + 1) / share), 1, a.scale, lane,
-               [&](int st) { return place_of(st * F::kRows + (lane & (F::kRows - 1))); });
+    const int s0 = (int)((int64_t)steps * id / share), s1 = (int)((int64_t)steps * (id + 1) / share);
+    walk<T, D>(state, q, K, V, s1 - s0, a.scale, lane, [&](int i, int r) { return table[kv.pages.of(min((s0 + i) * F::kRows + r, rows - 1))]; },
+               [&](int page, int i, int r) {
+                 const int row = (s0 + i) * F::kRows + r;
+                 return row < rows && page >= 0 && page < num_pages ? (uint32_t)page * (uint32_t)page_size + (uint32_t)(row - kv.pages.of(row) * page_size) : kNoRow;
+               });
     merge_waves<T, D>(state, queries, reinterpret_cast<float*>(lds), record, nullptr);
     return;
   }
@@ -838,10 +845,20 @@ SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d) {
   return z;
 }
 
-// Parts of a unit: enough waves for the chip, two steps each at least.
+// Workgroups that a unit's `steps` are cut into.  512 are resident together; a round of them costs about two steps besides what its waves have to do, so
+// that long lists are cut for one round and a step a wave is the least.
 int chosen_parts(int units, int count, int page_size, int step_rows) {
   const int64_t steps = ((int64_t)count * page_size + step_rows - 1) / step_rows;
-  return (int)std::max<int64_t>(1, std::min<int64_t>((1024 + units - 1) / units, steps / (2 * kAttWaves)));
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int parts = 1; parts <= 64 && (parts == 1 || (int64_t)kAttWaves * (parts - 1) < steps); ++parts) {
+    const int64_t rounds = ((int64_t)units * parts + kGroups - 1) / kGroups, cost = rounds * (2 + (steps + kAttWaves * parts - 1) / (kAttWaves * parts));
+    if (cost < least) {
+      least = cost;
+      best = parts;
+    }
+  }
+  return best;
 }
 
 }  // namespace

@@ -5,6 +5,7 @@
 // down_c = sum_g min(q_gc, 0), ranks pages without reading their keys.  It is summed in 64 bits and rounded to 32 once: the order of the
 // pages then does not depend on the order of the sum.
 #include <algorithm>
+#include <type_traits>
 
 #include "fc_common.h"
 #include "paged.h"
@@ -16,7 +17,8 @@ namespace {
 constexpr int kBoundThreads = 256, kBoundWaves = kBoundThreads / 64;
 constexpr int kRowsAtOnce = 4;         // of a lane
 constexpr int kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
-constexpr int kChooseThreads = 256;
+constexpr int kPagesAtOnce = 4, kQueriesAtOnce = 8;
+constexpr int kMostKeys = 4096;        // that a workgroup has in LDS, or in registers
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -112,102 +114,224 @@ __device__ __forceinline__ uint32_t key_of(float score) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// grid = (parts of a unit's pages, units)
-template <typename T, int D>
-__global__ __launch_bounds__(kScoreThreads) void page_score_kernel(PagedArgs a, const T* __restrict__ Q, int G, const T* __restrict__ bounds, int first, int last,
-                                                                   uint32_t* __restrict__ keys) {
-  typedef Columns<T> C;
-  constexpr int N = C::kCount, kLanes = D / N, kAbreast = 64 / kLanes;
-  const int u = blockIdx.y, b = u / (a.L * a.H), in = u - b * a.L * a.H;
-  const int lane = threadIdx.x & 63, mine = lane / kLanes, part = lane % kLanes;
-  const int blocks = pages_of(a, b, in / a.H);
-  double up[N], down[N];
+__device__ __forceinline__ double add_lanes_16(double v) { // the sum over each 16 lanes, in all of them
+  auto moved = [](double x, auto ctrl) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, decltype(ctrl)::value, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), decltype(ctrl)::value, 0xF, 0xF, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  v += moved(v, std::integral_constant<int, 0xB1>{});      // quad_perm: the neighbour, then the other pair
+  v += moved(v, std::integral_constant<int, 0x4E>{});
+  v += moved(v, std::integral_constant<int, 0x141>{});     // row_half_mirror, row_mirror
+  return v + moved(v, std::integral_constant<int, 0x140>{});
+}
+
+// A lane's 16 bytes of what a unit's queries make of each column: up = (sum + sum of magnitudes) / 2, down = (sum - sum of magnitudes) / 2.  A thread sums
+// up a column, all find theirs in LDS; the caller has a barrier between both.
+template <typename T, int D> __device__ __forceinline__ void sum_queries(const T* q, int G, double (*sums)[D], int thread) {
+  if (thread >= D) return;
+  double sum = 0.0, size = 0.0;
+  for (int g0 = 0; g0 < G; g0 += kQueriesAtOnce) {
+    T v[kQueriesAtOnce];
 #pragma unroll
-  for (int i = 0; i < N; ++i) up[i] = down[i] = 0.0;
-  for (int g = 0; g < G; ++g) {
-    float x[N];
-    C::get(*reinterpret_cast<const u32x4*>(Q + ((int64_t)u * G + g) * D + part * N), x);
+    for (int j = 0; j < kQueriesAtOnce; ++j) v[j] = q[(int64_t)min(g0 + j, G - 1) * D + thread];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      up[i] += x[i] > 0.f ? (double)x[i] : x[i] < 0.f ? 0.0 : (double)x[i];       // (what is not a number is in both)
-      down[i] += x[i] < 0.f ? (double)x[i] : x[i] > 0.f ? 0.0 : (double)x[i];
+    for (int j = 0; j < kQueriesAtOnce; ++j) {
+      float x;
+      if constexpr (sizeof(T) == 2) x = bf16_to_f32(v[j]);
+      else x = v[j];
+      if (g0 + j < G) {
+        sum += (double)x;
+        size += fabs((double)x);
+      }
     }
   }
-  const int waves = gridDim.x * kScoreWaves, wave = blockIdx.x * kScoreWaves + (threadIdx.x >> 6);
-  const int32_t* const table = a.table + b * a.table_b + (int64_t)in * a.max_pages;
-  for (int p0 = wave * kAbreast; p0 < blocks; p0 += waves * kAbreast) {
-    const int p = p0 + mine;
-    const int page = p < blocks ? table[p] : -1;
-    const bool there = page >= 0 && page < a.num_pages;
-    const T* const from = bounds + (int64_t)(there ? page : 0) * 2 * D + part * N;
-    float low[N], high[N];
-    C::get(*reinterpret_cast<const u32x4*>(from), low);
-    C::get(*reinterpret_cast<const u32x4*>(from + D), high);
-    double s = 0.0;
+  sums[0][thread] = 0.5 * (sum + size);
+  sums[1][thread] = 0.5 * (sum - size);
+}
+
+// Keys of pages first, first + stride, ... (a wave's; kAbreast side by side, kPagesAtOnce of a lane group under way together), of a unit's `blocks`.
+template <typename T, int D, typename Put>
+__device__ __forceinline__ void score_pages(const PagedArgs& a, const int32_t* table, const T* bounds, const double (*sums)[D], int begin, int stride, int blocks,
+                                            int first, int last, int lane, const Put& put) {
+  typedef Columns<T> C;
+  constexpr int N = C::kCount, kLanes = D / N, kAbreast = 64 / kLanes;
+  const int mine = lane / kLanes, part = lane % kLanes;
+  int page[kPagesAtOnce];
+  auto look_up = [&](int p0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) s = fma((double)low[i], down[i], fma((double)high[i], up[i], s));
+    for (int j = 0; j < kPagesAtOnce; ++j) page[j] = table[min(p0 + j * kAbreast + mine, a.max_pages - 1)];
+  };
+  u32x4 low[kPagesAtOnce], high[kPagesAtOnce];
+  bool there[kPagesAtOnce];
+  auto request = [&](int p0) {
 #pragma unroll
-    for (int d = kLanes / 2; d; d >>= 1) s += __shfl_xor(s, d, 64);
-    if (part == 0 && p < blocks)
-      keys[(int64_t)u * a.max_pages + p] = !there ? 0u : (p < first || p >= blocks - last) ? 0xFFFFFFFFu : key_of((float)s);
+    for (int j = 0; j < kPagesAtOnce; ++j) {
+      there[j] = p0 + j * kAbreast + mine < blocks && page[j] >= 0 && page[j] < a.num_pages;
+      const T* const from = bounds + (int64_t)(there[j] ? page[j] : 0) * 2 * D + part * N;
+      low[j] = *reinterpret_cast<const u32x4*>(from);
+      high[j] = *reinterpret_cast<const u32x4*>(from + D);
+    }
+  };
+  look_up(begin);
+  if (begin < blocks) request(begin);
+  __syncthreads();                                         // (the sums are there)
+  double up[N], down[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    up[i] = sums[0][part * N + i];
+    down[i] = sums[1][part * N + i];
+  }
+  for (int p0 = begin; p0 < blocks; p0 += stride) {
+    const bool more = p0 + stride < blocks;
+    if (more) look_up(p0 + stride);
+    double s[kPagesAtOnce];
+    bool had[kPagesAtOnce];
+#pragma unroll
+    for (int j = 0; j < kPagesAtOnce; ++j) {
+      float x[N], y[N];
+      C::get(low[j], x);
+      C::get(high[j], y);
+      had[j] = there[j];
+      s[j] = 0.0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[j] = fma((double)x[i], down[i], fma((double)y[i], up[i], s[j]));
+    }
+    if (more) request(p0 + stride);
+#pragma unroll
+    for (int j = 0; j < kPagesAtOnce; ++j) {
+      if constexpr (kLanes == 8) {
+#pragma unroll
+        for (int d = 4; d; d >>= 1) s[j] += __shfl_xor(s[j], d, 64);
+      } else {
+        s[j] = add_lanes_16(s[j]);
+        if (kLanes == 32) s[j] += __shfl_xor(s[j], 16, 64);
+      }
+      const int p = p0 + j * kAbreast + mine;
+      if (part == 0 && p < blocks) put(p, !had[j] ? 0u : (p < first || p >= blocks - last) ? 0xFFFFFFFFu : key_of((float)s[j]));
+    }
   }
 }
 
-// The `count` largest keys of a unit, of equal ones the first, in the order of the table.  A workgroup per unit: the smallest key that is
-// taken is found bit by bit.
-__global__ __launch_bounds__(kChooseThreads) void choose_kernel(PagedArgs a, const uint32_t* __restrict__ keys, int count, int32_t* __restrict__ chosen) {
-  constexpr int kWaves = kChooseThreads / 64;
-  __shared__ int counts[2][kWaves], above_of[kWaves], equal_of[kWaves];
-  const int u = blockIdx.x, b = u / (a.L * a.H), in = u - b * a.L * a.H, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// grid = (parts of a unit's pages, units): few units, or more pages than choose_whole_kernel has room for
+template <typename T, int D>
+__global__ __launch_bounds__(kScoreThreads) void page_score_kernel(PagedArgs a, const T* __restrict__ Q, int G, const T* __restrict__ bounds, int first, int last,
+                                                                   uint32_t* __restrict__ keys) {
+  constexpr int kAtATime = 64 / (D / Columns<T>::kCount) * kPagesAtOnce;
+  __shared__ double sums[2][D];
+  const int u = blockIdx.y, b = u / (a.L * a.H), in = u - b * a.L * a.H;
+  const int waves = gridDim.x * kScoreWaves, wave = blockIdx.x * kScoreWaves + (threadIdx.x >> 6);
   const int blocks = pages_of(a, b, in / a.H);
-  const uint32_t* const key = keys + (int64_t)u * a.max_pages;
-  int turn = 0;
-  auto at_least = [&](uint32_t least) {
-    int n = 0;
-    for (int p = tid; p < blocks; p += kChooseThreads) n += key[p] >= least ? 1 : 0;
+  if ((int)blockIdx.x * kScoreWaves * kAtATime >= blocks) return;
+  sum_queries<T, D>(Q + (int64_t)u * G * D, G, sums, threadIdx.x);
+  score_pages<T, D>(a, a.table + b * a.table_b + (int64_t)in * a.max_pages, bounds, sums, wave * kAtATime, waves * kAtATime, blocks, first, last,
+                    threadIdx.x & 63, [&](int p, uint32_t key) { keys[(int64_t)u * a.max_pages + p] = key; });
+}
+
+// The `count` largest keys of a unit, of equal ones the first, in the order of the table, by WAVES waves (thread `tid` of them).  The smallest key that
+// is taken is found bit by bit, by ballots.  A lane has up to K keys in registers, and where there are more reads all of them again for each bit.
+template <int K, int WAVES, typename Get>
+__device__ __forceinline__ void choose_largest(int blocks, int count, int tid, const Get& get, int32_t* __restrict__ out) {
+  constexpr int kThreads = 64 * WAVES, kHeld = K * kThreads;
+  __shared__ int counts[2][WAVES], both[2][WAVES];
+  const int lane = tid & 63, wave = tid >> 6;
+  uint32_t held[K];
+  auto load = [&](int base) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d, 64);
+    for (int j = 0; j < K; ++j) held[j] = get(min(base + j * kThreads + tid, max(blocks - 1, 0)));
+#pragma unroll
+    for (int j = 0; j < K; ++j) held[j] = base + j * kThreads + tid < blocks ? held[j] : 0u;
+  };
+  load(0);
+  const bool whole = blocks <= kHeld;
+  int turn = 0;
+  auto over_waves = [&](int n) {
+    if constexpr (WAVES == 1) return n;
     if (lane == 0) counts[turn][wave] = n;
     __syncthreads();
     n = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) n += counts[turn][w];
+    for (int w = 0; w < WAVES; ++w) n += counts[turn][w];
     turn ^= 1;
     return n;
   };
-  const int want = min(count, at_least(1u));
-  uint32_t least = 1u;
-  int with_least = 0;
-  if (want > 0) {
-    uint32_t found = 0;
-    for (int bit = 31; bit >= 0; --bit)
-      if (at_least(found | 1u << bit) >= want) found |= 1u << bit;
-    least = found;
-    with_least = want - (found == 0xFFFFFFFFu ? 0 : at_least(found + 1u));       // of those that are equal to it
-  }
-  int32_t* const out = chosen + (int64_t)u * count;
-  int taken = 0, equal = 0;
-  for (int p0 = 0; p0 < blocks && want > 0; p0 += kChooseThreads) {
-    const int p = p0 + tid;
-    const uint32_t k = p < blocks ? key[p] : 0u;
-    const uint64_t eq = __ballot(k == least && p < blocks), gt = __ballot(k > least);
-    if (lane == 0) { equal_of[wave] = __popcll(eq); above_of[wave] = __popcll(gt); }
-    __syncthreads();
-    const uint64_t before = (1ull << lane) - 1ull;
-    int eq_before = equal + __popcll(eq & before), gt_before = taken - min(equal, with_least) + __popcll(gt & before);
-    int eq_all = 0, gt_all = 0;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) { eq_before += equal_of[w]; gt_before += above_of[w]; }
-      eq_all += equal_of[w];
-      gt_all += above_of[w];
+  auto at_least = [&](uint32_t least) {                    // (least > 0)
+    int n = 0;
+    for (int base = 0; base < blocks; base += kHeld) {
+      if (!whole) load(base);
+#pragma unroll
+      for (int j = 0; j < K; ++j) n += __popcll(__ballot(held[j] >= least));
     }
-    const bool mine = k > least || (k == least && p < blocks && eq_before < with_least);
-    if (mine) out[gt_before + min(eq_before, with_least)] = p;
-    taken += gt_all + min(equal + eq_all, with_least) - min(equal, with_least);
-    equal += eq_all;
-    __syncthreads();
+    return over_waves(n);
+  };
+  const int want = min(count, at_least(1u));
+  uint32_t least = 0u;
+  int with_least = 0;                                      // how many of those that are equal to it
+  if (want > 0) {
+    for (int bit = 31; bit >= 0; --bit)
+      if (at_least(least | 1u << bit) >= want) least |= 1u << bit;
+    with_least = want - (least == 0xFFFFFFFFu ? 0 : at_least(least + 1u));
   }
-  for (int i = want + tid; i < count; i += kChooseThreads) out[i] = -1;
+  int above = 0, equal = 0;                                // before this place
+  if constexpr (WAVES > 1) __syncthreads();                // (all have read the last count)
+  if (want > 0)
+    for (int base = 0; base < blocks; base += kHeld) {
+      if (!whole) load(base);
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        const uint64_t gt = __ballot(held[j] > least), eq = __ballot(held[j] == least), before = (1ull << lane) - 1ull;
+        int gt_before = above + __popcll(gt & before), eq_before = equal + __popcll(eq & before);
+        if constexpr (WAVES == 1) {
+          above += __popcll(gt);
+          equal += __popcll(eq);
+        } else {
+          if (lane == 0) { counts[j & 1][wave] = __popcll(gt); both[j & 1][wave] = __popcll(eq); }
+          __syncthreads();
+#pragma unroll
+          for (int w = 0; w < WAVES; ++w) {
+            const int g = counts[j & 1][w], e = both[j & 1][w];
+            if (w < wave) { gt_before += g; eq_before += e; }
+            above += g;
+            equal += e;
+          }
+        }
+        if (held[j] > least || (held[j] == least && eq_before < with_least)) out[gt_before + min(eq_before, with_least)] = base + j * kThreads + tid;
+      }
+    }
+  for (int i = want + tid; i < count; i += kThreads) out[i] = -1;
+}
+
+// ... by a wave alone where it has registers for all keys: a barrier for each bit costs more than the others' help.
+template <int WAVES, typename Get>
+__device__ __forceinline__ void choose_by(int blocks, int count, const Get& get, int32_t* out) {
+  if (blocks <= 8 * 64) {
+    if (threadIdx.x < 64) choose_largest<8, 1>(blocks, count, threadIdx.x, get, out);
+  } else {
+    choose_largest<kMostKeys / (64 * WAVES), WAVES>(blocks, count, threadIdx.x, get, out);
+  }
+}
+
+__global__ __launch_bounds__(1024) void choose_kernel(PagedArgs a, const uint32_t* __restrict__ keys, int count, int32_t* __restrict__ chosen) {
+  const int u = blockIdx.x, b = u / (a.L * a.H), in = u - b * a.L * a.H;
+  const uint32_t* const key = keys + (int64_t)u * a.max_pages;
+  choose_by<16>(pages_of(a, b, in / a.H), count, [&](int p) { return key[p]; }, chosen + (int64_t)u * count);
+}
+
+// Both in one: a workgroup a unit, keys in LDS.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void choose_whole_kernel(PagedArgs a, const T* __restrict__ Q, int G, const T* __restrict__ bounds, int count, int first,
+                                                                  int last, int32_t* __restrict__ chosen) {
+  constexpr int kAtATime = 64 / (D / Columns<T>::kCount) * kPagesAtOnce;
+  __shared__ double sums[2][D];
+  extern __shared__ uint32_t keys[];
+  const int u = blockIdx.x, b = u / (a.L * a.H), in = u - b * a.L * a.H, wave = threadIdx.x >> 6;
+  const int blocks = pages_of(a, b, in / a.H);
+  sum_queries<T, D>(Q + (int64_t)u * G * D, G, sums, threadIdx.x);
+  score_pages<T, D>(a, a.table + b * a.table_b + (int64_t)in * a.max_pages, bounds, sums, wave * kAtATime, WAVES * kAtATime, blocks, first, last,
+                    threadIdx.x & 63, [&](int p, uint32_t key) { keys[p] = key; });
+  __syncthreads();
+  choose_by<WAVES>(blocks, count, [&](int p) { return keys[p]; }, chosen + (int64_t)u * count);
 }
 
 }  // namespace
@@ -230,21 +354,37 @@ hipError_t choose_launch(const void* Q, int group, const fc_paged_kv& kv, const 
   const PagedArgs a = paged_args(kv);
   const int units = a.B * a.L * a.H;
   uint32_t* const keys = static_cast<uint32_t*>(ws);
+  auto by_type = [&](auto launch) {
+    if (kv.dtype == FC_BF16) kv.head_dim == 128 ? launch(uint16_t{}, std::integral_constant<int, 128>{}) : launch(uint16_t{}, std::integral_constant<int, 64>{});
+    else kv.head_dim == 128 ? launch(float{}, std::integral_constant<int, 128>{}) : launch(float{}, std::integral_constant<int, 64>{});
+  };
+  if (a.max_pages <= kMostKeys && units >= 64) {
+    ProfileScope ps("choose_whole_kernel", s);
+    by_type([&](auto type, auto dim) {
+      typedef decltype(type) T;
+      constexpr int D = decltype(dim)::value;
+      auto launch = [&](auto kern, int waves) {
+        hipLaunchKernelGGL(kern, dim3(units), dim3(64 * waves), a.max_pages * sizeof(uint32_t), s, a, static_cast<const T*>(Q), group, static_cast<const T*>(bounds),
+                           count, first, last, chosen);
+      };
+      units <= 256 ? launch(choose_whole_kernel<T, D, 16>, 16) : launch(choose_whole_kernel<T, D, 4>, 4);
+    });
+    return hipGetLastError();
+  }
   {
     ProfileScope ps("page_score_kernel", s);
-    const int abreast = 64 / (kv.head_dim / (kv.dtype == FC_BF16 ? 8 : 4)) * kScoreWaves;
-    const unsigned parts = (unsigned)std::max(1, std::min((a.max_pages + abreast - 1) / abreast, (2048 + units - 1) / units));
-    auto launch = [&](auto kern, auto type) {
+    const int at_a_time = 64 / (kv.head_dim / (kv.dtype == FC_BF16 ? 8 : 4)) * kPagesAtOnce * kScoreWaves;
+    const unsigned parts = (unsigned)std::max(1, std::min((a.max_pages + at_a_time - 1) / at_a_time, (4096 + units - 1) / units));
+    by_type([&](auto type, auto dim) {
       typedef decltype(type) T;
-      hipLaunchKernelGGL(kern, dim3(parts, units), dim3(kScoreThreads), 0, s, a, static_cast<const T*>(Q), group, static_cast<const T*>(bounds), first, last, keys);
-    };
-    if (kv.dtype == FC_BF16) kv.head_dim == 128 ? launch(page_score_kernel<uint16_t, 128>, uint16_t{}) : launch(page_score_kernel<uint16_t, 64>, uint16_t{});
-    else kv.head_dim == 128 ? launch(page_score_kernel<float, 128>, float{}) : launch(page_score_kernel<float, 64>, float{});
+      hipLaunchKernelGGL((page_score_kernel<T, decltype(dim)::value>), dim3(parts, units), dim3(kScoreThreads), 0, s, a, static_cast<const T*>(Q), group,
+                         static_cast<const T*>(bounds), first, last, keys);
+    });
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ProfileScope ps("choose_kernel", s);
-  hipLaunchKernelGGL(choose_kernel, dim3(units), dim3(kChooseThreads), 0, s, a, static_cast<const uint32_t*>(keys), count, chosen);
+  hipLaunchKernelGGL(choose_kernel, dim3(units), dim3(1024), 0, s, a, static_cast<const uint32_t*>(keys), count, chosen);
   return hipGetLastError();
 }
 

@@ -10,6 +10,19 @@ namespace {
 
 constexpr int kMostPagedRows = (1 << 25) - 1;
 
+// Quotients of numbers below 2^31: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, m d is above 2^(31 + l) by d <= 2^l at most, so that
+// n m / 2^(31 + l) is n / d and less than 2^-31 n / d * 2^l / 2^l beyond: the same whole part.  m has 32 bits for d > 1.
+struct Divider {
+  uint32_t m;
+  int shift;                     // l - 1; negative: d is 1
+  __device__ __forceinline__ int of(int n) const { return shift < 0 ? n : (int)(__umulhi((uint32_t)n, m) >> shift); }
+};
+inline Divider divider(int d) {
+  if (d == 1) return {0u, -1};
+  const int l = 32 - __builtin_clz((unsigned)(d - 1));
+  return {(uint32_t)((1ull << (31 + l)) / (unsigned)d + 1), l - 1};
+}
+
 struct PagedArgs {
   const void* K;
   const void* V;
@@ -17,11 +30,12 @@ struct PagedArgs {
   const int32_t* table;          // [B][L][H][max_pages], table_b between sequences
   int64_t rows_b, table_b, num_pages;
   int B, L, H, page_size, max_pages;
+  Divider pages;                 // by the page's size
 };
 
 inline PagedArgs paged_args(const fc_paged_kv& kv) {
   return PagedArgs{kv.K, kv.V, kv.rows, kv.block_table, kv.rows_stride_b, kv.table_stride_b, kv.num_pages,
-                   kv.batch, kv.layers, kv.kv_heads, kv.page_size, kv.max_pages};
+                   kv.batch, kv.layers, kv.kv_heads, kv.page_size, kv.max_pages, divider(kv.page_size)};
 }
 
 // Rows of a layer that its table can reach.

@@ -319,6 +319,22 @@ def test_choose_pages(dtype, rows, H, G, d, ps, count, first, last, lost):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("dtype,B,L,H,G,d,ps,most,count,first,last,lost", [
+    ("bf16", 5, 7, 2, 7, 128, 16, 500, 9, 1, 2, 0.1), ("f32", 3, 11, 2, 3, 64, 16, 2000, 70, 0, 0, 0.1), ("bf16", 10, 14, 2, 1, 64, 16, 400, 12, 2, 0, 0.3),
+    ("f32", 13, 10, 2, 4, 128, 32, 900, 5, 0, 1, 0.0), ("bf16", 4, 8, 2, 2, 64, 4, 3000, 513, 5, 5, 0.0), ("bf16", 9, 15, 2, 2, 64, 4, 3000, 100, 0, 3, 0.0),
+])
+def test_choose_pages_of_many_units(dtype, B, L, H, G, d, ps, most, count, first, last, lost):
+    fc = _fc()
+    rng = np.random.default_rng(most + count)
+    rows = rng.integers(0, most + 1, (B, L))
+    rows[0, :3] = 0, 1, most
+    c = Cache(rng, rows, H, d, ps, dtype, lost=lost)
+    bounds = fc.page_bounds(c.kv)
+    Q = _rand(rng, (B, L, G * H, d), _dt(dtype))
+    got = fc.choose_pages(Q, c.kv, bounds, count, first=first, last=last)
+    assert np.array_equal(got.cpu().numpy(), pr.choose_pages(_f64(Q), _f64(bounds), rows, c.table_np, ps, count, first, last))
+
+
 def test_choice_between_equal_scores_and_without_numbers():
     fc = _fc()
     rng = np.random.default_rng(2)
