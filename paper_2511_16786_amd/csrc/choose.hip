@@ -152,17 +152,21 @@ template <typename T, int D> __device__ __forceinline__ void sum_queries(const T
 }
 
 // Keys of pages first, first + stride, ... (a wave's; kAbreast side by side, kPagesAtOnce of a lane group under way together), of a unit's `blocks`.
+// The queries (at q) are summed up behind the first requests.
 template <typename T, int D, typename Put>
-__device__ __forceinline__ void score_pages(const PagedArgs& a, const int32_t* table, const T* bounds, const double (*sums)[D], int begin, int stride, int blocks,
-                                            int first, int last, int lane, const Put& put) {
+__device__ __forceinline__ int score_pages(const PagedArgs& a, int b, int in, const T* bounds, const T* q, int G, double (*sums)[D], int begin, int stride,
+                                           int first, int last, int lane, const Put& put) {
   typedef Columns<T> C;
   constexpr int N = C::kCount, kLanes = D / N, kAbreast = 64 / kLanes;
   const int mine = lane / kLanes, part = lane % kLanes;
+  const int32_t* const table = a.table + b * a.table_b + (int64_t)in * a.max_pages;
   int page[kPagesAtOnce];
   auto look_up = [&](int p0) {
 #pragma unroll
     for (int j = 0; j < kPagesAtOnce; ++j) page[j] = table[min(p0 + j * kAbreast + mine, a.max_pages - 1)];
   };
+  look_up(begin);
+  const int blocks = pages_of(a, b, in / a.H);
   u32x4 low[kPagesAtOnce], high[kPagesAtOnce];
   bool there[kPagesAtOnce];
   auto request = [&](int p0) {
@@ -174,9 +178,9 @@ __device__ __forceinline__ void score_pages(const PagedArgs& a, const int32_t* t
       high[j] = *reinterpret_cast<const u32x4*>(from + D);
     }
   };
-  look_up(begin);
   if (begin < blocks) request(begin);
-  __syncthreads();                                         // (the sums are there)
+  sum_queries<T, D>(q, G, sums, threadIdx.x);
+  __syncthreads();
   double up[N], down[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -212,6 +216,7 @@ __device__ __forceinline__ void score_pages(const PagedArgs& a, const int32_t* t
       if (part == 0 && p < blocks) put(p, !had[j] ? 0u : (p < first || p >= blocks - last) ? 0xFFFFFFFFu : key_of((float)s[j]));
     }
   }
+  return blocks;
 }
 
 // grid = (parts of a unit's pages, units): few units, or more pages than choose_whole_kernel has room for
@@ -222,11 +227,7 @@ __global__ __launch_bounds__(kScoreThreads) void page_score_kernel(PagedArgs a, 
   __shared__ double sums[2][D];
   const int u = blockIdx.y, b = u / (a.L * a.H), in = u - b * a.L * a.H;
   const int waves = gridDim.x * kScoreWaves, wave = blockIdx.x * kScoreWaves + (threadIdx.x >> 6);
-  const int blocks = pages_of(a, b, in / a.H);
-  if ((int)blockIdx.x * kScoreWaves * kAtATime >= blocks) return;
-  sum_queries<T, D>(Q + (int64_t)u * G * D, G, sums, threadIdx.x);
-  score_pages<T, D>(a, a.table + b * a.table_b + (int64_t)in * a.max_pages, bounds, sums, wave * kAtATime, waves * kAtATime, blocks, first, last,
-                    threadIdx.x & 63, [&](int p, uint32_t key) { keys[(int64_t)u * a.max_pages + p] = key; });
+  score_pages<T, D>(a, b, in, bounds, Q + (int64_t)u * G * D, G, sums, wave * kAtATime, waves * kAtATime, first, last, threadIdx.x & 63, [&](int p, uint32_t key) { keys[(int64_t)u * a.max_pages + p] = key; });
 }
 
 // The `count` largest keys of a unit, of equal ones the first, in the order of the table, by WAVES waves (thread `tid` of them).  The smallest key that
@@ -306,7 +307,10 @@ __device__ __forceinline__ void choose_largest(int blocks, int count, int tid, c
 template <int WAVES, typename Get>
 __device__ __forceinline__ void choose_by(int blocks, int count, const Get& get, int32_t* out) {
   if (blocks <= 8 * 64) {
-    if (threadIdx.x < 64) choose_largest<8, 1>(blocks, count, threadIdx.x, get, out);
+    if (threadIdx.x >= 64) return;
+    if (blocks <= 2 * 64) choose_largest<2, 1>(blocks, count, threadIdx.x, get, out);
+    else if (blocks <= 4 * 64) choose_largest<4, 1>(blocks, count, threadIdx.x, get, out);
+    else choose_largest<8, 1>(blocks, count, threadIdx.x, get, out);
   } else {
     choose_largest<kMostKeys / (64 * WAVES), WAVES>(blocks, count, threadIdx.x, get, out);
   }
@@ -326,10 +330,8 @@ __global__ __launch_bounds__(64 * WAVES) void choose_whole_kernel(PagedArgs a, c
   __shared__ double sums[2][D];
   extern __shared__ uint32_t keys[];
   const int u = blockIdx.x, b = u / (a.L * a.H), in = u - b * a.L * a.H, wave = threadIdx.x >> 6;
-  const int blocks = pages_of(a, b, in / a.H);
-  sum_queries<T, D>(Q + (int64_t)u * G * D, G, sums, threadIdx.x);
-  score_pages<T, D>(a, a.table + b * a.table_b + (int64_t)in * a.max_pages, bounds, sums, wave * kAtATime, WAVES * kAtATime, blocks, first, last,
-                    threadIdx.x & 63, [&](int p, uint32_t key) { keys[p] = key; });
+  const int blocks = score_pages<T, D>(a, b, in, bounds, Q + (int64_t)u * G * D, G, sums, wave * kAtATime, WAVES * kAtATime, first, last, threadIdx.x & 63,
+                                       [&](int p, uint32_t key) { keys[p] = key; });
   __syncthreads();
   choose_by<WAVES>(blocks, count, [&](int p) { return keys[p]; }, chosen + (int64_t)u * count);
 }
