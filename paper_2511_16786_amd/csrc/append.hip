@@ -17,7 +17,7 @@ namespace fc {
 namespace {
 
 constexpr int kAppThreads = 256, kAppWaves = kAppThreads / 64;
-constexpr int kHeadsAtOnce = 4, kMostPairs = 4, kMostAbreast = 8, kMostTurns = 8;
+constexpr int kHeadsAtOnce = 5, kMostPairs = 4, kMostAbreast = 8, kMostTurns = 8;
 constexpr int kTokensAtOnce = 4;       // of a lane, with bounds
 
 struct NewRows {                 // strides in bytes
@@ -44,6 +44,7 @@ struct AppendArgs {
   int per_group;                 // tokens of a workgroup
   uint32_t chunks_inverse, abreast_inverse;
   int abreast, turns, across;    // heads of a token side by side; how many of them a thread has; workgroups side by side
+  int at_once;                   // of the turns, under way together
   int turning;                   // heads of the first part that are turned; the keys among them unless there are bounds
   // keys with bounds
   int stretches, stretch;        // of a head; tokens of one
@@ -51,6 +52,13 @@ struct AppendArgs {
   int streams, end0, end1, end2; // first pair behind the first, second and third stream
   float magnitude;
 };
+
+__device__ __forceinline__ float as_float(uint16_t x) { return bf16_to_f32(x); }
+__device__ __forceinline__ float as_float(float x) { return x; }
+template <typename T> __device__ __forceinline__ T as_type(float x) {      // (of a value that the type has)
+  if constexpr (sizeof(T) == 2) return (T)(__float_as_uint(x) >> 16);
+  else return x;
+}
 
 template <int P> __device__ __forceinline__ void sines_of(const AppendArgs& a, const fc_rotary_plan& plan, int row, int first, float (&sn)[P], float (&cs)[P]) {
   int32_t where[P];
@@ -116,23 +124,21 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const fc_rotary
   const bool turned = chunk < a.turned && h0 + beside < a.turning;
   float sn[P], cs[P];
   if (turned) sines_of<P>(a, plan, row, chunk * P, sn, cs);
-  for (int hw = h0; hw < h1; hw += kHeadsAtOnce * a.abreast) {
+  for (int hw = h0; hw < h1; hw += a.at_once * a.abreast) {
     Vec<T, kPiece> v[kHeadsAtOnce][kPieces];
-    char* out[kHeadsAtOnce];
+    int64_t slot[kHeadsAtOnce];
 #pragma unroll
     for (int i = 0; i < kHeadsAtOnce; ++i) {
       const int h = hw + i * a.abreast + beside;
-      if (h >= h1) break;
+      if (i >= a.at_once || h >= h1) break;
       const char* in;
       if (h < a.q.heads) {
         in = a.q.in + b * a.q.sb + t * a.q.st + h * a.q.sh;
-        out[i] = a.q_out + b * a.ob + t * a.ot + h * a.oh;
       } else {
         const bool key = h < a.turning;
         const int kv = h - (key ? a.q.heads : a.turning);
-        const int64_t slot = a.slots[b * a.slots_b + kv * a.slots_h + t];
+        slot[i] = a.slots[b * a.slots_b + kv * a.slots_h + t];
         in = key ? a.k.in + b * a.k.sb + t * a.k.st + kv * a.k.sh : a.v.in + b * a.v.sb + t * a.v.st + kv * a.v.sh;
-        out[i] = slot >= 0 && slot < a.num_slots ? (key ? a.k_pages : a.v_pages) + slot * a.row_bytes : nullptr;
       }
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) v[i][j] = get<PAST, T, kPiece>(in + at + j * apart);
@@ -140,76 +146,110 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const fc_rotary
 #pragma unroll
     for (int i = 0; i < kHeadsAtOnce; ++i) {
       const int h = hw + i * a.abreast + beside;
-      if (h >= h1) break;
+      if (i >= a.at_once || h >= h1) break;
       if (turned && h < a.turning) turn<T, P, INTERLEAVED>(v[i], sn, cs);
-      if (!out[i]) continue;
+      char* out;
+      if (h < a.q.heads) {
+        out = a.q_out + b * a.ob + t * a.ot + h * a.oh;
+      } else {
+        if (slot[i] < 0 || slot[i] >= a.num_slots) continue;
+        out = (h < a.turning ? a.k_pages : a.v_pages) + slot[i] * a.row_bytes;
+      }
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) put<PAST>(out[i] + at + j * apart, v[i][j]);
+      for (int j = 0; j < kPieces; ++j) put<PAST>(out + at + j * apart, v[i][j]);
     }
   }
 }
 
-// A stretch of a KV head's tokens: the runs of tokens with a page in common that begin in it, up to their ends.
-template <typename T, int P, bool INTERLEAVED>
-__device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary_plan& plan, int group) {
-  constexpr int kPieces = INTERLEAVED ? 1 : 2, kPiece = 2 * P / kPieces;
-  const int lane = threadIdx.x & 63, item = __builtin_amdgcn_readfirstlane(group * kAppWaves + (int)(threadIdx.x >> 6));
+// A stretch of a KV head's tokens: the runs of tokens with a page in common that begin in it, up to their ends.  ALONE: a wave has it (a single token),
+// else the workgroup, whose lane groups' results meet in LDS.
+template <typename T, int P, bool INTERLEAVED, bool ALONE>
+__device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary_plan& plan, int group, float* lds) {
+  constexpr int kPieces = INTERLEAVED ? 1 : 2, kPiece = 2 * P / kPieces, kCols = 2 * P;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = ALONE ? group * kAppWaves + wave : group;
   const int head = item / a.stretches, b = head / a.k.heads, h = head - b * a.k.heads;
   if (b * a.tokens >= a.rows) return;
   const int t0 = (item - head * a.stretches) * a.stretch, t1 = min(a.tokens, t0 + a.stretch);
   const int64_t* const slots = a.slots + b * a.slots_b + h * a.slots_h;
   const char* const in = a.k.in + b * a.k.sb + h * a.k.sh;
-  const int lanes = min(64, a.chunks), rows_abreast = 64 / lanes, mine = lane / lanes;
+  const int lanes = min(64, a.chunks), of_wave = 64 / lanes, abreast = ALONE ? of_wave : kAppWaves * of_wave;
+  const int in_wave = lane / lanes, mine = ALONE ? in_wave : wave * of_wave + in_wave;       // lane group: tokens mine, mine + abreast, ... of a look-up
   // the page of a token, -1 without one
-  auto page_of = [&](int64_t slot) -> int64_t { return slot >= 0 && slot < a.num_slots ? (int64_t)((uint32_t)slot / (uint32_t)a.page_size) : -1; };
+  auto page_of = [&](int64_t slot) { return slot >= 0 && slot < a.num_slots ? (int)((uint32_t)slot / (uint32_t)a.page_size) : -1; };
   for (int first = 0; first < a.chunks; first += lanes) {  // (one turn: a head's chunks but those of narrow pieces fit a wave)
-    const int chunk = first + lane - mine * lanes;
-    const bool has = mine < rows_abreast && chunk < a.chunks;
+    const int chunk = first + lane - in_wave * lanes;
+    const bool has = in_wave < of_wave && chunk < a.chunks;
     int at, apart;
     place_of_chunk<T, P, kPiece>(a, has ? chunk : 0, at, apart);
     float low[kPieces][kPiece], high[kPieces][kPiece];
-    int64_t run = t0 > 0 ? page_of(slots[t0 - 1]) : -1;    // page that the tokens before have
-    bool open = false, begun = false;                      // whether the run is this wave's; whether it has the page's first row
+    int run = t0 > 0 ? page_of(slots[t0 - 1]) : -1;        // page that the tokens before have
+    bool open = false, begun = false;                      // whether the run is this one's; whether it has the page's first row
+    // what the page's bounds are, with those of before
+    auto write = [&](char* to, float l, float g, int which, int c) {
+      T* const low_at = reinterpret_cast<T*>(to) + c;
+      if (which == 0) {
+        if (!begun) l = fminf(l, as_float(*low_at));
+        *low_at = as_type<T>(l);
+      } else {
+        T* const high_at = reinterpret_cast<T*>(to + a.row_bytes) + c;
+        if (!begun) g = fmaxf(g, as_float(*high_at));
+        *high_at = as_type<T>(g);
+      }
+    };
     auto flush = [&]() {
       if (!open) return;
-      // rows side by side, one after another: the order does not matter to least and largest
-      for (int r = 1; r < rows_abreast; ++r) {
+      open = false;
+      char* const to = a.bounds + 2 * (int64_t)run * a.row_bytes;
+      if constexpr (ALONE) {                               // (a token: the first lane group has it)
+        if (has && mine == 0)
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j)
+          for (int j = 0; j < kPieces; ++j) {
+            if (!begun) {
+              float l[kPiece], g[kPiece];
+              widen<T, kPiece>(get<false, T, kPiece>(to + at + j * apart), l);
+              widen<T, kPiece>(get<false, T, kPiece>(to + a.row_bytes + at + j * apart), g);
 #pragma unroll
-          for (int c = 0; c < kPiece; ++c) {
-            const float l = __shfl(low[j][c], (lane + r * lanes) & 63, 64), g = __shfl(high[j][c], (lane + r * lanes) & 63, 64);
-            if (mine == 0) {
-              low[j][c] = fminf(low[j][c], l);
-              high[j][c] = fmaxf(high[j][c], g);
+              for (int c = 0; c < kPiece; ++c) {
+                low[j][c] = fminf(low[j][c], l[c]);
+                high[j][c] = fmaxf(high[j][c], g[c]);
+              }
             }
+            put<false>(to + at + j * apart, narrow<T, kPiece>(low[j]));
+            put<false>(to + a.row_bytes + at + j * apart, narrow<T, kPiece>(high[j]));
           }
-      }
-      if (has && mine == 0) {
-        char* const to = a.bounds + 2 * run * a.row_bytes + at;
+      } else {
+        const int cols = lanes * kCols;                    // (of a lane group, chunk by chunk)
+        if (has)
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j) {
-          if (!begun) {
-            float l[kPiece], g[kPiece];
-            widen<T, kPiece>(get<false, T, kPiece>(to + j * apart), l);
-            widen<T, kPiece>(get<false, T, kPiece>(to + a.row_bytes + j * apart), g);
+          for (int j = 0; j < kPieces; ++j)
 #pragma unroll
             for (int c = 0; c < kPiece; ++c) {
-              low[j][c] = fminf(low[j][c], l[c]);
-              high[j][c] = fmaxf(high[j][c], g[c]);
+              float* const place = lds + (int64_t)mine * 2 * cols + (chunk - first) * kCols + j * kPiece + c;
+              place[0] = low[j][c];
+              place[cols] = high[j][c];
             }
+        __syncthreads();
+        const int groups = abreast;
+        for (int i = threadIdx.x; i < 2 * cols; i += kAppThreads) {
+          const int which = i >= cols ? 1 : 0, col = i - which * cols, ch = first + col / kCols, k = col % kCols;
+          if (ch >= a.chunks) continue;
+          float v = lds[i];
+          for (int r = 1; r < groups; ++r) {
+            const float w = lds[(int64_t)r * 2 * cols + i];
+            v = which ? fmaxf(v, w) : fminf(v, w);
           }
-          put<false>(to + j * apart, narrow<T, kPiece>(low[j]));
-          put<false>(to + a.row_bytes + j * apart, narrow<T, kPiece>(high[j]));
+          int from, between;
+          place_of_chunk<T, P, kPiece>(a, ch, from, between);
+          write(to + from + k / kPiece * between, v, v, which, k % kPiece);
         }
+        __syncthreads();
       }
-      open = false;
     };
     int cur = t0;
     while (cur < a.tokens) {
       // the next tokens' slots, a lane each, and how many of them are of the same page
       const int64_t slot = slots[min(cur + lane, a.tokens - 1)];
-      const int page_mine = (int)page_of(slot);
+      const int page_mine = page_of(slot);
       const int page = __builtin_amdgcn_readfirstlane(page_mine);
       const uint64_t other = __ballot(page_mine != page || cur + lane >= a.tokens);
       const int n = other ? __builtin_ctzll(other) : 64;
@@ -229,18 +269,18 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
       if (open) {
         const int offset = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)a.page_size);
         begun = begun || __ballot(lane < n && offset == 0) != 0;
-        for (int i = 0; i < n; i += kTokensAtOnce * rows_abreast) {
+        for (int i = 0; i < n; i += kTokensAtOnce * abreast) {
           Vec<T, kPiece> v[kTokensAtOnce][kPieces];
 #pragma unroll
           for (int u = 0; u < kTokensAtOnce; ++u) {
-            const int t = i + u * rows_abreast + mine;
+            const int t = i + u * abreast + mine;
             if (has && t < n)
 #pragma unroll
               for (int j = 0; j < kPieces; ++j) v[u][j] = get<false, T, kPiece>(in + (int64_t)(cur + t) * a.k.st + at + j * apart);
           }
 #pragma unroll
           for (int u = 0; u < kTokensAtOnce; ++u) {
-            const int t = i + u * rows_abreast + mine;
+            const int t = i + u * abreast + mine;
             const int off = __shfl(offset, min(t, 63), 64);
             if (has && t < n) {
               if (chunk < a.turned) {
@@ -272,8 +312,11 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
 
 template <typename T, int P, bool INTERLEAVED, bool PAST>
 __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendArgs a, const fc_rotary_plan plan) {
-  if ((int)blockIdx.x < a.bound_groups) append_keys<T, P, INTERLEAVED>(a, plan, blockIdx.x);
-  else append_rows<T, P, INTERLEAVED, PAST>(a, plan, (int)blockIdx.x - a.bound_groups);
+  extern __shared__ __align__(16) float lds[];
+  if ((int)blockIdx.x < a.bound_groups) {
+    if (a.tokens == 1) append_keys<T, P, INTERLEAVED, true>(a, plan, blockIdx.x, nullptr);
+    else append_keys<T, P, INTERLEAVED, false>(a, plan, blockIdx.x, lds);
+  } else append_rows<T, P, INTERLEAVED, PAST>(a, plan, (int)blockIdx.x - a.bound_groups);
 }
 
 }  // namespace
@@ -330,9 +373,11 @@ hipError_t append_launch(const fc_rotary_plan& plan, const int32_t* positions, c
     const int64_t one_turn = ((int64_t)a.rows * heads + places - 1) / places;  // workgroups if every thread has a single head
     // few tokens: all heads side by side; else at least four turns, for which the sines are made once (see rotary.hip)
     int abreast = 1;
-    while (abreast < kMostAbreast && 2 * abreast * kHeadsAtOnce <= heads) abreast *= 2;
+    while (abreast < kMostAbreast && 8 * abreast <= heads) abreast *= 2;
     a.abreast = std::min(std::min(heads, places), one_turn > 2048 ? abreast : heads);
     a.turns = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMostTurns, (heads + a.abreast - 1) / a.abreast), one_turn / 2048));
+    const int batches = (a.turns + kHeadsAtOnce - 1) / kHeadsAtOnce;
+    a.at_once = (a.turns + batches - 1) / batches;
     a.per_group = places / a.abreast;
     a.chunks_inverse = inverse_of(a.chunks);
     a.abreast_inverse = inverse_of(a.abreast);
@@ -341,18 +386,22 @@ hipError_t append_launch(const fc_rotary_plan& plan, const int32_t* positions, c
   } else {
     a.across = 1;
   }
+  size_t lds = 0;
   if (bounds && k.heads) {
     a.stretch = a.tokens == 1 ? 1 : std::min(64, std::max(16, page_size));
     a.stretches = (a.tokens + a.stretch - 1) / a.stretch;
-    const int64_t waves = (int64_t)k.batch * k.heads * a.stretches;
-    if (waves >= 1 << 26) return hipErrorInvalidConfiguration;
-    a.bound_groups = (int)((waves + kAppWaves - 1) / kAppWaves);
+    const int64_t items = (int64_t)k.batch * k.heads * a.stretches;
+    if (items >= 1 << 24) return hipErrorInvalidConfiguration;
+    a.bound_groups = (int)(a.tokens == 1 ? (items + kAppWaves - 1) / kAppWaves : items);
+    // a lane group's columns, least and largest, of as many groups as the waves have
+    const int lanes = std::min(64, a.chunks);
+    if (a.tokens > 1) lds = (size_t)kAppWaves * (64 / lanes) * 2 * lanes * 2 * pairs * sizeof(float);
   }
   const int64_t groups = a.bound_groups + row_groups;
   if (groups == 0) return hipSuccess;
   if (groups >= 1 << 24) return hipErrorInvalidConfiguration;                // (2^32 threads)
   ProfileScope ps("append_kernel", s);
-  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAppThreads), 0, s, a, plan); };
+  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAppThreads), lds, s, a, plan); };
   // what is read and written exceeds the cache, in pieces of whole lines (see rotary.hip)
   const bool past = 2LL * a.rows * (q.heads + k.heads + v.heads) * a.row_bytes > 256000000 && (plan.interleaved || half * e % 128 == 0);
   auto with = [&](auto type, auto n, auto interleaved) {
