@@ -18,7 +18,8 @@ namespace {
 
 constexpr int kAppThreads = 256, kAppWaves = kAppThreads / 64;
 constexpr int kHeadsAtOnce = 5, kMostPairs = 4, kMostAbreast = 8, kMostTurns = 8;
-constexpr int kTokensAtOnce = 4;       // of a lane, with bounds
+constexpr int kTokensAtOnce = 2;       // of a lane, with bounds
+constexpr int kLooked = kAppThreads;   // tokens whose slots a workgroup looks up together
 
 struct NewRows {                 // strides in bytes
   const char* in;
@@ -60,24 +61,22 @@ template <typename T> __device__ __forceinline__ T as_type(float x) {      // (o
   else return x;
 }
 
-template <int P> __device__ __forceinline__ void sines_of(const AppendArgs& a, const fc_rotary_plan& plan, int row, int first, float (&sn)[P], float (&cs)[P]) {
-  int32_t where[P];
-  where[0] = a.positions[row];
+// A token's positions in all streams.
+struct Positions { int32_t at[4]; };
+__device__ __forceinline__ Positions positions_of(const AppendArgs& a, int row) {
+  Positions p;
+  p.at[0] = a.positions[row];
 #pragma unroll
-  for (int i = 1; i < P; ++i) where[i] = where[0];
-  if (a.streams > 1) {
-    int32_t other[3];
-#pragma unroll
-    for (int k = 0; k < 3; ++k) other[k] = k + 1 < a.streams ? a.positions[(int64_t)(k + 1) * a.rows + row] : 0;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int pair = first + i;
-      where[i] = pair < a.end0 ? where[i] : pair < a.end1 ? other[0] : pair < a.end2 ? other[1] : other[2];
-    }
-  }
+  for (int k = 1; k < 4; ++k) p.at[k] = a.streams > 1 && k < a.streams ? a.positions[(int64_t)k * a.rows + row] : 0;
+  return p;
+}
+template <int P> __device__ __forceinline__ void sines_of(const AppendArgs& a, const fc_rotary_plan& plan, const Positions& p, int first, float (&sn)[P], float (&cs)[P]) {
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    sine_cosine(turned_by(where[i], plan.turns[first + i]), sn[i], cs[i]);
+    const int pair = first + i;
+    int32_t where = p.at[0];
+    if (a.streams > 1) where = pair < a.end0 ? where : pair < a.end1 ? p.at[1] : pair < a.end2 ? p.at[2] : p.at[3];
+    sine_cosine(turned_by(where, plan.turns[pair]), sn[i], cs[i]);
     sn[i] *= a.magnitude;
     cs[i] *= a.magnitude;
   }
@@ -123,40 +122,45 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const fc_rotary
   place_of_chunk<T, P, kPiece>(a, chunk, at, apart);
   const bool turned = chunk < a.turned && h0 + beside < a.turning;
   float sn[P], cs[P];
-  if (turned) sines_of<P>(a, plan, row, chunk * P, sn, cs);
+  if (turned) sines_of<P>(a, plan, positions_of(a, row), chunk * P, sn, cs);
+  // head `beside` of the queries, and what would be that of queries, keys and values as one: the rest of a head's place is the same for the wave
+  const char* const q_in = a.q.in + b * a.q.sb + t * a.q.st + beside * a.q.sh + at;
+  const char* const k_in = a.k.in + b * a.k.sb + t * a.k.st + (beside - a.q.heads) * a.k.sh + at;
+  const char* const v_in = a.v.in + b * a.v.sb + t * a.v.st + (beside - a.turning) * a.v.sh + at;
+  char* const q_out = a.q_out + b * a.ob + t * a.ot + beside * a.oh + at;
+  const int64_t* const slots = a.slots + b * a.slots_b + t;
   for (int hw = h0; hw < h1; hw += a.at_once * a.abreast) {
     Vec<T, kPiece> v[kHeadsAtOnce][kPieces];
     int64_t slot[kHeadsAtOnce];
 #pragma unroll
     for (int i = 0; i < kHeadsAtOnce; ++i) {
-      const int h = hw + i * a.abreast + beside;
+      const int hu = hw + i * a.abreast, h = hu + beside;
       if (i >= a.at_once || h >= h1) break;
       const char* in;
       if (h < a.q.heads) {
-        in = a.q.in + b * a.q.sb + t * a.q.st + h * a.q.sh;
+        in = q_in + hu * a.q.sh;
       } else {
         const bool key = h < a.turning;
-        const int kv = h - (key ? a.q.heads : a.turning);
-        slot[i] = a.slots[b * a.slots_b + kv * a.slots_h + t];
-        in = key ? a.k.in + b * a.k.sb + t * a.k.st + kv * a.k.sh : a.v.in + b * a.v.sb + t * a.v.st + kv * a.v.sh;
+        slot[i] = slots[(h - (key ? a.q.heads : a.turning)) * a.slots_h];
+        in = key ? k_in + hu * a.k.sh : v_in + hu * a.v.sh;
       }
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) v[i][j] = get<PAST, T, kPiece>(in + at + j * apart);
+      for (int j = 0; j < kPieces; ++j) v[i][j] = get<PAST, T, kPiece>(in + j * apart);
     }
 #pragma unroll
     for (int i = 0; i < kHeadsAtOnce; ++i) {
-      const int h = hw + i * a.abreast + beside;
+      const int hu = hw + i * a.abreast, h = hu + beside;
       if (i >= a.at_once || h >= h1) break;
       if (turned && h < a.turning) turn<T, P, INTERLEAVED>(v[i], sn, cs);
       char* out;
       if (h < a.q.heads) {
-        out = a.q_out + b * a.ob + t * a.ot + h * a.oh;
+        out = q_out + hu * a.oh;
       } else {
         if (slot[i] < 0 || slot[i] >= a.num_slots) continue;
-        out = (h < a.turning ? a.k_pages : a.v_pages) + slot[i] * a.row_bytes;
+        out = (h < a.turning ? a.k_pages : a.v_pages) + (uint64_t)(uint32_t)slot[i] * (uint32_t)a.row_bytes + at;
       }
 #pragma unroll
-      for (int j = 0; j < kPieces; ++j) put<PAST>(out + at + j * apart, v[i][j]);
+      for (int j = 0; j < kPieces; ++j) put<PAST>(out + j * apart, v[i][j]);
     }
   }
 }
@@ -164,7 +168,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, const fc_rotary
 // A stretch of a KV head's tokens: the runs of tokens with a page in common that begin in it, up to their ends.  ALONE: a wave has it (a single token),
 // else the workgroup, whose lane groups' results meet in LDS.
 template <typename T, int P, bool INTERLEAVED, bool ALONE>
-__device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary_plan& plan, int group, float* lds) {
+__device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary_plan& plan, int group, T* lds) {
   constexpr int kPieces = INTERLEAVED ? 1 : 2, kPiece = 2 * P / kPieces, kCols = 2 * P;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = ALONE ? group * kAppWaves + wave : group;
   const int head = item / a.stretches, b = head / a.k.heads, h = head - b * a.k.heads;
@@ -182,7 +186,21 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
     int at, apart;
     place_of_chunk<T, P, kPiece>(a, has ? chunk : 0, at, apart);
     float low[kPieces][kPiece], high[kPieces][kPiece];
-    int run = t0 > 0 ? page_of(slots[t0 - 1]) : -1;        // page that the tokens before have
+    // pages and places of the tokens from `looked` on, a thread each: one wait for memory for the pages that begin in a stretch
+    __shared__ int look_page[kLooked], look_place[kLooked];
+    int looked = t0 - 1;
+    auto look_up = [&]() {
+      const int64_t slot = slots[min(max(looked + (int)threadIdx.x, 0), a.tokens - 1)];
+      const int page = page_of(slot);
+      look_page[threadIdx.x] = page;
+      look_place[threadIdx.x] = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)a.page_size);
+      __syncthreads();
+    };
+    if constexpr (!ALONE) {
+      if (first) __syncthreads();                          // (the look-up before is done with)
+      look_up();
+    }
+    int run = t0 == 0 ? -1 : ALONE ? page_of(slots[t0 - 1]) : look_page[0];      // page that the tokens before have
     bool open = false, begun = false;                      // whether the run is this one's; whether it has the page's first row
     // what the page's bounds are, with those of before
     auto write = [&](char* to, float l, float g, int which, int c) {
@@ -224,18 +242,19 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
           for (int j = 0; j < kPieces; ++j)
 #pragma unroll
             for (int c = 0; c < kPiece; ++c) {
-              float* const place = lds + (int64_t)mine * 2 * cols + (chunk - first) * kCols + j * kPiece + c;
-              place[0] = low[j][c];
-              place[cols] = high[j][c];
+              T* const place = lds + mine * 2 * cols + (chunk - first) * kCols + j * kPiece + c;
+              place[0] = as_type<T>(low[j][c]);
+              place[cols] = as_type<T>(high[j][c]);
             }
         __syncthreads();
         const int groups = abreast;
         for (int i = threadIdx.x; i < 2 * cols; i += kAppThreads) {
           const int which = i >= cols ? 1 : 0, col = i - which * cols, ch = first + col / kCols, k = col % kCols;
           if (ch >= a.chunks) continue;
-          float v = lds[i];
+          float v = as_float(lds[i]);
+#pragma unroll 4
           for (int r = 1; r < groups; ++r) {
-            const float w = lds[(int64_t)r * 2 * cols + i];
+            const float w = as_float(lds[r * 2 * cols + i]);
             v = which ? fmaxf(v, w) : fminf(v, w);
           }
           int from, between;
@@ -248,8 +267,21 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
     int cur = t0;
     while (cur < a.tokens) {
       // the next tokens' slots, a lane each, and how many of them are of the same page
-      const int64_t slot = slots[min(cur + lane, a.tokens - 1)];
-      const int page_mine = page_of(slot);
+      int page_mine, offset;
+      if constexpr (ALONE) {
+        const int64_t slot = slots[min(cur + lane, a.tokens - 1)];
+        page_mine = page_of(slot);
+        offset = (int)((uint32_t)slot - (uint32_t)page_mine * (uint32_t)a.page_size);
+      } else {
+        if (cur + 64 > looked + kLooked && looked + kLooked < a.tokens) {
+          __syncthreads();
+          looked = cur;
+          look_up();
+        }
+        const int at = min(cur + lane, a.tokens - 1) - looked;
+        page_mine = look_page[at];
+        offset = look_place[at];
+      }
       const int page = __builtin_amdgcn_readfirstlane(page_mine);
       const uint64_t other = __ballot(page_mine != page || cur + lane >= a.tokens);
       const int n = other ? __builtin_ctzll(other) : 64;
@@ -267,16 +299,17 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
         break;
       }
       if (open) {
-        const int offset = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)a.page_size);
         begun = begun || __ballot(lane < n && offset == 0) != 0;
         for (int i = 0; i < n; i += kTokensAtOnce * abreast) {
+          // (all loads before the first store: a load's wait behind one is for its end, too)
           Vec<T, kPiece> v[kTokensAtOnce][kPieces];
+          Positions where[kTokensAtOnce];
 #pragma unroll
           for (int u = 0; u < kTokensAtOnce; ++u) {
-            const int t = i + u * abreast + mine;
-            if (has && t < n)
+            const int t = min(i + u * abreast + mine, n - 1);
 #pragma unroll
-              for (int j = 0; j < kPieces; ++j) v[u][j] = get<false, T, kPiece>(in + (int64_t)(cur + t) * a.k.st + at + j * apart);
+            for (int j = 0; j < kPieces; ++j) v[u][j] = get<false, T, kPiece>(in + (int64_t)(cur + t) * a.k.st + at + j * apart);
+            where[u] = positions_of(a, b * a.tokens + cur + t);
           }
 #pragma unroll
           for (int u = 0; u < kTokensAtOnce; ++u) {
@@ -285,7 +318,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
             if (has && t < n) {
               if (chunk < a.turned) {
                 float sn[P], cs[P];
-                sines_of<P>(a, plan, b * a.tokens + cur + t, chunk * P, sn, cs);
+                sines_of<P>(a, plan, where[u], chunk * P, sn, cs);
                 turn<T, P, INTERLEAVED>(v[u], sn, cs);
               }
               char* const to = a.k_pages + ((int64_t)page * a.page_size + off) * a.row_bytes + at;
@@ -310,13 +343,17 @@ __device__ __forceinline__ void append_keys(const AppendArgs& a, const fc_rotary
   }
 }
 
-template <typename T, int P, bool INTERLEAVED, bool PAST>
+template <typename T, int P, bool INTERLEAVED, bool PAST, bool BOUNDS>
 __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendArgs a, const fc_rotary_plan plan) {
-  extern __shared__ __align__(16) float lds[];
-  if ((int)blockIdx.x < a.bound_groups) {
-    if (a.tokens == 1) append_keys<T, P, INTERLEAVED, true>(a, plan, blockIdx.x, nullptr);
-    else append_keys<T, P, INTERLEAVED, false>(a, plan, blockIdx.x, lds);
-  } else append_rows<T, P, INTERLEAVED, PAST>(a, plan, (int)blockIdx.x - a.bound_groups);
+  if constexpr (BOUNDS) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    if ((int)blockIdx.x < a.bound_groups) {
+      if (a.tokens == 1) append_keys<T, P, INTERLEAVED, true>(a, plan, blockIdx.x, nullptr);
+      else append_keys<T, P, INTERLEAVED, false>(a, plan, blockIdx.x, reinterpret_cast<T*>(lds));
+      return;
+    }
+  }
+  append_rows<T, P, INTERLEAVED, PAST>(a, plan, (int)blockIdx.x - (BOUNDS ? a.bound_groups : 0));
 }
 
 }  // namespace
@@ -395,7 +432,7 @@ hipError_t append_launch(const fc_rotary_plan& plan, const int32_t* positions, c
     a.bound_groups = (int)(a.tokens == 1 ? (items + kAppWaves - 1) / kAppWaves : items);
     // a lane group's columns, least and largest, of as many groups as the waves have
     const int lanes = std::min(64, a.chunks);
-    if (a.tokens > 1) lds = (size_t)kAppWaves * (64 / lanes) * 2 * lanes * 2 * pairs * sizeof(float);
+    if (a.tokens > 1) lds = (size_t)kAppWaves * (64 / lanes) * 2 * lanes * 2 * pairs * e;
   }
   const int64_t groups = a.bound_groups + row_groups;
   if (groups == 0) return hipSuccess;
@@ -406,8 +443,10 @@ hipError_t append_launch(const fc_rotary_plan& plan, const int32_t* positions, c
   const bool past = 2LL * a.rows * (q.heads + k.heads + v.heads) * a.row_bytes > 256000000 && (plan.interleaved || half * e % 128 == 0);
   auto with = [&](auto type, auto n, auto interleaved) {
     typedef decltype(type) T;
-    past ? launch(append_kernel<T, decltype(n)::value, decltype(interleaved)::value, true>)
-         : launch(append_kernel<T, decltype(n)::value, decltype(interleaved)::value, false>);
+    constexpr int kN = decltype(n)::value;
+    constexpr bool kInterleaved = decltype(interleaved)::value;
+    if (a.bound_groups) past ? launch(append_kernel<T, kN, kInterleaved, true, true>) : launch(append_kernel<T, kN, kInterleaved, false, true>);
+    else past ? launch(append_kernel<T, kN, kInterleaved, true, false>) : launch(append_kernel<T, kN, kInterleaved, false, false>);
   };
   typedef std::integral_constant<int, 4> Four;
   typedef std::integral_constant<int, 2> Two;
