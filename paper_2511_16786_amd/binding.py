@@ -680,12 +680,25 @@ class PagedKV:
 
 
 @functools.lru_cache(maxsize=1024)
-def _new_rows_of(shape, strides, dtype) -> FcHeadsDesc:
-    B, T, H, d = shape
-    sb, st, sh, sd = strides
-    if sd != 1 and d > 1:
+def _append_of(q_shape, k_shape, v_shape, out_shape, pos_shape, slots_shape, pages_shape, v_pages_shape, bounds_shape, q_strides, k_strides, v_strides,
+               out_strides, slots_strides, dtype, streams):
+    """What a call's shapes and strides come to, checked: references to the descriptors of Q, K and V (by what they say alone, as in _heads_of)."""
+    if len(q_shape) != 4 or len(k_shape) != 4 or k_shape[:2] != q_shape[:2] or k_shape[3] != q_shape[3] or v_shape != k_shape:
+        raise ValueError("Q, K and V must have shape [B, T, H, d], K and V as many heads, all with B, T and d in common")
+    B, T, H, d = k_shape
+    if pos_shape != (streams, B, T) and (streams != 1 or pos_shape != (B, T)):
+        raise ValueError(f"positions must have shape {(streams, B, T)}")
+    if slots_shape != (B, H, T) or (T > 1 and slots_strides[2] != 1):
+        raise ValueError(f"slots must have shape {(B, H, T)}, a head's tokens side by side")
+    if len(pages_shape) != 3 or pages_shape[2] != d or v_pages_shape != pages_shape:
+        raise ValueError(f"K_pages and V_pages must have shape [num_pages, page_size, {d}]")
+    if bounds_shape is not None and bounds_shape != (pages_shape[0], 2, d):
+        raise ValueError(f"bounds must have shape {(pages_shape[0], 2, d)}")
+    if d > 1 and (k_strides[3] != 1 or v_strides[3] != 1):
         raise ValueError("the head dimension must be contiguous")
-    return FcHeadsDesc(B, T, H, d, _type(dtype), 0, sb, st, sh, 0, 0, 0)
+    new = [FcHeadsDesc(B, T, H, d, _type(dtype), 0, *strides[:3], 0, 0, 0) for strides in (k_strides, v_strides)]
+    q = _heads_of(q_shape, out_shape, q_strides, out_strides, dtype)
+    return (ctypes.byref(q), *(ctypes.byref(x) for x in new), slots_strides[0], slots_strides[1], pages_shape[1], pages_shape[0])
 
 
 def append_paged(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor,
@@ -699,32 +712,23 @@ def append_paged(plan: FcRotaryPlan, positions: torch.Tensor, Q: torch.Tensor, K
     if torch.is_grad_enabled() and (Q.requires_grad or K.requires_grad or V.requires_grad or K_pages.requires_grad or V_pages.requires_grad or
                                     Q_out is not None and Q_out.requires_grad or bounds is not None and bounds.requires_grad):
         raise ValueError("append_paged records no gradients: call it under torch.no_grad()")
-    shape, kv_shape = Q.shape, K.shape
-    if len(shape) != 4 or len(kv_shape) != 4 or kv_shape[:2] != shape[:2] or kv_shape[3] != shape[3] or V.shape != kv_shape:
-        raise ValueError("Q, K and V must have shape [B, T, H, d], K and V as many heads, all with B, T and d in common")
-    B, T, H, d = kv_shape
     dtype = Q.dtype
-    if K.dtype is not dtype or V.dtype is not dtype or K.get_device() != index or V.get_device() != index:
-        raise ValueError(f"Q, K and V must have the same dtype and be on GPU {index}")
-    if plan.streams == 1 and positions.dim() == 2:
-        _want(positions, "positions", torch.int32, (B, T), index)
-    else:
-        _want(positions, "positions", torch.int32, (plan.streams, B, T), index)
-    if K_pages.dim() != 3:
-        raise ValueError("K_pages and V_pages must have shape [num_pages, page_size, d]")
-    pages, page_size = K_pages.shape[:2]
-    _want(K_pages, "K_pages", dtype, (pages, page_size, d), index)
-    _want(V_pages, "V_pages", dtype, (pages, page_size, d), index)
-    _want(bounds, "bounds", dtype, (pages, 2, d), index)
-    if slots.dtype is not torch.int64 or slots.shape != (B, H, T) or slots.get_device() != index or (T > 1 and slots.stride(2) != 1):
-        raise ValueError(f"slots must be a torch.int64 tensor of shape {(B, H, T)} on GPU {index}, a head's tokens side by side")
     if Q_out is None:
-        Q_out = torch.empty(shape, dtype=dtype, device=Q.device)
-    qd = _heads(Q, Q_out, "Q", index)
+        Q_out = torch.empty(Q.shape, dtype=dtype, device=Q.device)
+    if not (K.dtype is V.dtype is K_pages.dtype is V_pages.dtype is Q_out.dtype is dtype and (bounds is None or bounds.dtype is dtype) and
+            positions.dtype is torch.int32 and slots.dtype is torch.int64):
+        raise ValueError("Q, K, V, the pages, bounds and Q_out must have the same dtype, positions int32 and slots int64")
+    if not (K.get_device() == V.get_device() == K_pages.get_device() == V_pages.get_device() == Q_out.get_device() == positions.get_device() ==
+            slots.get_device() == index and (bounds is None or bounds.get_device() == index)):
+        raise ValueError(f"all tensors must be on GPU {index}")
+    if not (positions.is_contiguous() and K_pages.is_contiguous() and V_pages.is_contiguous() and (bounds is None or bounds.is_contiguous())):
+        raise ValueError("positions, pages and bounds must be contiguous")
+    q_ref, k_ref, v_ref, slots_b, slots_h, page_size, pages = _append_of(
+        Q.shape, K.shape, V.shape, Q_out.shape, positions.shape, slots.shape, K_pages.shape, V_pages.shape, None if bounds is None else bounds.shape,
+        Q.stride(), K.stride(), V.stride(), Q_out.stride(), slots.stride(), dtype, plan.streams)
     _check(_lib.flashcache_append_paged(
-        ctypes.byref(plan), positions.data_ptr(), Q.data_ptr(), Q_out.data_ptr(), ctypes.byref(qd), K.data_ptr(),
-        ctypes.byref(_new_rows_of(kv_shape, K.stride(), dtype)), V.data_ptr(), ctypes.byref(_new_rows_of(kv_shape, V.stride(), dtype)),
-        slots.data_ptr(), slots.stride(0), slots.stride(1), page_size, pages, K_pages.data_ptr(), V_pages.data_ptr(), _ptr(bounds), _stream()),
+        plan, positions.data_ptr(), Q.data_ptr(), Q_out.data_ptr(), q_ref, K.data_ptr(), k_ref, V.data_ptr(), v_ref, slots.data_ptr(), slots_b,
+        slots_h, page_size, pages, K_pages.data_ptr(), V_pages.data_ptr(), None if bounds is None else bounds.data_ptr(), _stream()),
         "flashcache_append_paged")
     return Q_out
 
