@@ -28,7 +28,7 @@ namespace {
 constexpr int kAttThreads = 256, kAttWaves = kAttThreads / 64;
 constexpr int kTileQueries = 128;      // of a workgroup
 constexpr int kLeastSteps = 4;         // of a piece
-constexpr int kGroups = 512;           // pieces that a launch over shared rows aims at: as many as are resident together
+constexpr int kGroups = 512;           // workgroups that are resident together
 constexpr int kStepsLooked = 64;       // steps whose rows' places are looked up together
 constexpr float kSlack = 16.f;         // how far scores (in log2) may exceed the running reference before it is moved
 
@@ -49,6 +49,18 @@ __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, 
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {        // to nearest
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v{a, b}), bf16x2));
+}
+// x less the lower or the upper of two bf16 values: exact where that value is x cut off.  (One operation; the constants are kept from the
+// compiler, which would take 0xBF800000 for an inline constant of another value in this instruction.)
+__device__ __forceinline__ float less_low(float x, uint32_t two) {
+  uint32_t c;
+  asm("s_mov_b32 %0, 0xbf80" : "=s"(c));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, c), x, false);
+}
+__device__ __forceinline__ float less_high(float x, uint32_t two) {
+  uint32_t c;
+  asm("s_mov_b32 %0, 0xbf800000" : "=s"(c));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, c), x, false);
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 template <typename V> __device__ __forceinline__ V load_past(const void* p) { return __builtin_nontemporal_load(static_cast<const V*>(p)); }
@@ -90,13 +102,18 @@ template <int D> struct Form<uint16_t, D> {
       x.w[tile][i][0] = u.x; x.w[tile][i][1] = u.y;
     }
   }
-  static __device__ __forceinline__ float4v scores(const Queries& q, const Keys& x, int tile) {
-    float4v acc = {0.f, 0.f, 0.f, 0.f};
+  // (the products of one sum are not next to each other)
+  template <int N> static __device__ __forceinline__ void scores(const Queries (&q)[N], const Keys& x, float4v (&acc)[N][kTiles]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j][0] = acc[j][1] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < KW / 4; ++s)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x.w[tile][4 * s], x.w[tile][4 * s + 1], x.w[tile][4 * s + 2], x.w[tile][4 * s + 3]),
-                                                    as_bf16x8(q.w[4 * s], q.w[4 * s + 1], q.w[4 * s + 2], q.w[4 * s + 3]), acc, 0, 0, 0);
-    return acc;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          acc[j][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x.w[tt][4 * s], x.w[tt][4 * s + 1], x.w[tt][4 * s + 2], x.w[tt][4 * s + 3]),
+                                                               as_bf16x8(q[j].w[4 * s], q[j].w[4 * s + 1], q[j].w[4 * s + 2], q[j].w[4 * s + 3]), acc[j][tt], 0, 0, 0);
   }
   static __device__ __forceinline__ void weights(const float (&p)[kTiles][4], Weights& w) {
     // each term is what the one before left, cut off to bf16: the third is exact
@@ -107,8 +124,10 @@ template <int D> struct Form<uint16_t, D> {
       for (int n = 0; n < 3; ++n) {
         const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
         w.term[n][j] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
-        a -= __uint_as_float(ua & 0xFFFF0000u);
-        b -= __uint_as_float(ub & 0xFFFF0000u);
+        if (n < 2) {
+          a = less_low(a, w.term[n][j]);
+          b = less_high(b, w.term[n][j]);
+        }
       }
     }
   }
@@ -193,11 +212,21 @@ template <int D> struct Form<float, D> {
       x.w[tile][i][4 * j] = u.x; x.w[tile][i][4 * j + 1] = u.y; x.w[tile][i][4 * j + 2] = u.z; x.w[tile][i][4 * j + 3] = u.w;
     }
   }
-  static __device__ __forceinline__ float4v scores(const Queries& q, const Keys& x, int tile) {
-    float4v acc = {0.f, 0.f, 0.f, 0.f};
+  template <int N> static __device__ __forceinline__ void scores(const Queries (&q)[N], const Keys& x, float4v (&acc)[N][kTiles]) {
+    float4v odd[N];
 #pragma unroll
-    for (int i = 0; i < KW; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w[tile][i], q.w[i], acc, 0, 0, 0);
-    return acc;
+    for (int j = 0; j < N; ++j) acc[j][0] = odd[j] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KW; i += 2)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        acc[j][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w[0][i], q[j].w[i], acc[j][0], 0, 0, 0);
+        odd[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w[0][i + 1], q[j].w[i + 1], odd[j], 0, 0, 0);
+      }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][0][i] += odd[j][i];
   }
   static __device__ __forceinline__ void weights(const float (&p)[kTiles][4], Weights& w) {
 #pragma unroll
@@ -258,16 +287,13 @@ template <typename T, int D, int N> struct State {
     }
   }
   // `there`: the step's rows that there are, a bit each
-  __device__ __forceinline__ void weigh(int j, const typename F::Queries& q, const typename F::Keys& x, uint32_t there, const Scale& scale, int g4,
-                                        typename F::Weights& w) {
+  __device__ __forceinline__ void weigh(int j, const float4v (&acc)[F::kTiles], uint32_t there, const Scale& scale, int g4, typename F::Weights& w) {
     float p[F::kTiles][4];
     float mx = -INFINITY;
 #pragma unroll
-    for (int tt = 0; tt < F::kTiles; ++tt) {
-      const float4v acc = F::scores(q, x, tt);
+    for (int tt = 0; tt < F::kTiles; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[tt][i] = acc[i];
-    }
+      for (int i = 0; i < 4; ++i) p[tt][i] = acc[tt][i];
     if (there != kAll)
 #pragma unroll
       for (int tt = 0; tt < F::kTiles; ++tt)
@@ -317,7 +343,7 @@ template <typename T, int D, int N> struct State {
 // A wave's steps 0 .. n - 1, two under way.  `begin(step, r)` loads what leads to the place of row r of a step, `finish` takes that and loads the place
 // (the cache row, or kNoRow): both for as many steps together as 64 lanes have rows of, and a turn ahead of their use.
 template <typename T, int D, typename Begin, typename Finish>
-__device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<T, D>::Queries& q, const T* K, const T* V, int n, const Scale& scale, int lane,
+__device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<T, D>::Queries (&q)[1], const T* K, const T* V, int n, const Scale& scale, int lane,
                                      const Begin& begin, const Finish& finish) {
   typedef Form<T, D> F;
   constexpr int kTogether = 64 / F::kRows;                 // steps of a look-up
@@ -363,7 +389,9 @@ __device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<
   auto turn = [&](int st, Step& x) {
     if (x.there) {
       typename F::Weights w[1];
-      state.weigh(0, q, x.k, x.there, scale, g4, w[0]);
+      float4v acc[1][F::kTiles];
+      F::template scores<1>(q, x.k, acc);
+      state.weigh(0, acc[0], x.there, scale, g4, w[0]);
       F::template add<1>(w, x.v, state.out);
     }
     if (st + 2 < n) ask(st + 2, x);
@@ -414,6 +442,30 @@ __device__ __forceinline__ void merge_waves(State<T, D, 1>& state, int rows, flo
   }
 }
 
+// Tile j of a wave's state into a record of `queries`, from query `from` on.
+template <typename T, int D, int N>
+__device__ __forceinline__ void write_record(const State<T, D, N>& state, int j, int from, int queries, float* record, int lane) {
+  typedef Form<T, D> F;
+  const int c16 = lane & 15, g4 = lane >> 4;
+  float sum = state.sum[j];
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (g4 == 0 && from + c16 < queries) {
+    record[from + c16] = state.m[j];
+    record[queries + from + c16] = sum;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int query = from + 4 * g4 + i;
+    if (query < queries)
+#pragma unroll
+      for (int t = 0; t < F::VT; t += 2) {                 // (neighbouring columns; records' rows lie at multiples of 8 bytes)
+        float* const to = record + 2 * queries + (int64_t)query * D + F::column(c16, t);
+        *reinterpret_cast<float2v*>(to) = float2v{state.out[j][t][i], state.out[j][t + 1][i]};
+      }
+  }
+}
+
 // ---- pages that a list names -------------------------------------------------------------------
 // grid = (parts, units): the waves of a unit's parts take its steps in turn, so that a list that ends early leaves none idle before the others.
 template <typename T, int D>
@@ -425,9 +477,9 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_chosen_kernel(PagedArgs
   const int rows = rows_of(a, b, in / a.H);
   const int32_t* const table = a.table + b * a.table_b + (int64_t)in * a.max_pages;
   const int32_t* const list = chosen + (int64_t)u * count;
-  typename F::Queries q;
-  F::queries(Q + ((int64_t)u * G + min(c16, G - 1)) * D, c16 < G, g4, q);
-  if (scale.negate) F::negate(q);
+  typename F::Queries q[1];
+  F::queries(Q + ((int64_t)u * G + min(c16, G - 1)) * D, c16 < G, g4, q[0]);
+  if (scale.negate) F::negate(q[0]);
   const int waves = gridDim.x * kAttWaves, wave = blockIdx.x * kAttWaves + uniform(threadIdx.x >> 6);
   const int steps = (count * a.page_size + F::kRows - 1) / F::kRows;
   // step i of the wave is step wave + i * waves of the unit
@@ -530,12 +582,13 @@ template <int D> __global__ __launch_bounds__(1024) void chosen_merge_kernel(con
 struct SharedArgs {
   PagedArgs common, own;         // of P prompts and of B sequences
   const int32_t* starts;         // [P + 1]
-  int G, groups;
-  int64_t most_common, most_own; // records of either kind that the workspace has
+  int G, groups;                 // pieces of prompts that the launch aims at
+  int most_common;               // records of prompts that the workspace has, and as many workgroups, the launch's first
+  int own_parts, step_rows;      // waves of a sequence's unit, each with a record; rows of a step
   Scale scale;
   float* common_records;
   float* own_records;
-  int2* span;                    // of each prompt's layers, then of each sequence's: first record, pieces of a unit
+  int2* span;                    // of each prompt's layers: first record, pieces of a unit
   float* out;
 };
 
@@ -547,16 +600,12 @@ __device__ __forceinline__ Run run_of(const SharedArgs& a, int p) {
 }
 __device__ __forceinline__ int tiles_of(const SharedArgs& a, int n) { return (n * a.G + kTileQueries - 1) / kTileQueries; }
 
-// Entry e: a layer of a prompt, or, behind all of these, of a sequence.  Its rows, and how many units and query tiles have them to read.
+// Entry e: a layer of a prompt.  Its rows, and how many units and query tiles have them to read.
 struct Entry { int rows, times; };
-__device__ __forceinline__ Entry entry_at(const SharedArgs& a, int e) {
-  const int L = a.own.L, shared = a.common.B * L;
-  if (e < shared) {
-    const int p = e / L;
-    return {rows_of(a.common, p, e - p * L), a.own.H * tiles_of(a, run_of(a, p).n)};
-  }
-  const int b = (e - shared) / L;
-  return {rows_of(a.own, b, e - shared - b * L), a.own.H};
+__device__ __forceinline__ Entry entry_at(const SharedArgs& a, int e, int entries) {
+  const int at = min(e, entries - 1), p = at / a.own.L;
+  const Entry x{rows_of(a.common, p, at - p * a.own.L), a.own.H * tiles_of(a, run_of(a, p).n)};
+  return e < entries ? x : Entry{0, 0};
 }
 template <int ROWS> __device__ __forceinline__ int steps_in(int rows) { return (rows + ROWS - 1) / ROWS; }
 
@@ -565,52 +614,84 @@ __device__ __forceinline__ int64_t wave_sum(int64_t v) {
   for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
   return v;
 }
-__device__ __forceinline__ int64_t wave_scan(int64_t v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t o = __shfl_up(v, d, 64);
-    if (lane >= d) v += o;
-  }
-  return v;
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v) {     // 0 where there is no source lane
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {          // sums up to and with each lane
+  v = dpp_add<0x111, 0xF>(v);      // row_shr:1, 2, 4, 8
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);      // row_bcast:15 into rows 1 and 3
+  return dpp_add<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
 }
 
-// A step's rows of K and V in LDS, two steps at a time; the places of 64 steps' rows, and which of them there are.
+// Steps' rows of K and V in LDS, kStages of them; the places of 64 steps' rows, and which of them there are.
+constexpr int kStages = 4;             // (three under way: request, wait and barrier below go by that)
 template <typename T, int D> struct Staged {
   typedef Form<T, D> F;
   static constexpr int kVectors = F::kRows * F::kPieces;   // of 16 bytes, of K or V
-  u32x4 k[2][kVectors], v[2][kVectors];
+  u32x4 k[kStages][kVectors], v[kStages][kVectors];
   uint32_t places[kStepsLooked * F::kRows];
   uint32_t there[kStepsLooked];
 };
 
-// Steps first .. end of a unit's rows for up to 64 N queries, N tiles a wave (tiles behind the last query are zeros).  Every thread has its part of a step's rows on the way to registers two steps ahead and
-// puts it into LDS, where the waves find the whole step; one barrier a step.
+// 16 bytes a lane from memory into LDS, side by side from `to` on (the same for the wave); nothing for lanes that are off.  It counts as a load; what it
+// writes is there behind a wait for it.  (Written out: behind the builtin the compiler waits for all loads under way before it reads LDS.  There is
+// no output register that could be taken for written before it is.)
+__device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+// All but the last `left` loads (an even number up to 8) are done with.
+__device__ __forceinline__ void wait_for_loads(int left) {
+  if (left == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  else if (left == 6) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+  else if (left == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+  else if (left == 2) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// Steps first .. end of a unit's rows for up to 64 N queries, N tiles a wave (tiles behind the last query are zeros).  Rows go from memory straight into
+// LDS, three steps ahead, a quarter of them by each wave; one barrier a step.
 template <typename T, int D, int N, typename Places, typename LoadQueries>
 __device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, int first, int end, int queries, const Scale& scale, float* record,
                                            const Places& place_of, const LoadQueries& load_queries) {
   typedef Form<T, D> F;
   typedef Staged<T, D> S;
   constexpr int kMine = S::kVectors / kAttThreads;         // vectors of K, and of V, a thread and step
-  static_assert(S::kVectors % kAttThreads == 0, "a thread has whole vectors");
+  static_assert(S::kVectors % kAttThreads == 0 && 4 * kMine <= 8, "a thread has whole vectors; two steps' loads at most are waited for by number");
   S& s = *static_cast<S*>(lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
   typename F::Queries q[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) load_queries(16 * (wave + j * kAttWaves), q[j]);
   State<T, D, N> state;
-  struct Part { u32x4 k[kMine], v[kMine]; };
-  auto request = [&](int at, Part& x) {                    // of step `at` of those that were looked up
+  // (rows that are not there stay what LDS has: values, for which a weight of 0 has to make 0)
+  u32x4* const all_v = &s.v[0][0];
+  for (int i = tid; i < kStages * S::kVectors; i += kAttThreads) all_v[i] = u32x4{0u, 0u, 0u, 0u};
+  const uint32_t k_at = lds_offset(&s.k[0][wave * 64]), v_at = lds_offset(&s.v[0][wave * 64]);
+  uint32_t place[kMine];                                   // of this thread's vectors, of the step that is requested next
+  auto look = [&](int at) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) place[i] = s.places[at * F::kRows + (i * kAttThreads + tid) / F::kPieces];
+  };
+  auto request = [&](int at) -> int {                      // step `at` of those that were looked up; how many loads of this wave that makes
+    int loads = 0;
+    const uint32_t stage = (uint32_t)(at % kStages) * (uint32_t)(S::kVectors * 16);
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-      const int n = i * kAttThreads + tid, row = n / F::kPieces, piece = n % F::kPieces;
-      const uint32_t place = s.places[at * F::kRows + row];
-      x.k[i] = x.v[i] = u32x4{0u, 0u, 0u, 0u};
-      if (place != kNoRow) {
-        const int64_t from = (int64_t)place * (D * (int)sizeof(T)) + piece * 16;
-        x.k[i] = load_past<u32x4>(reinterpret_cast<const char*>(K) + from);
-        x.v[i] = load_past<u32x4>(reinterpret_cast<const char*>(V) + from);
+      const int m = i * kAttThreads + tid, row = m / F::kPieces, piece = m % F::kPieces;
+      if (place[i] != kNoRow) {
+        const int64_t from = (int64_t)place[i] * (D * (int)sizeof(T));
+        // (K's swapped places, the other way round)
+        load_to_lds(reinterpret_cast<const char*>(K) + from + (F::k_place(row, piece) - row * F::kPieces) * 16, k_at + stage + i * kAttThreads * 16);
+        load_to_lds(reinterpret_cast<const char*>(V) + from + piece * 16, v_at + stage + i * kAttThreads * 16);
       }
+      loads += __any(place[i] != kNoRow) ? 2 : 0;          // (none without a lane that has a row)
     }
+    look(min(at + 1, kStepsLooked - 1));
+    return loads;
   };
   for (int base = first; base < end; base += kStepsLooked) {
     const int n = min(kStepsLooked, end - base);
@@ -626,156 +707,150 @@ __device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, in
       }
     }
     __syncthreads();
-    Part pa, pb;
-    request(0, pa);
-    if (n > 1) request(1, pb);
-    auto turn = [&](int at, Part& x) {
-      const int buffer = at & 1;
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const int m = i * kAttThreads + tid;
-        s.k[buffer][F::k_place(m / F::kPieces, m % F::kPieces)] = x.k[i];
-        s.v[buffer][m] = x.v[i];
-      }
-      if (at + 2 < n) request(at + 2, x);
+    look(0);
+    request(0);
+    int after = n > 1 ? request(1) : 0, after_that = n > 2 ? request(2) : 0;     // loads of the steps behind the one that is waited for
+    for (int at = 0; at < n; ++at) {
       const uint32_t there = (uint32_t)uniform((int)s.there[at]);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (what is on the way from memory stays there)
+      // this wave's part of the step is in LDS; behind the barrier everybody's is, and the step before is done with
+      wait_for_loads(after + after_that);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
+      after = after_that;
+      after_that = at + kStages - 1 < n ? request(at + kStages - 1) : 0;
       if (there) {
-        typename F::Weights w[N];
-        {
-          typename F::Keys k;
-          F::read(s.k[buffer], c16, g4, k);
-#pragma unroll
-          for (int j = 0; j < N; ++j) state.weigh(j, q[j], k, there, scale, g4, w[j]);
-        }
+        const int stage = at % kStages;
+        typename F::Keys k;
         typename F::Values v;
-        F::read(s.v[buffer], c16, g4, v);
+        F::read(s.k[stage], c16, g4, k);
+        F::read(s.v[stage], c16, g4, v);
+        asm volatile("" ::: "memory");                     // (both are on the way before the products begin)
+        float4v acc[N][F::kTiles];
+        F::template scores<N>(q, k, acc);
+        typename F::Weights w[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) state.weigh(j, acc[j], there, scale, g4, w[j]);
         F::template add<N>(w, v, state.out);
       }
-    };
-    for (int at = 0; at < n; at += 2) {
-      turn(at, pa);
-      if (at + 1 < n) turn(at + 1, pb);
     }
   }
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int from = 16 * (wave + j * kAttWaves);
-    if (from >= queries) break;
-    float sum = state.sum[j];
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (g4 == 0 && from + c16 < queries) {
-      record[from + c16] = state.m[j];
-      record[queries + from + c16] = sum;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int query = from + 4 * g4 + i;
-      if (query < queries)
-#pragma unroll
-        for (int t = 0; t < F::VT; ++t) record[2 * queries + (int64_t)query * D + F::column(c16, t)] = state.out[j][t][i];
-    }
-  }
+  for (int j = 0; j < N; ++j) write_record<T, D, N>(state, j, 16 * (wave + j * kAttWaves), queries, record, lane);
 }
 
 template <typename T, int D> constexpr size_t shared_lds_bytes() { return sizeof(Staged<T, D>) > merge_bytes(D) ? sizeof(Staged<T, D>) : merge_bytes(D); }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArgs a, const T* __restrict__ Q) {
+// A sequence's own rows: a wave has every own_parts-th step of a unit.  (Nothing here depends on what other sequences hold: to find a place among them
+// by their rows, as the prompts' pieces do, took longer than the rows.)
+template <typename T, int D> __device__ __forceinline__ void own_part(const SharedArgs& a, const T* Q, int64_t wave) {
   typedef Form<T, D> F;
-  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4, L = a.own.L, H = a.own.H, G = a.G, parts = a.own_parts;
+  const int u = uniform((int)(wave / parts)), part = uniform((int)(wave - (int64_t)u * parts));
+  if (u >= a.own.B * L * H) return;
+  const int b = u / (L * H), in = u - b * L * H, rows = uniform(rows_of(a.own, b, in / H));
+  const int n = (steps_in<F::kRows>(rows) - part + parts - 1) / parts;
+  if (n <= 0) return;
+  const int32_t* const table = a.own.table + b * a.own.table_b + (int64_t)in * a.own.max_pages;
+  typename F::Queries q[1];
+  F::queries(Q + ((int64_t)u * G + min(c16, G - 1)) * D, c16 < G, g4, q[0]);
+  if (a.scale.negate) F::negate(q[0]);
+  State<T, D, 1> state;
+  walk<T, D>(state, q, static_cast<const T*>(a.own.K), static_cast<const T*>(a.own.V), n, a.scale, lane,
+             [&](int i, int r) { return table[a.own.pages.of(min((part + i * parts) * F::kRows + r, rows - 1))]; },
+             [&](int page, int i, int r) {
+               const int row = (part + i * parts) * F::kRows + r;
+               return row < rows && page >= 0 && page < a.own.num_pages
+                          ? (uint32_t)page * (uint32_t)a.own.page_size + (uint32_t)(row - a.own.pages.of(row) * a.own.page_size) : kNoRow;
+             });
+  write_record<T, D, 1>(state, 0, 0, G, a.own_records + wave * record_floats(G, D), lane);
+}
+
+// A piece of a prompt's rows for up to 128 queries of its sequences.  Pieces are as long as each other, whatever the layers hold: every wave finds out
+// by itself how many pieces the layers before make.
+template <typename T, int D> __device__ __forceinline__ void common_piece(const SharedArgs& a, const T* Q, int w, unsigned char* lds) {
+  typedef Form<T, D> F;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4, wave = uniform(threadIdx.x >> 6);
-  const int L = a.own.L, H = a.own.H, G = a.G, shared = a.common.B * L, entries = shared + a.own.B * L;
-  // every wave finds out which piece is its workgroup's
-  int64_t total = 0;
-  for (int e0 = 0; e0 < entries; e0 += 64) {
-    if (e0 + lane < entries) {
-      const Entry x = entry_at(a, e0 + lane);
-      total += (int64_t)steps_in<F::kRows>(x.rows) * x.times;
-    }
+  const int L = a.own.L, H = a.own.H, G = a.G, entries = a.common.B * L;
+  if (entries == 0) return;
+  const Entry front = entry_at(a, lane, entries);          // (mostly all)
+  int64_t total = (int64_t)steps_in<F::kRows>(front.rows) * front.times;
+  int units = front.rows > 0 ? front.times : 0;
+  for (int e0 = 64; e0 < entries; e0 += 64) {
+    const Entry x = entry_at(a, e0 + lane, entries);
+    total += (int64_t)steps_in<F::kRows>(x.rows) * x.times;
+    units += x.rows > 0 ? x.times : 0;
   }
   total = wave_sum(total);
-  const int each = (int)max((int64_t)kLeastSteps, (total + a.groups - 1) / a.groups);
-  const int64_t w = blockIdx.x;
-  int64_t before = 0, before_own = 0;
-  int entry = -1, rows = 0, pieces = 0;
-  int64_t place = 0;
+  units = (int)wave_sum(units);
+  // a unit's last piece is part of one: as many pieces as are resident together, with one for each unit among them; of more units than that twice as many
+  // as units at most
+  const int64_t aim = max(a.groups - units, (units + 1) / 2);
+  const int each = (int)max((int64_t)kLeastSteps, (total + aim - 1) / max(aim, (int64_t)1));
+  int before = 0, entry = -1, rows = 0, pieces = 0, place = 0;     // (all pieces are fewer than most_common, below 2^31, unless starts fall)
   for (int e0 = 0; e0 < entries && entry < 0; e0 += 64) {
-    Entry x{0, 0};
-    if (e0 + lane < entries) x = entry_at(a, e0 + lane);
-    const int mine = (steps_in<F::kRows>(x.rows) + each - 1) / each;
-    const int64_t upto = before + wave_scan((int64_t)mine * x.times, lane);
-    // (records of sequences are counted from the first of them on)
-    const uint64_t first_own = __ballot(e0 + lane >= shared);
-    if (e0 < shared && first_own) before_own = __shfl(upto - (int64_t)mine * x.times, __builtin_ctzll(first_own), 64);
-    if (e0 == shared) before_own = before;
+    const Entry x = e0 == 0 ? front : entry_at(a, e0 + lane, entries);
+    const int mine = (steps_in<F::kRows>(x.rows) + each - 1) / each, all = mine * x.times, upto = before + wave_scan(all);
     const uint64_t past = __ballot(upto > w);
     if (past) {
       const int from = __builtin_ctzll(past);
       entry = e0 + from;
       rows = __builtin_amdgcn_readlane(x.rows, from);
       pieces = __builtin_amdgcn_readlane(mine, from);
-      place = w - __shfl(upto - (int64_t)mine * x.times, from, 64);
+      place = w - __builtin_amdgcn_readlane(upto - all, from);
     }
-    before = __shfl(upto, 63, 64);
+    before = __builtin_amdgcn_readlane(upto, 63);
   }
   if (entry < 0) return;
-  const bool is_own = entry >= shared;
-  const int64_t index = is_own ? w - before_own : w;
-  if (index >= (is_own ? a.most_own : a.most_common)) return;
-  if (place == 0 && threadIdx.x == 0) a.span[entry] = int2{(int)index, pieces};
-  const int unit = uniform((int)(place / pieces)), piece = uniform((int)(place - (int64_t)unit * pieces));
+  if (place == 0 && threadIdx.x == 0) a.span[entry] = int2{w, pieces};
+  const int unit = place / pieces, piece = place - unit * pieces;
   // the unit's head, and the tile's queries
-  const int seq = is_own ? (entry - shared) / L : entry / L, l = (is_own ? entry - shared : entry) - seq * L;
-  int h = unit, first = seq, queries = G, tile = 0;
-  if (!is_own) {
-    const Run run = run_of(a, seq);
-    const int tiles = tiles_of(a, run.n);
-    h = unit / tiles;
-    tile = unit - h * tiles;
-    first = run.first;
-    queries = min(kTileQueries, run.n * G - tile * kTileQueries);
-  }
-  const PagedArgs& kv = is_own ? a.own : a.common;
-  const int32_t* const table = kv.table + seq * kv.table_b + ((int64_t)l * H + h) * kv.max_pages;
-  const int page_size = kv.page_size;
-  const int64_t num_pages = kv.num_pages;
+  const int p = entry / L, l = entry - p * L;
+  const Run run = run_of(a, p);
+  const int tiles = tiles_of(a, run.n), h = unit / tiles, tile = unit - h * tiles, queries = min(kTileQueries, run.n * G - tile * kTileQueries);
+  const PagedArgs& kv = a.common;
+  const int32_t* const table = kv.table + p * kv.table_b + ((int64_t)l * H + h) * kv.max_pages;
   const T* const K = static_cast<const T*>(kv.K);
   const T* const V = static_cast<const T*>(kv.V);
   auto place_of = [&](int row) -> uint32_t {
     if (row >= rows) return kNoRow;
-    const int p = kv.pages.of(row), page = table[p];
-    return page >= 0 && page < num_pages ? (uint32_t)page * (uint32_t)page_size + (uint32_t)(row - p * page_size) : kNoRow;
+    const int at = kv.pages.of(row), page = table[at];
+    return page >= 0 && page < kv.num_pages ? (uint32_t)page * (uint32_t)kv.page_size + (uint32_t)(row - at * kv.page_size) : kNoRow;
   };
   // query c16 of a tile of 16
   auto load_queries = [&](int from, typename F::Queries& q) {
     const bool has = from + c16 < queries;
-    const int r = tile * kTileQueries + from + c16, b = has ? first + r / G : first, g = has ? r % G : 0;
+    const int r = tile * kTileQueries + from + c16, b = has ? run.first + r / G : run.first, g = has ? r % G : 0;
     F::queries(Q + (((int64_t)b * L + l) * H * G + (int64_t)h * G + g) * D, has, g4, q);
     if (a.scale.negate) F::negate(q);
   };
-  float* const record = is_own ? a.own_records + index * record_floats(G, D) : a.common_records + index * record_floats(kTileQueries, D);
-  const int steps = steps_in<F::kRows>(rows);
+  float* const record = a.common_records + w * record_floats(kTileQueries, D);
+  const int steps = steps_in<F::kRows>(rows), s0 = (int)((int64_t)steps * piece / pieces), s1 = (int)((int64_t)steps * (piece + 1) / pieces);
   if (queries <= 16) {
-    typename F::Queries q;
-    load_queries(0, q);
-    const int share = pieces * kAttWaves, id = piece * kAttWaves + wave;
+    typename F::Queries q[1];
+    load_queries(0, q[0]);
     State<T, D, 1> state;
-    const int s0 = (int)((int64_t)steps * id / share), s1 = (int)((int64_t)steps * (id + 1) / share);
-    walk<T, D>(state, q, K, V, s1 - s0, a.scale, lane, [&](int i, int r) { return table[kv.pages.of(min((s0 + i) * F::kRows + r, rows - 1))]; },
+    // the waves take the piece's steps in turn
+    walk<T, D>(state, q, K, V, (s1 - s0 - wave + kAttWaves - 1) / kAttWaves, a.scale, lane,
+               [&](int i, int r) { return table[kv.pages.of(min((s0 + wave + i * kAttWaves) * F::kRows + r, rows - 1))]; },
                [&](int page, int i, int r) {
-                 const int row = (s0 + i) * F::kRows + r;
-                 return row < rows && page >= 0 && page < num_pages ? (uint32_t)page * (uint32_t)page_size + (uint32_t)(row - kv.pages.of(row) * page_size) : kNoRow;
+                 const int row = (s0 + wave + i * kAttWaves) * F::kRows + r;
+                 return row < rows && page >= 0 && page < kv.num_pages
+                            ? (uint32_t)page * (uint32_t)kv.page_size + (uint32_t)(row - kv.pages.of(row) * kv.page_size) : kNoRow;
                });
     merge_waves<T, D>(state, queries, reinterpret_cast<float*>(lds), record, nullptr);
-    return;
+  } else if (queries <= 64) {
+    wide_piece<T, D, 1>(lds, K, V, s0, s1, queries, a.scale, record, place_of, load_queries);
+  } else {
+    wide_piece<T, D, 2>(lds, K, V, s0, s1, queries, a.scale, record, place_of, load_queries);
   }
-  const int s0 = (int)((int64_t)steps * piece / pieces), s1 = (int)((int64_t)steps * (piece + 1) / pieces);
-  if (queries <= 64) wide_piece<T, D, 1>(lds, K, V, s0, s1, queries, a.scale, record, place_of, load_queries);
-  else wide_piece<T, D, 2>(lds, K, V, s0, s1, queries, a.scale, record, place_of, load_queries);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArgs a, const T* __restrict__ Q) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  if ((int)blockIdx.x < a.most_common) common_piece<T, D>(a, Q, blockIdx.x, lds);
+  else own_part<T, D>(a, Q, (int64_t)((int)blockIdx.x - a.most_common) * kAttWaves + uniform(threadIdx.x >> 6));
 }
 
 // A workgroup a unit of a sequence: the records of the prompt's pieces and of its own, in order; threads as in chosen_merge_kernel.
@@ -785,7 +860,6 @@ template <int D> __global__ __launch_bounds__(1024) void shared_merge_kernel(Sha
   const int b = u / (L * H), l = u / H % L, h = u % H, items = G * (D / 4);
   const int per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = threadIdx.x - slot * per_slot, g = item / (D / 4), c4 = item % (D / 4);
   const int own_rows = rows_of(a.own, b, l);
-  const int2 own_span = a.span[(P + b) * L + l];
   int p = -1;
   for (int p0 = 0; p0 < P && p < 0; p0 += 64) {
     bool mine = false;
@@ -803,13 +877,13 @@ template <int D> __global__ __launch_bounds__(1024) void shared_merge_kernel(Sha
     const Run run = run_of(a, p);
     const int tiles = tiles_of(a, run.n), at = (b - run.first) * G + g, tile = at / kTileQueries;
     const int64_t index = span.x + (int64_t)(h * tiles + tile) * span.y, size = record_floats(kTileQueries, D);
-    if (item < items && rows > 0 && span.x >= 0 && span.y > 0 && index + span.y <= a.most_common)
+    if (item < items && rows > 0 && span.x >= 0 && span.y > 0 && index >= 0 && index + span.y <= a.most_common)
       part.join_records<D>(a.common_records + index * size, slot, span.y, slots, size, min(kTileQueries, run.n * G - tile * kTileQueries),
                            at - tile * kTileQueries, c4);
   }
-  const int64_t index = own_span.x + (int64_t)h * own_span.y, size = record_floats(G, D);
-  if (item < items && own_rows > 0 && own_span.x >= 0 && own_span.y > 0 && index + own_span.y <= a.most_own)
-    part.join_records<D>(a.own_records + index * size, slot, own_span.y, slots, size, G, g, c4);
+  const int64_t size = record_floats(G, D);
+  if (item < items)
+    part.join_records<D>(a.own_records + (int64_t)u * a.own_parts * size, slot, min(a.own_parts, (own_rows + a.step_rows - 1) / a.step_rows), slots, size, G, g, c4);
   finish_parts(part, slots, item, items, slot, joined, a.out + (int64_t)u * G * D);
 }
 
@@ -834,13 +908,19 @@ int64_t most_tiles(int P, int B, int G) {
 }
 
 struct SharedSizes {
+  int groups, own_parts;
   int64_t common, own, span, total;    // records, entries, bytes
 };
-SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d) {
+SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d, int dtype) {
   SharedSizes z;
-  z.common = kGroups + (int64_t)L * H * most_tiles(P, B, G);
-  z.own = kGroups + (int64_t)L * H * B;
-  z.span = (int64_t)(P + B) * L;
+  const int64_t units = (int64_t)B * L * H;
+  // pieces of prompts: as many workgroups as are resident together; of sequences: as many waves, 16 of a unit at most
+  z.groups = d == 64 ? 768 : 512;
+  z.own_parts = (int)std::max<int64_t>(1, std::min<int64_t>(16, 2048 / units));
+  const int64_t tiles = (int64_t)L * H * most_tiles(P, B, G);
+  z.common = P ? std::max<int64_t>(z.groups, tiles + tiles / 2 + 1) + 1 : 0;
+  z.own = units * z.own_parts;
+  z.span = (int64_t)P * L;
   z.total = (z.common * record_floats(kTileQueries, d) + z.own * record_floats(G, d)) * (int64_t)sizeof(float) + z.span * (int64_t)sizeof(int2);
   return z;
 }
@@ -894,20 +974,20 @@ hipError_t attend_chosen_launch(const void* Q, int group, const fc_paged_kv& kv,
 }
 
 size_t attend_shared_workspace_bytes(int P, int B, int L, int H, int group, int d, int dtype) {
-  (void)dtype;
-  return (size_t)shared_sizes(P, B, L, H, group, d).total; }
+  return (size_t)shared_sizes(P, B, L, H, group, d, dtype).total;
+}
 
 hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& common, const int32_t* starts, const fc_paged_kv& own, float scale, float* out, void* ws,
                                 hipStream_t s) {
   const int P = common.batch, B = own.batch, L = own.layers, H = own.kv_heads, d = own.head_dim;
-  const SharedSizes z = shared_sizes(P, B, L, H, group, d);
+  const SharedSizes z = shared_sizes(P, B, L, H, group, d, own.dtype);
   float* const records = static_cast<float*>(ws);
   float* const own_records = records + z.common * record_floats(kTileQueries, d);
-  SharedArgs a{paged_args(common), paged_args(own), starts, group, kGroups, z.common, z.own, scale_of(scale), records, own_records,
+  SharedArgs a{paged_args(common), paged_args(own), starts, group, z.groups, (int)z.common, z.own_parts, own.dtype == FC_BF16 ? 32 : 16, scale_of(scale), records, own_records,
                reinterpret_cast<int2*>(own_records + z.own * record_floats(group, d)), out};
   {
     ProfileScope ps("attend_shared_kernel", s);
-    const int64_t groups = kGroups + (int64_t)L * H * (most_tiles(P, B, group) + B);
+    const int64_t groups = z.common + (z.own + kAttWaves - 1) / kAttWaves;
     auto launch = [&](auto kern, size_t lds, auto type) {
       typedef decltype(type) T;
       hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAttThreads), lds, s, a, static_cast<const T*>(Q));
@@ -922,7 +1002,7 @@ hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& com
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ProfileScope ps("shared_merge_kernel", s);
-  const MergeShape m = merge_shape(B * L * H, std::max(1, kGroups / (L * H)), group, d);
+  const MergeShape m = merge_shape(B * L * H, std::max(P ? z.groups / (L * H) : 1, z.own_parts), group, d);
   auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(B * L * H), dim3(m.threads), m.lds, s, a, m.slots); };
   d == 128 ? launch(shared_merge_kernel<128>) : launch(shared_merge_kernel<64>);
   return hipGetLastError();
