@@ -131,20 +131,23 @@ template <int D> struct Form<uint16_t, D> {
       }
     }
   }
-  // of N tiles of queries that read the same rows
-  template <int N> static __device__ __forceinline__ void add(const Weights (&p)[N], const Values& x, float4v (&out)[N][VT]) {
+  // V's columns as the product takes them
+  struct Operands { bf16x8 v[VT]; };
+  static __device__ __forceinline__ void operands(const Values& x, Operands& o) {
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       const uint32_t sel = (t & 1) ? 0x07060302u : 0x05040100u;
       const int w = t >> 1;
       auto two = [&](int tile, int i) { return __builtin_amdgcn_perm(x.w[tile][i + 1][w], x.w[tile][i][w], sel); };
-      const bf16x8 v = as_bf16x8(two(0, 0), two(0, 2), two(1, 0), two(1, 2));
-#pragma unroll
-      for (int n = 0; n < 3; ++n)
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          out[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(p[j].term[n][0], p[j].term[n][1], p[j].term[n][2], p[j].term[n][3]), v, out[j][t], 0, 0, 0);
+      o.v[t] = as_bf16x8(two(0, 0), two(0, 2), two(1, 0), two(1, 2));
     }
+  }
+  static __device__ __forceinline__ void add(const Weights& p, const Operands& x, float4v (&out)[VT]) {
+#pragma unroll
+    for (int n = 0; n < 3; ++n)
+#pragma unroll
+      for (int t = 0; t < VT; ++t)
+        out[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(p.term[n][0], p.term[n][1], p.term[n][2], p.term[n][3]), x.v[t], out[t], 0, 0, 0);
   }
   // ... from LDS, 16 bytes of a row a place: K's places are swapped within a row by its number, or the 16 lanes of a read would meet in the same banks
   static constexpr int kPieces = D / 8;
@@ -232,13 +235,13 @@ template <int D> struct Form<float, D> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w.p[i] = p[0][i];
   }
-  template <int N> static __device__ __forceinline__ void add(const Weights (&p)[N], const Values& x, float4v (&out)[N][VT]) {
+  typedef Values Operands;
+  static __device__ __forceinline__ void operands(const Values& x, Operands& o) { o = x; }
+  static __device__ __forceinline__ void add(const Weights& p, const Operands& x, float4v (&out)[VT]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int t = 0; t < VT; ++t)
-#pragma unroll
-        for (int j = 0; j < N; ++j) out[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[j].p[i], x.w[0][i][t], out[j][t], 0, 0, 0);
+      for (int t = 0; t < VT; ++t) out[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(p.p[i], x.w[0][i][t], out[t], 0, 0, 0);
   }
   static constexpr int kPieces = D / 4;
   static __device__ __forceinline__ int k_place(int row, int piece) { return row * kPieces + (piece ^ row); }      // (16 rows)
@@ -264,7 +267,7 @@ template <int D> struct Form<float, D> {
   }
 };
 
-// The scale of scores in log2 units, above 0 or 0 (queries change their signs for a negative one), and how scores are compared with a reference.
+// The scale of scores in log2 units, above 0 (queries change their signs for a negative one), and how scores are compared with a reference.
 struct Scale {
   float log2e, inverse;
   bool negate;
@@ -286,24 +289,20 @@ template <typename T, int D, int N> struct State {
       for (int t = 0; t < F::VT; ++t) out[j][t] = float4v{0.f, 0.f, 0.f, 0.f};
     }
   }
-  // `there`: the step's rows that there are, a bit each
-  __device__ __forceinline__ void weigh(int j, const float4v (&acc)[F::kTiles], uint32_t there, const Scale& scale, int g4, typename F::Weights& w) {
-    float p[F::kTiles][4];
-    float mx = -INFINITY;
-#pragma unroll
-    for (int tt = 0; tt < F::kTiles; ++tt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[tt][i] = acc[tt][i];
+  // A step's products of K and queries: those of rows that are not there (`there`: a bit each for those that are) are left out, and the reference is moved
+  // if one exceeds it.
+  __device__ __forceinline__ void refer(int j, float4v (&acc)[F::kTiles], uint32_t there, const Scale& scale, int g4) {
     if (there != kAll)
 #pragma unroll
       for (int tt = 0; tt < F::kTiles; ++tt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!((there >> (16 * tt + 4 * g4 + i)) & 1u)) p[tt][i] = -INFINITY;
+          if (!((there >> (16 * tt + 4 * g4 + i)) & 1u)) acc[tt][i] = -INFINITY;
+    float mx = -INFINITY;
 #pragma unroll
     for (int tt = 0; tt < F::kTiles; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, p[tt][i]);
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, acc[tt][i]);
     if (__any(mx > limit[j])) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -320,17 +319,14 @@ template <typename T, int D, int N> struct State {
         for (int t = 0; t < F::VT; ++t) out[j][t][i] *= a;
       }
     }
+  }
+  // ... as weights
+  __device__ __forceinline__ void weigh(int j, const float4v (&acc)[F::kTiles], const Scale& scale, typename F::Weights& w) {
+    float p[F::kTiles][4], more = 0.f;
 #pragma unroll
     for (int tt = 0; tt < F::kTiles; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[tt][i] = __builtin_amdgcn_exp2f(fmaf(p[tt][i], scale.log2e, -shift[j]));
-    if (there != kAll)                                     // (a scale of 0 would make a number of what is not there)
-#pragma unroll
-      for (int tt = 0; tt < F::kTiles; ++tt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!((there >> (16 * tt + 4 * g4 + i)) & 1u)) p[tt][i] = 0.f;
-    float more = 0.f;
+      for (int i = 0; i < 4; ++i) p[tt][i] = __builtin_amdgcn_exp2f(fmaf(acc[tt][i], scale.log2e, -shift[j]));
 #pragma unroll
     for (int tt = 0; tt < F::kTiles; ++tt)
 #pragma unroll
@@ -388,11 +384,14 @@ __device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<
   if (n > 1) ask(1, xb);
   auto turn = [&](int st, Step& x) {
     if (x.there) {
-      typename F::Weights w[1];
       float4v acc[1][F::kTiles];
       F::template scores<1>(q, x.k, acc);
-      state.weigh(0, acc[0], x.there, scale, g4, w[0]);
-      F::template add<1>(w, x.v, state.out);
+      state.refer(0, acc[0], x.there, scale, g4);
+      typename F::Weights w;
+      state.weigh(0, acc[0], scale, w);
+      typename F::Operands v;
+      F::operands(x.v, v);
+      F::add(w, v, state.out[0]);
     }
     if (st + 2 < n) ask(st + 2, x);
   };
@@ -728,10 +727,18 @@ __device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, in
         asm volatile("" ::: "memory");                     // (both are on the way before the products begin)
         float4v acc[N][F::kTiles];
         F::template scores<N>(q, k, acc);
-        typename F::Weights w[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) state.weigh(j, acc[j], there, scale, g4, w[j]);
-        F::template add<N>(w, v, state.out);
+        for (int j = 0; j < N; ++j) state.refer(j, acc[j], there, scale, g4);
+        typename F::Operands o;
+        F::operands(v, o);
+        // a tile's products beside the next one's weights
+        typename F::Weights w[N];
+        state.weigh(0, acc[0], scale, w[0]);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          if (j + 1 < N) state.weigh(j + 1, acc[j + 1], scale, w[j + 1]);
+          F::add(w[j], o, state.out[j]);
+        }
       }
     }
   }
@@ -897,7 +904,7 @@ MergeShape merge_shape(int units, int records, int G, int d) {
 }
 
 Scale scale_of(float scale) {
-  const float s = fabsf(scale) * 1.4426950408889634f;
+  const float s = fmaxf(fabsf(scale) * 1.4426950408889634f, 1.17549435e-38f);    // (0 would make a number of what is not there)
   return Scale{s, 1.f / s, scale < 0.f};
 }
 
