@@ -724,7 +724,6 @@ __device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, in
         typename F::Values v;
         F::read(s.k[stage], c16, g4, k);
         F::read(s.v[stage], c16, g4, v);
-        asm volatile("" ::: "memory");                     // (both are on the way before the products begin)
         float4v acc[N][F::kTiles];
         F::template scores<N>(q, k, acc);
 #pragma unroll
@@ -921,9 +920,9 @@ struct SharedSizes {
 SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d, int dtype) {
   SharedSizes z;
   const int64_t units = (int64_t)B * L * H;
-  // pieces of prompts: as many workgroups as are resident together; of sequences: as many waves, 16 of a unit at most
+  // pieces of prompts: as many workgroups as are resident together; of sequences: parts for four times as many waves, 16 of a unit at most
   z.groups = d == 64 ? 768 : 512;
-  z.own_parts = (int)std::max<int64_t>(1, std::min<int64_t>(16, 2048 / units));
+  z.own_parts = (int)std::max<int64_t>(1, std::min<int64_t>(16, 8192 / units));
   const int64_t tiles = (int64_t)L * H * most_tiles(P, B, G);
   z.common = P ? std::max<int64_t>(z.groups, tiles + tiles / 2 + 1) + 1 : 0;
   z.own = units * z.own_parts;
@@ -990,11 +989,17 @@ hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& com
   const SharedSizes z = shared_sizes(P, B, L, H, group, d, own.dtype);
   float* const records = static_cast<float*>(ws);
   float* const own_records = records + z.common * record_floats(kTileQueries, d);
-  SharedArgs a{paged_args(common), paged_args(own), starts, group, z.groups, (int)z.common, z.own_parts, own.dtype == FC_BF16 ? 32 : 16, scale_of(scale), records, own_records,
+  // ... for as many waves as are resident together, and where units are more, parts of four steps by what the tables reach: sequences hold different
+  // numbers of rows, which shorter parts even out (432 units of up to 700 fp32 rows in 4 parts 94 us, in 11 89; 32 units of up to 256 bf16 rows in 2 parts 16.2,
+  // in 10 13.2)
+  const int step_rows = own.dtype == FC_BF16 ? 32 : 16;
+  const int64_t units = (int64_t)B * L * H, reach = (int64_t)own.max_pages * own.page_size / step_rows;
+  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(z.own_parts, std::max(std::min(2048 / units, reach), reach / 4)));
+  SharedArgs a{paged_args(common), paged_args(own), starts, group, z.groups, (int)z.common, parts, step_rows, scale_of(scale), records, own_records,
                reinterpret_cast<int2*>(own_records + z.own * record_floats(group, d)), out};
   {
     ProfileScope ps("attend_shared_kernel", s);
-    const int64_t groups = z.common + (z.own + kAttWaves - 1) / kAttWaves;
+    const int64_t groups = z.common + (units * parts + kAttWaves - 1) / kAttWaves;
     auto launch = [&](auto kern, size_t lds, auto type) {
       typedef decltype(type) T;
       hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAttThreads), lds, s, a, static_cast<const T*>(Q));
@@ -1009,7 +1014,7 @@ hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& com
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ProfileScope ps("shared_merge_kernel", s);
-  const MergeShape m = merge_shape(B * L * H, std::max(P ? z.groups / (L * H) : 1, z.own_parts), group, d);
+  const MergeShape m = merge_shape(B * L * H, std::max(P ? z.groups / (L * H) : 1, parts), group, d);
   auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(B * L * H), dim3(m.threads), m.lds, s, a, m.slots); };
   d == 128 ? launch(shared_merge_kernel<128>) : launch(shared_merge_kernel<64>);
   return hipGetLastError();
