@@ -508,9 +508,17 @@ struct Part {
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = o[i] * w1 + o2[i] * w2;
   }
-  // records from, from + step, ... below end at `base`, each of `queries` rows, `size` floats; kAtOnce of them under way
+  // records from, from + step, ... below end at `base`, each of `queries` rows, `size` floats; as many under way as there are, up to eight
   template <int D> __device__ __forceinline__ void join_records(const float* base, int from, int end, int step, int64_t size, int queries, int row, int c4) {
-    constexpr int kAtOnce = 8;
+    const int n = end - from;
+    if (n <= 0) return;
+    if (n <= step) join_some<D, 1>(base, from, end, step, size, queries, row, c4);
+    else if (n <= 2 * step) join_some<D, 2>(base, from, end, step, size, queries, row, c4);
+    else if (n <= 4 * step) join_some<D, 4>(base, from, end, step, size, queries, row, c4);
+    else join_some<D, 8>(base, from, end, step, size, queries, row, c4);
+  }
+  template <int D, int kAtOnce>
+  __device__ __forceinline__ void join_some(const float* base, int from, int end, int step, int64_t size, int queries, int row, int c4) {
     for (int k0 = from; k0 < end; k0 += kAtOnce * step) {
       float ms[kAtOnce], sums[kAtOnce];
       float4v os[kAtOnce];
@@ -866,24 +874,27 @@ template <int D> __global__ __launch_bounds__(1024) void shared_merge_kernel(Sha
   const int b = u / (L * H), l = u / H % L, h = u % H, items = G * (D / 4);
   const int per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = threadIdx.x - slot * per_slot, g = item / (D / 4), c4 = item % (D / 4);
   const int own_rows = rows_of(a.own, b, l);
-  int p = -1;
-  for (int p0 = 0; p0 < P && p < 0; p0 += 64) {
-    bool mine = false;
-    if (p0 + lane < P) {
-      const Run run = run_of(a, p0 + lane);
-      mine = b >= run.first && b < run.first + run.n;
+  // the prompt whose sequence this is, with what its layer holds: 64 prompts' together, a lane each, in one wait for memory
+  Run run{0, 0};
+  int2 span{0, 0};
+  for (int p0 = 0; p0 < P; p0 += 64) {
+    const int mine = min(p0 + lane, P - 1);
+    const Run r = run_of(a, mine);
+    const int rows = rows_of(a.common, mine, l);
+    const int2 s = a.span[mine * L + l];
+    const uint64_t found = __ballot(p0 + lane < P && b >= r.first && b < r.first + r.n);
+    if (found) {
+      const int from = __builtin_ctzll(found);
+      run = Run{__builtin_amdgcn_readlane(r.first, from), __builtin_amdgcn_readlane(r.n, from)};
+      if (__builtin_amdgcn_readlane(rows, from) > 0) span = int2{__builtin_amdgcn_readlane(s.x, from), __builtin_amdgcn_readlane(s.y, from)};
+      break;
     }
-    const uint64_t found = __ballot(mine);
-    if (found) p = p0 + __builtin_ctzll(found);
   }
   Part part;
-  if (p >= 0) {
-    const int rows = rows_of(a.common, p, l);
-    const int2 span = a.span[p * L + l];
-    const Run run = run_of(a, p);
+  if (span.y > 0 && span.x >= 0) {
     const int tiles = tiles_of(a, run.n), at = (b - run.first) * G + g, tile = at / kTileQueries;
     const int64_t index = span.x + (int64_t)(h * tiles + tile) * span.y, size = record_floats(kTileQueries, D);
-    if (item < items && rows > 0 && span.x >= 0 && span.y > 0 && index >= 0 && index + span.y <= a.most_common)
+    if (item < items && index + span.y <= a.most_common)
       part.join_records<D>(a.common_records + index * size, slot, span.y, slots, size, min(kTileQueries, run.n * G - tile * kTileQueries),
                            at - tile * kTileQueries, c4);
   }
