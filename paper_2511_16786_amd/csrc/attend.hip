@@ -63,6 +63,8 @@ __device__ __forceinline__ float less_high(float x, uint32_t two) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, c), x, false);
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// Past the last-level cache: for V's rows, whole lines at a time.  A load of K takes half a line of each of 16 rows, and the other half is to be there for
+// the next one (64 pages of 28 layers: both past it 46.9 us, V alone 44.9, neither 50.0; 26 small pages of 8 x 28 39.3 / 36.4 / 42.2).
 template <typename V> __device__ __forceinline__ V load_past(const void* p) { return __builtin_nontemporal_load(static_cast<const V*>(p)); }
 
 // The 16 queries of a tile as the score product takes them, and 16 or 32 rows (a step) of K and V as both products take them.
@@ -88,7 +90,7 @@ template <int D> struct Form<uint16_t, D> {
     const uint16_t* const p = base + row * D + 8 * g4;
 #pragma unroll
     for (int i = 0; i < KW / 4; ++i) {
-      const u32x4 u = load_past<u32x4>(p + 32 * i);
+      const u32x4 u = *reinterpret_cast<const u32x4*>(p + 32 * i);
       x.w[tile][4 * i] = u.x; x.w[tile][4 * i + 1] = u.y; x.w[tile][4 * i + 2] = u.z; x.w[tile][4 * i + 3] = u.w;
     }
   }
@@ -203,7 +205,7 @@ template <int D> struct Form<float, D> {
     const float* const p = base + row * D + 4 * g4;
 #pragma unroll
     for (int j = 0; j < KW / 4; ++j) {
-      const float4v u = load_past<float4v>(p + 16 * j);
+      const float4v u = *reinterpret_cast<const float4v*>(p + 16 * j);
       x.w[tile][4 * j] = u.x; x.w[tile][4 * j + 1] = u.y; x.w[tile][4 * j + 2] = u.z; x.w[tile][4 * j + 3] = u.w;
     }
   }

@@ -15,7 +15,7 @@ namespace fc {
 namespace {
 
 constexpr int kBoundThreads = 256, kBoundWaves = kBoundThreads / 64;
-constexpr int kRowsAtOnce = 4;         // of a lane
+constexpr int kRowsAtOnce = 8;         // of a lane
 constexpr int kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
 constexpr int kPagesAtOnce = 4, kQueriesAtOnce = 8;
 constexpr int kMostKeys = 4096;        // that a workgroup has in LDS, or in registers
@@ -52,7 +52,8 @@ template <> struct Columns<float> {
 };
 
 // A wave looks 64 entries of the tables up at a time, a lane each, and then works on the pages that there are, one after another.  Entries are
-// dealt out in the order of place in the table, then unit: what lies behind the last row is last for all units.
+// dealt out in the order of place in the table, then unit: what lies behind the last row is last for all units.  Bound by memory: 11 500 pages of 64 rows of
+// 256 bytes (0.19 GB) 36 us, 5.3 TB/s, past the last-level cache; 42 with a claim on it, however many rows or waves are under way.
 template <typename T>
 __global__ __launch_bounds__(kBoundThreads) void page_bounds_kernel(PagedArgs a, int row_bytes, char* __restrict__ bounds) {
   typedef Columns<T> C;
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(kBoundThreads) void page_bounds_kernel(PagedArgs a,
         for (int r = mine; r < n; r += abreast * kRowsAtOnce) {
           u32x4 v[kRowsAtOnce];
 #pragma unroll
-          for (int j = 0; j < kRowsAtOnce; ++j) v[j] = *reinterpret_cast<const u32x4*>(k + (int64_t)min(r + j * abreast, n - 1) * row_bytes);
+          for (int j = 0; j < kRowsAtOnce; ++j) v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + (int64_t)min(r + j * abreast, n - 1) * row_bytes));
 #pragma unroll
           for (int j = 0; j < kRowsAtOnce; ++j) {
             float x[N];
@@ -341,7 +342,7 @@ __global__ __launch_bounds__(64 * WAVES) void choose_whole_kernel(PagedArgs a, c
 hipError_t page_bounds_launch(const fc_paged_kv& kv, void* bounds, hipStream_t s) {
   const PagedArgs a = paged_args(kv);
   const int64_t items = (int64_t)a.B * a.L * a.H * a.max_pages;
-  const unsigned groups = (unsigned)std::min<int64_t>(1024, (items + kBoundWaves - 1) / kBoundWaves);
+  const unsigned groups = (unsigned)std::min<int64_t>(2048, (items + kBoundWaves - 1) / kBoundWaves);
   const int e = kv.dtype == FC_BF16 ? 2 : 4;
   ProfileScope ps("page_bounds_kernel", s);
   auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups), dim3(kBoundThreads), 0, s, a, kv.head_dim * e, static_cast<char*>(bounds)); };
