@@ -802,7 +802,14 @@ template <typename T, int D> __device__ __forceinline__ void common_piece(const 
   // a unit's last piece is part of one: as many pieces as are resident together, with one for each unit among them; of more units than that twice as many
   // as units at most
   const int64_t aim = max(a.groups - units, (units + 1) / 2);
-  const int each = (int)max((int64_t)kLeastSteps, (total + aim - 1) / max(aim, (int64_t)1));
+  int each = (int)max((int64_t)kLeastSteps, (total + aim - 1) / max(aim, (int64_t)1));
+  if (entries <= 64)                                       // the shortest that makes as many (units' last pieces are half of one in the mean)
+    for (int least = (int)max((int64_t)kLeastSteps, (total + a.groups - 1) / a.groups); least < each;) {
+      const int middle = (least + each) / 2;
+      const int made = __builtin_amdgcn_readlane(wave_scan((steps_in<F::kRows>(front.rows) + middle - 1) / middle * front.times), 63);
+      if (made <= a.groups) each = middle;
+      else least = middle + 1;
+    }
   int before = 0, entry = -1, rows = 0, pieces = 0, place = 0;     // (all pieces are fewer than most_common, below 2^31, unless starts fall)
   for (int e0 = 0; e0 < entries && entry < 0; e0 += 64) {
     const Entry x = e0 == 0 ? front : entry_at(a, e0 + lane, entries);
@@ -933,8 +940,9 @@ struct SharedSizes {
 SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d, int dtype) {
   SharedSizes z;
   const int64_t units = (int64_t)B * L * H;
-  // pieces of prompts: as many workgroups as are resident together; of sequences: parts for four times as many waves, 16 of a unit at most
-  z.groups = d == 64 ? 768 : 512;
+  // pieces of prompts: nearly as many workgroups as are resident together (two on a compute unit, three of 64 columns; 16 answers to 28 layers: 512 of
+  // them 148 us, 480 138, 448 150); of sequences: parts for four times as many waves, 16 of a unit at most
+  z.groups = d == 64 ? 720 : 480;
   z.own_parts = (int)std::max<int64_t>(1, std::min<int64_t>(16, 8192 / units));
   const int64_t tiles = (int64_t)L * H * most_tiles(P, B, G);
   z.common = P ? std::max<int64_t>(z.groups, tiles + tiles / 2 + 1) + 1 : 0;
