@@ -452,13 +452,13 @@ fc_status flashcache_choose_pages(const void* Q, int32_t q_heads, const fc_paged
  *   Q    device in, [B][L][q_heads][d] in the cache's dtype; out  device out, float [B][L][q_heads][d]
  *   workspace  device, 16-byte aligned, flashcache_decode_chosen_workspace_bytes() bytes (may be 0); one for each call that may run at the same time
  * d in {64, 128}, 1 to 16 query heads a KV head for both dtypes, count * page_size below 2^30.  Products on the matrix cores: of bf16 exact in fp32, with
- * probabilities of 17 bits; of fp32 in fp32.  Sums and softmax in fp32. */
+ * probabilities of 24 bits; of fp32 in fp32.  Sums and softmax in fp32. */
 size_t flashcache_decode_chosen_workspace_bytes(const fc_paged_kv* kv, int32_t q_heads, int32_t count);
 fc_status flashcache_decode_attention_chosen(const void* Q, int32_t q_heads, const fc_paged_kv* kv, const int32_t* chosen, int32_t count, float scale,
                                              float* out, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Decode-step attention of sequences that share the rows of a prompt (several answers to it, for instance): sequence b attends to the rows that
- * common holds for prompt p, where starts[p] <= b < starts[p + 1], and then to its own.  A prompt's rows are read once for up to 16 query heads of its
+ * common holds for prompt p, where starts[p] <= b < starts[p + 1], and then to its own.  A prompt's rows are read once for up to 128 query heads of its
  * sequences together.
  *   Q       device in, [B][L][q_heads][d] in the caches' dtype
  *   common  the prompts' cache, batch = P of them (0 or more); own  the sequences', batch = B; layers, kv_heads, head_dim and dtype are the same in both,

@@ -593,6 +593,7 @@ struct SharedArgs {
   const int32_t* starts;         // [P + 1]
   int G, groups;                 // pieces of prompts that the launch aims at
   int most_common;               // records of prompts that the workspace has, and as many workgroups, the launch's first
+  int record_rows;               // queries that a prompt's record has room for
   int own_parts, step_rows;      // waves of a sequence's unit, each with a record; rows of a step
   Scale scale;
   float* common_records;
@@ -847,7 +848,7 @@ template <typename T, int D> __device__ __forceinline__ void common_piece(const 
     F::queries(Q + (((int64_t)b * L + l) * H * G + (int64_t)h * G + g) * D, has, g4, q);
     if (a.scale.negate) F::negate(q);
   };
-  float* const record = a.common_records + w * record_floats(kTileQueries, D);
+  float* const record = a.common_records + w * record_floats(a.record_rows, D);
   const int steps = steps_in<F::kRows>(rows), s0 = (int)((int64_t)steps * piece / pieces), s1 = (int)((int64_t)steps * (piece + 1) / pieces);
   if (queries <= 16) {
     typename F::Queries q[1];
@@ -902,7 +903,7 @@ template <int D> __global__ __launch_bounds__(1024) void shared_merge_kernel(Sha
   Part part;
   if (span.y > 0 && span.x >= 0) {
     const int tiles = tiles_of(a, run.n), at = (b - run.first) * G + g, tile = at / kTileQueries;
-    const int64_t index = span.x + (int64_t)(h * tiles + tile) * span.y, size = record_floats(kTileQueries, D);
+    const int64_t index = span.x + (int64_t)(h * tiles + tile) * span.y, size = record_floats(a.record_rows, D);
     if (item < items && index + span.y <= a.most_common)
       part.join_records<D>(a.common_records + index * size, slot, span.y, slots, size, min(kTileQueries, run.n * G - tile * kTileQueries),
                            at - tile * kTileQueries, c4);
@@ -934,7 +935,7 @@ int64_t most_tiles(int P, int B, int G) {
 }
 
 struct SharedSizes {
-  int groups, own_parts;
+  int groups, record_rows, own_parts;
   int64_t common, own, span, total;    // records, entries, bytes
 };
 SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d, int dtype) {
@@ -948,7 +949,8 @@ SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d, int dtype) {
   z.common = P ? std::max<int64_t>(z.groups, tiles + tiles / 2 + 1) + 1 : 0;
   z.own = units * z.own_parts;
   z.span = (int64_t)P * L;
-  z.total = (z.common * record_floats(kTileQueries, d) + z.own * record_floats(G, d)) * (int64_t)sizeof(float) + z.span * (int64_t)sizeof(int2);
+  z.record_rows = std::min(kTileQueries, B * G);
+  z.total = (z.common * record_floats(z.record_rows, d) + z.own * record_floats(G, d)) * (int64_t)sizeof(float) + z.span * (int64_t)sizeof(int2);
   return z;
 }
 
@@ -1009,14 +1011,14 @@ hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& com
   const int P = common.batch, B = own.batch, L = own.layers, H = own.kv_heads, d = own.head_dim;
   const SharedSizes z = shared_sizes(P, B, L, H, group, d, own.dtype);
   float* const records = static_cast<float*>(ws);
-  float* const own_records = records + z.common * record_floats(kTileQueries, d);
+  float* const own_records = records + z.common * record_floats(z.record_rows, d);
   // ... for as many waves as are resident together, and where units are more, parts of four steps by what the tables reach: sequences hold different
   // numbers of rows, which shorter parts even out (432 units of up to 700 fp32 rows in 4 parts 94 us, in 11 89; 32 units of up to 256 bf16 rows in 2 parts 16.2,
   // in 10 13.2)
   const int step_rows = own.dtype == FC_BF16 ? 32 : 16;
   const int64_t units = (int64_t)B * L * H, reach = (int64_t)own.max_pages * own.page_size / step_rows;
   const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(z.own_parts, std::max(std::min(2048 / units, reach), reach / 4)));
-  SharedArgs a{paged_args(common), paged_args(own), starts, group, z.groups, (int)z.common, parts, step_rows, scale_of(scale), records, own_records,
+  SharedArgs a{paged_args(common), paged_args(own), starts, group, z.groups, (int)z.common, z.record_rows, parts, step_rows, scale_of(scale), records, own_records,
                reinterpret_cast<int2*>(own_records + z.own * record_floats(group, d)), out};
   {
     ProfileScope ps("attend_shared_kernel", s);

@@ -10,8 +10,8 @@ namespace {
 
 constexpr int kMostPagedRows = (1 << 25) - 1;
 
-// Quotients of numbers below 2^31: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, m d is above 2^(31 + l) by d <= 2^l at most, so that
-// n m / 2^(31 + l) is n / d and less than 2^-31 n / d * 2^l / 2^l beyond: the same whole part.  m has 32 bits for d > 1.
+// Quotients of numbers n below 2^31 by d: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, the product m d is 2^(31 + l) + e with 0 < e <= d <= 2^l,
+// so that n m / 2^(31 + l) = n / d + n e / (d 2^(31 + l)), and what is added is below 1 / d: the same whole part.  m has 32 bits for d > 1.
 struct Divider {
   uint32_t m;
   int shift;                     // l - 1; negative: d is 1

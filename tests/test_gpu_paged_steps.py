@@ -399,6 +399,9 @@ def test_attention_over_chosen_pages(dtype, rows, H, G, d, ps, count, lost):
     ([[129]], [[3]] * 19, [0, 19], 2, 7, 128, 128, 7, 0.1),
     ([[40], [41]], [[3]] * 5, [-7, 2, 99], 1, 2, 64, 1, 16, 0.0),
     ([[9000]], [[3000]] * 2, [0, 2], 1, 5, 128, 64, 16, 0.0),
+    ([[500, 77]], [[9, 0]] * 30, [0, 30], 1, 4, 128, 4, 4, 0.5),
+    ([[500, 77]], [[9, 0]] * 30, [0, 30], 1, 4, 64, 4, 4, 0.5),
+    ([[-3, 90], [41, 17]], [[-1, 8]] * 6, [0, 4, 6], 2, 16, 64, 8, 2, 0.0),
 ])
 def test_attention_to_a_shared_prompt(dtype, common, own, starts, H, G, d, ps, ps_own, lost):
     fc = _fc()
@@ -456,6 +459,59 @@ def test_many_prompts_and_layers():
                 K, V = np.concatenate((k, K)), np.concatenate((v, V))
         return K, V
     _check_attention(fc.decode_attention_shared(Q, cc.kv, _int(starts), co.kv, 0.125), Q, 0.125, _Rows(G, rows_for), "bf16")
+
+
+@pytest.mark.parametrize("dtype,d,B,G,rows", [("bf16", 128, 5, 4, 40000), ("bf16", 64, 20, 6, 70001), ("f32", 128, 9, 8, 20001), ("f32", 64, 6, 3, 33000)])
+def test_long_pieces_of_a_shared_prompt(dtype, d, B, G, rows):
+    """Pieces of more steps than are looked up together (32 units, many rows), against float64 on the GPU."""
+    fc = _fc()
+    dt, L, H, ps = _dt(dtype), 8, 4, 48
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    most = -(-rows // ps)
+    pages = L * H * most + 2
+    K, V = (torch.randn((pages, ps, d), generator=g, device="cuda").to(dt) for _ in "KV")
+    table = torch.randperm(pages, generator=g, device="cuda")[:L * H * most].view(1, L, H, most).to(torch.int32)
+    held = torch.tensor([[rows - 37 * l for l in range(L)]], dtype=torch.int32, device="cuda")
+    own = fc.PagedKV(K, V, torch.zeros((B, L), dtype=torch.int32, device="cuda"), torch.full((B, L, H, 1), -1, dtype=torch.int32, device="cuda"))
+    Q = torch.randn((B, L, H * G, d), generator=g, device="cuda").to(dt)
+    scale = 1.0 / math.sqrt(d)
+    got = fc.decode_attention_shared(Q, fc.PagedKV(K, V, held, table), _int([0, B]), own, scale)
+    for l in range(L):
+        n = int(held[0, l])
+        for h in range(H):
+            j = torch.arange(n, device="cuda")
+            at = table[0, l, h].long()[j // ps] * ps + j % ps
+            k, v = K.view(-1, d)[at].double(), V.view(-1, d)[at].double()
+            q = Q[:, l, h * G:(h + 1) * G].double().reshape(-1, d)
+            logit = q @ k.t().contiguous() * scale
+            p = torch.softmax(logit, 1)
+            want, size = p @ v, p @ v.abs()
+            terms = (q.abs() @ k.abs().t().contiguous()).max() * scale
+            slip = 2 * (d * U * terms + 4 * U * (logit.abs().max() + 1)) + (n / 16 + 64) * U
+            assert bool(((got[:, l, h * G:(h + 1) * G].double().reshape(-1, d) - want).abs() <= slip * size).all())
+
+
+def test_calls_at_once_on_two_streams():
+    """Workspaces of their own, rows beyond the table and below zero."""
+    fc = _fc()
+    rng = np.random.default_rng(51)
+    co, cc = Cache(rng, [[300, -2], [64, 9]], 2, 64, 16, "bf16", most=5), Cache(rng, [[400, 3]], 2, 64, 16, "bf16", most=9)
+    Q = _rand(rng, (2, 2, 6, 64), torch.bfloat16)
+    bounds, starts = fc.page_bounds(co.kv), _int([0, 2])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for s in streams * 3:
+        with torch.cuda.stream(s):
+            chosen = fc.choose_pages(Q, co.kv, bounds, 5, first=0, last=0)
+            outs.append((fc.decode_attention_chosen(Q, co.kv, chosen, 0.2), fc.decode_attention_shared(Q, cc.kv, starts, co.kv, 0.2)))
+    torch.cuda.synchronize()
+
+    def rows_for(b, l, h):
+        return tuple(np.concatenate(x) for x in zip(cc.unit(0, l, h), co.unit(b, l, h)))
+    for a, b in outs:
+        _check_attention(a, Q, 0.2, _Rows(3, co.unit), "bf16")
+        _check_attention(b, Q, 0.2, _Rows(3, rows_for), "bf16")
 
 
 # ---- as they are used -------------------------------------------------------------------------
