@@ -554,37 +554,38 @@ struct Part {
   }
 };
 
-// The parts that a workgroup's `slots` threads of each item have, in order, and the result of the first.
-__device__ __forceinline__ void finish_parts(Part& part, int slots, int item, int items, int slot, float* lds, float* out) {
+// The parts that a workgroup's `slots` threads of each item have, in order, and the result of the first at `out`.
+__device__ __forceinline__ void finish_parts(Part& part, int slots, int per_slot, int slot, bool has, float* lds, float* out) {
   if (slots > 1) {
-    float* const mine = lds + ((int64_t)slot * items + item) * 6;
-    if (slot > 0 && item < items) {
+    float* const mine = lds + threadIdx.x * 6;
+    if (slot > 0 && has) {
       mine[0] = part.m;
       mine[1] = part.sum;
 #pragma unroll
       for (int i = 0; i < 4; ++i) mine[2 + i] = part.o[i];
     }
     __syncthreads();
-    if (slot == 0 && item < items)
+    if (slot == 0 && has)
       for (int j = 1; j < slots; ++j) {
-        const float* const x = mine + (int64_t)j * items * 6;
+        const float* const x = mine + j * per_slot * 6;
         part.join(x[0], x[1], float4v{x[2], x[3], x[4], x[5]});
       }
   }
-  if (slot == 0 && item < items) {
+  if (slot == 0 && has) {
     const float sum = part.sum == 0.f ? 1.f : part.sum;    // (no rows: zeros)
-    *reinterpret_cast<float4v*>(out + 4 * item) = float4v{part.o[0] / sum, part.o[1] / sum, part.o[2] / sum, part.o[3] / sum};
+    *reinterpret_cast<float4v*>(out) = float4v{part.o[0] / sum, part.o[1] / sum, part.o[2] / sum, part.o[3] / sum};
   }
 }
 
-// A workgroup a unit; a thread has four columns of one query and every `slots`-th record.
+// grid = (units, parts of a unit's items): an item is four columns of one query; a thread has every `slots`-th record of one.
 template <int D> __global__ __launch_bounds__(1024) void chosen_merge_kernel(const float* __restrict__ records, int parts, int G, int slots, float* __restrict__ out) {
   extern __shared__ float joined[];
-  const int u = blockIdx.x, items = G * (D / 4), per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = threadIdx.x - slot * per_slot;
+  const int u = blockIdx.x, per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = blockIdx.y * per_slot + threadIdx.x - slot * per_slot;
+  const bool has = item < G * (D / 4);
   const int64_t size = record_floats(G, D);
   Part part;
-  if (item < items) part.join_records<D>(records + (int64_t)u * parts * size, slot, parts, slots, size, G, item / (D / 4), item % (D / 4));
-  finish_parts(part, slots, item, items, slot, joined, out + (int64_t)u * G * D);
+  if (has) part.join_records<D>(records + (int64_t)u * parts * size, slot, parts, slots, size, G, item / (D / 4), item % (D / 4));
+  finish_parts(part, slots, per_slot, slot, has, joined, out + (int64_t)u * G * D + 4 * item);
 }
 
 // ---- rows of a shared prompt, and of each sequence ---------------------------------------------
@@ -877,12 +878,14 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArg
   else own_part<T, D>(a, Q, (int64_t)((int)blockIdx.x - a.most_common) * kAttWaves + uniform(threadIdx.x >> 6));
 }
 
-// A workgroup a unit of a sequence: the records of the prompt's pieces and of its own, in order; threads as in chosen_merge_kernel.
+// The records of the prompt's pieces and of the sequence's own, in order; grid and threads as of chosen_merge_kernel.
 template <int D> __global__ __launch_bounds__(1024) void shared_merge_kernel(SharedArgs a, int slots) {
   extern __shared__ float joined[];
   const int L = a.own.L, H = a.own.H, G = a.G, u = blockIdx.x, lane = threadIdx.x & 63, P = a.common.B;
-  const int b = u / (L * H), l = u / H % L, h = u % H, items = G * (D / 4);
-  const int per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = threadIdx.x - slot * per_slot, g = item / (D / 4), c4 = item % (D / 4);
+  const int b = u / (L * H), l = u / H % L, h = u % H;
+  const int per_slot = blockDim.x / slots, slot = threadIdx.x / per_slot, item = blockIdx.y * per_slot + threadIdx.x - slot * per_slot;
+  const int g = item / (D / 4), c4 = item % (D / 4);
+  const bool has = item < G * (D / 4);
   const int own_rows = rows_of(a.own, b, l);
   // the prompt whose sequence this is, with what its layer holds: 64 prompts' together, a lane each, in one wait for memory
   Run run{0, 0};
@@ -904,23 +907,26 @@ template <int D> __global__ __launch_bounds__(1024) void shared_merge_kernel(Sha
   if (span.y > 0 && span.x >= 0) {
     const int tiles = tiles_of(a, run.n), at = (b - run.first) * G + g, tile = at / kTileQueries;
     const int64_t index = span.x + (int64_t)(h * tiles + tile) * span.y, size = record_floats(a.record_rows, D);
-    if (item < items && index + span.y <= a.most_common)
+    if (has && index + span.y <= a.most_common)
       part.join_records<D>(a.common_records + index * size, slot, span.y, slots, size, min(kTileQueries, run.n * G - tile * kTileQueries),
                            at - tile * kTileQueries, c4);
   }
   const int64_t size = record_floats(G, D);
-  if (item < items)
+  if (has)
     part.join_records<D>(a.own_records + (int64_t)u * a.own_parts * size, slot, min(a.own_parts, (own_rows + a.step_rows - 1) / a.step_rows), slots, size, G, g, c4);
-  finish_parts(part, slots, item, items, slot, joined, a.out + (int64_t)u * G * D);
+  finish_parts(part, slots, per_slot, slot, has, joined, a.out + (int64_t)u * G * D + 4 * item);
 }
 
-// Threads of a merge: as many as a unit has items, in whole waves, for each slot; more slots where few units have many records.
-struct MergeShape { int slots, threads; size_t lds; };
+// Shape of a merge: threads for all items of a unit, or, of few units, a wave's in each of several workgroups; more slots where there are many records.
+struct MergeShape {
+  int slots, threads, along;
+  size_t lds;
+};
 MergeShape merge_shape(int units, int records, int G, int d) {
-  const int items = G * (d / 4), per_slot = (items + 63) / 64 * 64;
+  const int items = G * (d / 4), all = (items + 63) / 64 * 64, per_slot = units >= 256 ? all : 64, along = (items + per_slot - 1) / per_slot;
   int slots = 1;
-  while (slots < 8 && records > 8 * slots && units * 2 * slots * per_slot <= 256 * 1024 && 2 * slots * per_slot <= 1024) slots *= 2;
-  return {slots, slots * per_slot, slots > 1 ? (size_t)slots * items * 6 * sizeof(float) : 0};
+  while (slots < 16 && records > 4 * slots && (int64_t)units * along * 2 * slots * per_slot <= 256 * 1024 && 2 * slots * per_slot <= 1024) slots *= 2;
+  return {slots, slots * per_slot, along, slots > 1 ? (size_t)slots * per_slot * 6 * sizeof(float) : 0};
 }
 
 Scale scale_of(float scale) {
@@ -997,7 +1003,7 @@ hipError_t attend_chosen_launch(const void* Q, int group, const fc_paged_kv& kv,
   if (e != hipSuccess || parts == 1) return e;
   ProfileScope ps("chosen_merge_kernel", s);
   const MergeShape m = merge_shape(units, parts, group, d);
-  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(units), dim3(m.threads), m.lds, s, records, parts, group, m.slots, out); };
+  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(units, m.along), dim3(m.threads), m.lds, s, records, parts, group, m.slots, out); };
   d == 128 ? launch(chosen_merge_kernel<128>) : launch(chosen_merge_kernel<64>);
   return hipGetLastError();
 }
@@ -1038,7 +1044,7 @@ hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& com
   if (e != hipSuccess) return e;
   ProfileScope ps("shared_merge_kernel", s);
   const MergeShape m = merge_shape(B * L * H, std::max(P ? z.groups / (L * H) : 1, parts), group, d);
-  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(B * L * H), dim3(m.threads), m.lds, s, a, m.slots); };
+  auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(B * L * H, m.along), dim3(m.threads), m.lds, s, a, m.slots); };
   d == 128 ? launch(shared_merge_kernel<128>) : launch(shared_merge_kernel<64>);
   return hipGetLastError();
 }
