@@ -674,9 +674,10 @@ __device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, in
   static_assert(S::kVectors % kAttThreads == 0 && 4 * kMine <= 8, "a thread has whole vectors; two steps' loads at most are waited for by number");
   S& s = *static_cast<S*>(lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
+  const int from = 16 * wave;                              // the wave's first query
   typename F::Queries q[N];
 #pragma unroll
-  for (int j = 0; j < N; ++j) load_queries(16 * (wave + j * kAttWaves), q[j]);
+  for (int j = 0; j < N; ++j) load_queries(from + j * 16 * kAttWaves, q[j]);
   State<T, D, N> state;
   // (rows that are not there stay what LDS has: values, for which a weight of 0 has to make 0)
   u32x4* const all_v = &s.v[0][0];
@@ -730,7 +731,7 @@ __device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, in
       asm volatile("" ::: "memory");
       after = after_that;
       after_that = at + kStages - 1 < n ? request(at + kStages - 1) : 0;
-      if (there) {
+      if (there && from < queries) {
         const int stage = at % kStages;
         typename F::Keys k;
         typename F::Values v;
@@ -754,7 +755,7 @@ __device__ __forceinline__ void wide_piece(void* lds, const T* K, const T* V, in
     }
   }
 #pragma unroll
-  for (int j = 0; j < N; ++j) write_record<T, D, N>(state, j, 16 * (wave + j * kAttWaves), queries, record, lane);
+  for (int j = 0; j < N; ++j) write_record<T, D, N>(state, j, from + j * 16 * kAttWaves, queries, record, lane);
 }
 
 template <typename T, int D> constexpr size_t shared_lds_bytes() { return sizeof(Staged<T, D>) > merge_bytes(D) ? sizeof(Staged<T, D>) : merge_bytes(D); }
