@@ -431,7 +431,8 @@ fc_status flashcache_append_paged(const fc_rotary_plan* plan, const int32_t* pos
                                   int64_t slots_stride_b, int64_t slots_stride_h, int32_t page_size, int64_t num_pages, void* K_pages,
                                   void* V_pages, void* bounds, void* hip_stream);
 
-/* Bounds (as above) of all pages that hold rows, from the cache; those of other pages stay as they are.  kv->V is not read.  Rows up to 1024 bytes. */
+/* Bounds (as above) of all pages that hold rows, from the cache; those of other pages stay as they are.  kv->V is not read.  Rows up to 1024 bytes.  A page that
+ * is in several units' tables has to hold as many rows for each. */
 fc_status flashcache_page_bounds(const fc_paged_kv* kv, void* bounds, void* hip_stream);
 
 /* The pages of each unit that its q_heads / kv_heads = G queries can score highest in: `count` places in its table, rising, -1 behind the last.  A page's

@@ -4,6 +4,10 @@
 // q_c high_c), so that the sum over the G query heads of a unit, sum_c high_c up_c + low_c down_c with up_c = sum_g max(q_gc, 0) and
 // down_c = sum_g min(q_gc, 0), ranks pages without reading their keys.  It is summed in 64 bits and rounded to 32 once: the order of the
 // pages then does not depend on the order of the sum.
+//
+// A few bytes and operations a page: bound by chains of loads and by the search for the smallest key that is taken.  From 64 units on a workgroup has a
+// unit, scores and choice: 112 units of 512 pages 15 us (scores 9.7), 896 of 102 pages 16 (12.2); as two kernels 9.0 + 6.1 and 15.6 + 7.4.  Fewer units'
+// scores are shared out over more workgroups: 4 units of 512 pages 4.3 + 6.0.  64-bit arithmetic is not what takes the time (products left out: the same).
 #include <algorithm>
 #include <type_traits>
 
@@ -370,6 +374,7 @@ hipError_t choose_launch(const void* Q, int group, const fc_paged_kv& kv, const 
         hipLaunchKernelGGL(kern, dim3(units), dim3(64 * waves), a.max_pages * sizeof(uint32_t), s, a, static_cast<const T*>(Q), group, static_cast<const T*>(bounds),
                            count, first, last, chosen);
       };
+      // (112 units of 512 pages: sixteen waves each 14 us, four 19; of more units four, so that several are on a compute unit)
       units <= 256 ? launch(choose_whole_kernel<T, D, 16>, 16) : launch(choose_whole_kernel<T, D, 4>, 4);
     });
     return hipGetLastError();
