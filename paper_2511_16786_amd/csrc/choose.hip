@@ -6,8 +6,8 @@
 // pages then does not depend on the order of the sum.
 //
 // A few bytes and operations a page: bound by chains of loads and by the search for the smallest key that is taken.  From 64 units on a workgroup has a
-// unit, scores and choice: 112 units of 512 pages 15 us (scores 9.7), 896 of 102 pages 16 (12.2); as two kernels 9.0 + 6.1 and 15.6 + 7.4.  Fewer units'
-// scores are shared out over more workgroups: 4 units of 512 pages 4.3 + 6.0.  64-bit arithmetic is not what takes the time (products left out: the same).
+// unit, scores and choice: 112 units of 512 pages 15 us (scores 9.7), 896 of 102 pages 16 (12.2); as two kernels 9.0 + 5.2 and 15.6 + 6.5.  Fewer units'
+// scores are shared out over more workgroups: 4 units of 512 pages 4.3 + 5.1.  64-bit arithmetic is not what takes the time (products left out: the same).
 #include <algorithm>
 #include <type_traits>
 
@@ -275,9 +275,13 @@ __device__ __forceinline__ void choose_largest(int blocks, int count, int tid, c
   uint32_t least = 0u;
   int with_least = 0;                                      // how many of those that are equal to it
   if (want > 0) {
-    for (int bit = 31; bit >= 0; --bit)
-      if (at_least(least | 1u << bit) >= want) least |= 1u << bit;
-    with_least = want - (least == 0xFFFFFFFFu ? 0 : at_least(least + 1u));
+    bool exact = false;                                    // as many keys as are wanted are not smaller: they are the ones
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+      const int n = at_least(least | 1u << bit);
+      if (n >= want) least |= 1u << bit;
+      exact = n == want;
+    }
+    with_least = exact ? want : want - (least == 0xFFFFFFFFu ? 0 : at_least(least + 1u));
   }
   int above = 0, equal = 0;                                // before this place
   if constexpr (WAVES > 1) __syncthreads();                // (all have read the last count)
