@@ -598,7 +598,7 @@ struct SharedArgs {
   PagedArgs common, own;         // of P prompts and of B sequences
   const int32_t* starts;         // [P + 1]
   int G, groups;                 // pieces of prompts that the launch aims at
-  int most_common;               // records of prompts that the workspace has, and as many workgroups, the launch's first
+  int most_common, common_groups;        // records of prompts that the workspace has; workgroups for them, the launch's first
   int record_rows;               // queries that a prompt's record has room for
   int own_parts, step_rows;      // waves of a sequence's unit, each with a record; rows of a step
   Scale scale;
@@ -880,8 +880,8 @@ template <typename T, int D> __device__ __forceinline__ void common_piece(const 
 template <typename T, int D>
 __global__ __launch_bounds__(kAttThreads, 2) void attend_shared_kernel(SharedArgs a, const T* __restrict__ Q) {
   extern __shared__ __align__(16) unsigned char lds[];
-  if ((int)blockIdx.x < a.most_common) common_piece<T, D>(a, Q, blockIdx.x, lds);
-  else own_part<T, D>(a, Q, (int64_t)((int)blockIdx.x - a.most_common) * kAttWaves + uniform(threadIdx.x >> 6));
+  if ((int)blockIdx.x < a.common_groups) common_piece<T, D>(a, Q, blockIdx.x, lds);
+  else own_part<T, D>(a, Q, (int64_t)((int)blockIdx.x - a.common_groups) * kAttWaves + uniform(threadIdx.x >> 6));
 }
 
 // The records of the prompt's pieces and of the sequence's own, in order; grid and threads as of chosen_merge_kernel.
@@ -1030,11 +1030,14 @@ hipError_t attend_shared_launch(const void* Q, int group, const fc_paged_kv& com
   const int step_rows = own.dtype == FC_BF16 ? 32 : 16;
   const int64_t units = (int64_t)B * L * H, reach = (int64_t)own.max_pages * own.page_size / step_rows;
   const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(z.own_parts, std::max(std::min(2048 / units, reach), reach / 4)));
-  SharedArgs a{paged_args(common), paged_args(own), starts, group, z.groups, (int)z.common, z.record_rows, parts, step_rows, scale_of(scale), records, own_records,
+  // (no more workgroups for prompts than the shortest pieces of all that the tables reach)
+  const int64_t pieces = ((int64_t)common.max_pages * common.page_size + kLeastSteps * step_rows - 1) / (kLeastSteps * step_rows);
+  const int64_t common_groups = P ? std::min<int64_t>(z.common, (int64_t)L * H * most_tiles(P, B, group) * pieces) : 0;
+  SharedArgs a{paged_args(common), paged_args(own), starts, group, z.groups, (int)z.common, (int)common_groups, z.record_rows, parts, step_rows, scale_of(scale), records, own_records,
                reinterpret_cast<int2*>(own_records + z.own * record_floats(group, d)), out};
   {
     ProfileScope ps("attend_shared_kernel", s);
-    const int64_t groups = z.common + (units * parts + kAttWaves - 1) / kAttWaves;
+    const int64_t groups = common_groups + (units * parts + kAttWaves - 1) / kAttWaves;
     auto launch = [&](auto kern, size_t lds, auto type) {
       typedef decltype(type) T;
       hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kAttThreads), lds, s, a, static_cast<const T*>(Q));
