@@ -654,7 +654,7 @@ template <typename T, int D> struct Staged {
 
 // 16 bytes a lane from memory into LDS, side by side from `to` on (the same for the wave); nothing for lanes that are off.  It counts as a load; what it
 // writes is there behind a wait for it.  (Written out: behind the builtin the compiler waits for all loads under way before it reads LDS.  There is
-// no output register that could be taken for written before it is.)
+// no output register that could be taken for written before it is, and these kernels use m0 for nothing else: it is reserved, so it cannot be named as written.)
 __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory");
 }
