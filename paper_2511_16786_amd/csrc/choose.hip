@@ -70,8 +70,7 @@ __global__ __launch_bounds__(kBoundThreads) void page_bounds_kernel(PagedArgs a,
     int page = -1, rows = 0;
     if (item < items) {
       const int at = (int)(item / units), u = (int)(item - at * units), b = u / (a.L * a.H), in = u - b * a.L * a.H;
-      rows = rows_of(a, b, in / a.H) - at * a.page_size;
-      rows = min(rows, a.page_size);
+      rows = (int)max((int64_t)0, min((int64_t)a.page_size, rows_of(a, b, in / a.H) - (int64_t)at * a.page_size));
       if (rows > 0) page = a.table[b * a.table_b + (int64_t)in * a.max_pages + at];
     }
     uint64_t there = __ballot(rows > 0 && page >= 0 && page < a.num_pages);

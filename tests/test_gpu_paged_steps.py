@@ -297,6 +297,19 @@ def test_page_bounds_of_many_pages_a_short_table_and_nans():
 
 
 # ---- choice -----------------------------------------------------------------------------------
+def test_page_bounds_of_a_table_that_reaches_past_31_bits():
+    # place 2^26 of a table of pages of 64 rows begins at row 2^32: it holds none of the unit's 5 rows
+    fc = _fc()
+    rng = np.random.default_rng(29)
+    K = _rand(rng, (2, 64, 64), torch.bfloat16)
+    table = torch.full((1, 1, 1, (1 << 26) + 1), -1, dtype=torch.int32, device="cuda")
+    table[..., 0], table[..., -1] = 0, 1
+    bounds = torch.full((2, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    fc.page_bounds(fc.PagedKV(K, K, _int([[5]]), table), bounds)
+    assert torch.equal(bounds[0], torch.stack([K[0, :5].amin(0), K[0, :5].amax(0)]))
+    assert (bounds[1] == 7.0).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,H,G,d,ps,count,first,last,lost", [
     ([[1]], 1, 1, 64, 16, 1, 0, 0, 0.0), ([[0, 40], [500, 1000]], 2, 7, 128, 16, 9, 1, 2, 0.0), ([[2000, 300]], 3, 2, 64, 16, 40, 0, 0, 0.2),
