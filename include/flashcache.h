@@ -402,8 +402,8 @@ fc_status flashcache_mx_decode_attention(const void* Q, const void* pages, const
 
 /* A paged cache as flashcache_select_gather_paged writes it: row j of unit (b,l,h) is in slot j % page_size of page block_table[b][l][h][j /
  * page_size] of K and V [num_pages][page_size][head_dim], all pointers device.  rows [batch][layers] are the rows that every head of a layer
- * holds (negative values count as 0, what the table does not reach is not there), block_table [batch][layers][kv_heads][max_pages]; both may be a layer's
- * slice of a larger one, with `rows_stride_b` and `table_stride_b` elements from a sequence to the next.  Pages that are negative or from num_pages on
+ * holds (negative values count as 0; what the table does not reach is not there, nor are rows behind the first 2^25 - 1), block_table
+ * [batch][layers][kv_heads][max_pages]; both may be a layer's slice of a larger one, with `rows_stride_b` and `table_stride_b` elements from a sequence to the next.  Pages that are negative or from num_pages on
  * are not there, and neither are their rows.  Fewer than 2^32 - 1 rows in all pages; K and V aligned to 16 bytes, rows multiples of 16 bytes. */
 typedef struct {
   int32_t batch, layers, kv_heads, head_dim;
@@ -442,7 +442,7 @@ fc_status flashcache_page_bounds(const fc_paged_kv* kv, void* bounds, void* hip_
  *   Q       device in, [B][L][q_heads][d] in the cache's dtype, of kv's batch, layers and head_dim;  bounds  as above;  kv's K and V are not read
  *   chosen  device out, int32 [B][L][kv_heads][count]
  *   workspace  device, 16-byte aligned, flashcache_choose_pages_workspace_bytes() bytes; calls that may run at the same time need one each
- * d in {64, 128}, G from 1 to 16. */
+ * d in {64, 128}, G from 1 to 16, count below 2^30. */
 size_t flashcache_choose_pages_workspace_bytes(const fc_paged_kv* kv);
 fc_status flashcache_choose_pages(const void* Q, int32_t q_heads, const fc_paged_kv* kv, const void* bounds, int32_t count, int32_t first,
                                   int32_t last, int32_t* chosen, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -615,6 +615,7 @@ fc_status flashcache_choose_pages(const void* Q, int32_t q_heads, const fc_paged
   fc_status st = check_attended(kv, q_heads);
   if (st != FC_OK) return st;
   if (count < 1 || first < 0 || last < 0 || (int64_t)first + last > count) return FC_EINVAL;
+  if (count >= 1 << 30) return FC_EUNSUPPORTED;
   if (kv->batch == 0) return FC_OK;
   st = check_paged_pointers(kv, true);
   if (st != FC_OK) return st;

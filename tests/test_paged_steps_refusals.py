@@ -67,6 +67,13 @@ def test_choice_refuses_arguments():
     assert call(kv=_kv(batch=0), Q=None, ws=None, size=0) == 0
 
 
+def test_choice_refuses_counts_beyond_31_bits():
+    # (the places behind the last page are written in steps of up to 1024: below 2^30 no step passes 31 bits)
+    from paper_2511_16786_amd import binding as b
+    for count in (1 << 30, 2 ** 31 - 1):
+        assert b._lib.flashcache_choose_pages(16, 4, ref(_kv()), 16, count, 1, 1, 4, 16, 1 << 40, None) == EUNSUPPORTED
+
+
 @pytest.mark.parametrize("over,status", BAD_CACHES + ATTENDED)
 def test_attention_refuses_caches(over, status):
     from paper_2511_16786_amd import binding as b
