@@ -7,7 +7,8 @@
 //
 // A few bytes and operations a page: bound by chains of loads and by the search for the smallest key that is taken.  From 64 units on a workgroup has a
 // unit, scores and choice: 112 units of 512 pages 15 us (scores 9.7), 896 of 102 pages 16 (12.2); as two kernels 9.0 + 5.2 and 15.6 + 6.5.  Fewer units'
-// scores are shared out over more workgroups: 4 units of 512 pages 4.3 + 5.1.  64-bit arithmetic is not what takes the time (products left out: the same).
+// scores are shared out over more workgroups: 4 units of 512 pages 4.3 + 5.1, unless a unit's bounds are no more than a workgroup has under way at once: 1 to 63 units
+// of 64 pages of 128 bf16 columns one after another 4.2 to 5.0 in place of 5.7 to 6.5.  64-bit arithmetic is not what takes the time (products left out: the same).
 #include <algorithm>
 #include <type_traits>
 
@@ -23,6 +24,7 @@ constexpr int kRowsAtOnce = 8;         // of a lane
 constexpr int kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
 constexpr int kPagesAtOnce = 4, kQueriesAtOnce = 8;
 constexpr int kMostKeys = 4096;        // that a workgroup has in LDS, or in registers
+constexpr int kFewBounds = 65536;      // bytes of a unit's bounds
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -223,7 +225,7 @@ __device__ __forceinline__ int score_pages(const PagedArgs& a, int b, int in, co
   return blocks;
 }
 
-// grid = (parts of a unit's pages, units): few units, or more pages than choose_whole_kernel has room for
+// grid = (parts of a unit's pages, units): few units of more than a few pages, or more pages than choose_whole_kernel has room for
 template <typename T, int D>
 __global__ __launch_bounds__(kScoreThreads) void page_score_kernel(PagedArgs a, const T* __restrict__ Q, int G, const T* __restrict__ bounds, int first, int last,
                                                                    uint32_t* __restrict__ keys) {
@@ -368,7 +370,10 @@ hipError_t choose_launch(const void* Q, int group, const fc_paged_kv& kv, const 
     if (kv.dtype == FC_BF16) kv.head_dim == 128 ? launch(uint16_t{}, std::integral_constant<int, 128>{}) : launch(uint16_t{}, std::integral_constant<int, 64>{});
     else kv.head_dim == 128 ? launch(float{}, std::integral_constant<int, 128>{}) : launch(float{}, std::integral_constant<int, 64>{});
   };
-  if (a.max_pages <= kMostKeys && units >= 64) {
+  // many units, or few pages (one launch in place of two, at 1 to 63 units one after another: 128 pages of 128 bf16 columns 5.3 to 5.8 us, 6.4 to 7.1;
+  // 256, or 64 KB more, 6.8 to 7.5 and 6.3 to 7.5, 512 10.9 to 11.9 and 7.7 to 9.7)
+  const bool few = (int64_t)a.max_pages * 2 * kv.head_dim * (kv.dtype == FC_BF16 ? 2 : 4) <= kFewBounds;
+  if (a.max_pages <= kMostKeys && (units >= 64 || few)) {
     ProfileScope ps("choose_whole_kernel", s);
     by_type([&](auto type, auto dim) {
       typedef decltype(type) T;

@@ -332,6 +332,24 @@ def test_choose_pages(dtype, rows, H, G, d, ps, count, first, last, lost):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,H,G,d,most", [
+    ([[0, 1, 403, 800, 1600, 2400]], 1, 4, 128, None), ([[70, 0], [33, 1021]], 2, 3, 64, 900), ([[512]], 3, 2, 128, None), ([[513]], 3, 2, 128, None),
+    ([[256, 255]], 1, 7, 128, None), ([[257, 30]], 1, 7, 128, None), ([[0, 5]], 1, 2, 128, 5000),
+])
+def test_choose_pages_of_few_units(dtype, rows, H, G, d, most):
+    # short layers in a long table, and tables around the longest that a workgroup scores and searches by itself
+    fc = _fc()
+    rng = np.random.default_rng(rows[0][-1])
+    c = Cache(rng, rows, H, d, 4, dtype, most=most, lost=0.1)
+    bounds = fc.page_bounds(c.kv)
+    B, L = c.rows_np.shape
+    Q = _rand(rng, (B, L, G * H, d), _dt(dtype))
+    for count, first, last in ((1, 0, 0), (9, 1, 2), (150, 0, 1)):
+        got = fc.choose_pages(Q, c.kv, bounds, count, first=first, last=last)
+        assert np.array_equal(got.cpu().numpy(), pr.choose_pages(_f64(Q), _f64(bounds), c.rows_np, c.table_np, 4, count, first, last)), count
+
+
 @pytest.mark.parametrize("dtype,B,L,H,G,d,ps,most,count,first,last,lost", [
     ("bf16", 5, 7, 2, 7, 128, 16, 500, 9, 1, 2, 0.1), ("f32", 3, 11, 2, 3, 64, 16, 2000, 70, 0, 0, 0.1), ("bf16", 10, 14, 2, 1, 64, 16, 400, 12, 2, 0, 0.3),
     ("f32", 13, 10, 2, 4, 128, 32, 900, 5, 0, 1, 0.0), ("bf16", 4, 8, 2, 2, 64, 4, 3000, 513, 5, 5, 0.0), ("bf16", 9, 15, 2, 2, 64, 4, 3000, 100, 0, 3, 0.0),
