@@ -453,7 +453,8 @@ fc_status flashcache_choose_pages(const void* Q, int32_t q_heads, const fc_paged
  *   Q    device in, [B][L][q_heads][d] in the cache's dtype; out  device out, float [B][L][q_heads][d]
  *   workspace  device, 16-byte aligned, flashcache_decode_chosen_workspace_bytes() bytes (may be 0); one for each call that may run at the same time
  * d in {64, 128}, 1 to 16 query heads a KV head for both dtypes, count * page_size below 2^30.  Products on the matrix cores: of bf16 exact in fp32, with
- * probabilities of 24 bits; of fp32 in fp32.  Sums and softmax in fp32. */
+ * probabilities of 24 bits; of fp32 in fp32.  Sums and softmax in fp32.  A NaN in a query, or in an attended key, makes that query's result NaN, one in an
+ * attended value its column.  Scores of -infinity have no weight, and a query that has no others gives zeros; an infinite value of V gives NaN or infinity. */
 size_t flashcache_decode_chosen_workspace_bytes(const fc_paged_kv* kv, int32_t q_heads, int32_t count);
 fc_status flashcache_decode_attention_chosen(const void* Q, int32_t q_heads, const fc_paged_kv* kv, const int32_t* chosen, int32_t count, float scale,
                                              float* out, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -468,7 +469,7 @@ fc_status flashcache_decode_attention_chosen(const void* Q, int32_t q_heads, con
  *           of their own alone.  (Starts that fall give unspecified values)
  *   out     device out, float [B][L][q_heads][d]; a unit without attended rows gives zeros
  *   workspace  device, 16-byte aligned, flashcache_decode_shared_workspace_bytes() bytes; calls that may run at the same time need one each
- * d in {64, 128}, 1 to 16 query heads a KV head; precision as for flashcache_decode_attention_chosen. */
+ * d in {64, 128}, 1 to 16 query heads a KV head; precision, and what is not a number, as for flashcache_decode_attention_chosen. */
 size_t flashcache_decode_shared_workspace_bytes(int32_t prompts, int32_t batch, int32_t layers, int32_t kv_heads, int32_t q_heads, int32_t head_dim,
                                                 int32_t dtype);
 fc_status flashcache_decode_attention_shared(const void* Q, int32_t q_heads, const fc_paged_kv* common, const int32_t* starts, const fc_paged_kv* own,

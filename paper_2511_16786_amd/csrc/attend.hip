@@ -408,6 +408,10 @@ __device__ __forceinline__ void walk(State<T, D, 1>& state, const typename Form<
   }
 }
 
+// What parts are weighted by, of the largest score that they have.  Without one (no rows, or scores that are not numbers, which no maximum takes) it is 0:
+// parts without rows are zeros and stay so, and what is not a number stays that.
+__device__ __forceinline__ float reference_of(float largest) { return largest > -INFINITY ? largest : 0.f; }
+
 // The waves' states as one, through LDS in a fixed order: into a record of `rows` queries, or (whole) the result itself.
 constexpr size_t merge_bytes(int d) { return (size_t)kAttWaves * 16 * (d + 2) * sizeof(float); }
 template <typename T, int D>
@@ -431,14 +435,14 @@ __device__ __forceinline__ void merge_waves(State<T, D, 1>& state, int rows, flo
     float M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kAttWaves; ++w) M = fmaxf(M, sm_m[w][g]);
+    const float ref = reference_of(M);
     float acc = 0.f, lt = 0.f;
-    if (M > -INFINITY)
 #pragma unroll
-      for (int w = 0; w < kAttWaves; ++w) {
-        const float f = exp2f(sm_m[w][g] - M);
-        acc = fmaf(sm_o[w][g][dim], f, acc);
-        lt = fmaf(sm_l[w][g], f, lt);
-      }
+    for (int w = 0; w < kAttWaves; ++w) {
+      const float f = exp2f(sm_m[w][g] - ref);
+      acc = fmaf(sm_o[w][g][dim], f, acc);
+      lt = fmaf(sm_l[w][g], f, lt);
+    }
     if (whole) {
       whole[(int64_t)g * D + dim] = acc / (lt == 0.f ? 1.f : lt);
     } else {
@@ -507,9 +511,8 @@ struct Part {
   float m = -INFINITY, sum = 0.f;
   float4v o = {0.f, 0.f, 0.f, 0.f};
   __device__ __forceinline__ void join(float m2, float sum2, const float4v& o2) {
-    const float M = fmaxf(m, m2);
-    if (M == -INFINITY) return;
-    const float w1 = exp2f(m - M), w2 = exp2f(m2 - M);
+    const float M = fmaxf(m, m2), ref = reference_of(M);
+    const float w1 = exp2f(m - ref), w2 = exp2f(m2 - ref);
     m = M;
     sum = sum * w1 + sum2 * w2;
 #pragma unroll
@@ -542,15 +545,14 @@ struct Part {
       float M = m;
 #pragma unroll
       for (int j = 0; j < kAtOnce; ++j) M = fmaxf(M, ms[j]);
-      if (M == -INFINITY) continue;
-      const float w = exp2f(m - M);
+      const float ref = reference_of(M), w = exp2f(m - ref);
       m = M;
       sum *= w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] *= w;
 #pragma unroll
       for (int j = 0; j < kAtOnce; ++j) {
-        const float v = exp2f(ms[j] - M);
+        const float v = exp2f(ms[j] - ref);
         sum = fmaf(sums[j], v, sum);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = fmaf(os[j][i], v, o[i]);

@@ -1,0 +1,129 @@
+"""Decode steps over the paged cache on the GPU where inputs are not finite, against float64 (oracle/paged_steps_ref.py): a NaN in a query or in an
+attended key makes all of that query's result NaN, one in an attended value its column, and neither anything else.
+
+What is finite has the tolerance of attention: a logit is off by at most d u sum |q k| scale, its scaling and exponential by 4 u (|logit| + 1), twice; the
+sums over n rows by n / 16 + 64 roundings, u = 2^-24, all of it relative to sum p |v|.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import paged_steps_ref as pr
+from test_gpu_paged_steps import U, Cache, _dt, _f64, _fc, _int, _rand
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def _plant(c, which, b, l, h, row, col, value=math.nan):
+    """`value` into K or V of one row of a unit."""
+    pages = c.K if which == "K" else c.V
+    pages[int(c.table_np[b, l, h, row // c.ps]), row % c.ps, col] = value
+    c.K64, c.V64 = _f64(c.K), _f64(c.V)
+
+
+def _check(got, Q, scale, G, rows_for):
+    """Returns how many heads of the result are NaN as a whole, and how many in part."""
+    got, Q = _f64(got), _f64(Q)
+    B, L, Hq, d = Q.shape
+    whole = part = 0
+    for b in range(B):
+        for l in range(L):
+            for g in range(Hq):
+                K, V = rows_for(b, l, g // G)
+                want, size, logit, terms = pr.attend(Q[b, l, g:g + 1], K, V, scale)
+                bad = np.isnan(want[0])
+                assert np.array_equal(np.isnan(got[b, l, g]), bad), (b, l, g, int(bad.sum()), int(np.isnan(got[b, l, g]).sum()))
+                whole += bad.all()
+                part += bad.any() and not bad.all()
+                if not bad.all():
+                    slip = 2 * (d * U * terms + 4 * U * (logit + 1)) + (K.shape[0] / 16 + 64) * U
+                    assert np.max((np.abs(got[b, l, g] - want[0]) - slip * size[0])[~bad]) <= 0, (b, l, g)
+    return whole, part
+
+
+# (one workgroup a unit; several; pages of which a NaN row is alone in its step; a unit of a single row)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,H,G,d,ps", [([[40, 5]], 2, 3, 64, 16), ([[2000, 1]], 1, 7, 128, 16), ([[1], [513]], 2, 16, 64, 32), ([[33, 400]], 1, 1, 128, 1)])
+def test_nan_in_attention_over_chosen_pages(dtype, rows, H, G, d, ps):
+    fc = _fc()
+    B, L = np.array(rows).shape
+    scale = 1.0 / math.sqrt(d)
+    for what in ("query", "first key", "last key", "value"):
+        rng = np.random.default_rng(d + ps)
+        c = Cache(rng, rows, H, d, ps, dtype)
+        Q = _rand(rng, (B, L, G * H, d), _dt(dtype))
+        if what == "query":
+            Q[0, 0, G - 1, 5] = math.nan
+        for b in range(B):
+            for l in range(L):
+                n = rows[b][l]
+                if what == "first key":
+                    _plant(c, "K", b, l, H - 1, 0, 7)
+                elif what == "last key":
+                    _plant(c, "K", b, l, H - 1, n - 1, d - 1)
+                elif what == "value":
+                    _plant(c, "V", b, l, 0, n // 2, 3)
+        chosen = np.broadcast_to(np.arange(c.most), (B, L, H, c.most))
+        got = fc.decode_attention_chosen(Q, c.kv, _int(chosen), scale)
+        found = _check(got, Q, scale, G, c.unit)
+        assert found == {"query": (1, 0), "value": (0, B * L * G)}.get(what, (B * L * G, 0)), what
+
+
+# (up to 16 queries a prompt, up to 64, more, two tiles of them; own rows alone, in one part and in many)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("common,own,G,H,d", [
+    (300, [1, 40], 7, 1, 128), (1, [1, 1], 2, 2, 64), (200, [1] * 9, 4, 1, 64), (129, [3] * 19, 7, 1, 128), (2000, [700, 1], 3, 2, 64), (0, [1, 700], 2, 2, 64),
+])
+def test_nan_in_attention_to_a_shared_prompt(dtype, common, own, G, H, d):
+    fc = _fc()
+    B, ps, scale = len(own), 16, 1.0 / math.sqrt(d)
+    for what in ("query", "first own key", "last own key", "prompt's key", "prompt's keys", "own value", "prompt's value"):
+        if common == 0 and what.startswith("prompt"):
+            continue
+        rng = np.random.default_rng(d + B)
+        cc, co = Cache(rng, [[common]], H, d, ps, dtype), Cache(rng, [[n] for n in own], H, d, ps, dtype)
+        Q = _rand(rng, (B, 1, G * H, d), _dt(dtype))
+        if what == "query":
+            Q[1, 0, 1, 0] = math.nan
+        elif what == "first own key":
+            _plant(co, "K", 0, 0, 0, 0, 1)
+        elif what == "last own key":
+            _plant(co, "K", B - 1, 0, 0, own[-1] - 1, 1)
+        elif what == "prompt's key":
+            _plant(cc, "K", 0, 0, H - 1, common // 2, 2)
+        elif what == "prompt's keys":
+            for row in range(common):
+                _plant(cc, "K", 0, 0, H - 1, row, 2)
+        elif what == "own value":
+            _plant(co, "V", 0, 0, 0, 0, 1)
+        else:
+            _plant(cc, "V", 0, 0, 0, common - 1, 1)
+        ws = fc.shared_workspace(Q, H, 1).fill_(255)
+        got = fc.decode_attention_shared(Q, cc.kv, _int([0, B]), co.kv, scale, workspace=ws)
+        found = _check(got, Q, scale, G, lambda b, l, h: tuple(np.concatenate(x) for x in zip(cc.unit(0, 0, h), co.unit(b, 0, h))))
+        assert found == {"query": (1, 0), "first own key": (G, 0), "last own key": (G, 0), "own value": (0, G),
+                         "prompt's value": (0, B * G)}.get(what, (B * G, 0)), what
+
+
+def test_a_nan_behind_a_units_rows_changes_nothing():
+    """Pages that a unit's rows or list do not reach, and a prompt that is another's."""
+    fc = _fc()
+    rng = np.random.default_rng(3)
+    G, d, ps = 3, 64, 16
+    cc, co = Cache(rng, [[90], [50]], 1, d, ps, "bf16"), Cache(rng, [[20]] * 4, 1, d, ps, "bf16")
+    for row in range(50):
+        _plant(cc, "K", 1, 0, 0, row, 0)
+    Q = _rand(rng, (4, 1, G, d), torch.bfloat16)
+    got = fc.decode_attention_shared(Q, cc.kv, _int([0, 2, 3]), co.kv, 0.125)
+
+    def rows_for(b, l, h):
+        return tuple(np.concatenate(x) for x in zip(cc.unit(0 if b < 2 else 1, 0, 0), co.unit(b, 0, 0))) if b < 3 else co.unit(b, 0, 0)
+    assert _check(got, Q, 0.125, G, rows_for) == (G, 0)
+    _plant(co, "K", 0, 0, 0, 3, 0)
+    chosen = _int([[[[1, -1]]], [[[0, 1]]], [[[1, 0]]], [[[-1, -1]]]])
+    got = fc.decode_attention_chosen(Q, co.kv, chosen, 0.125)
+    assert _check(got, Q, 0.125, G, lambda b, l, h: co.unit(b, 0, 0, ([1], [0, 1], [1, 0], [])[b])) == (0, 0)
+    assert bool((got[3] == 0).all())
