@@ -2,8 +2,8 @@
 //
 // A page's bounds are the lowest and the largest key of every column.  No key within them has a dot product with q above sum_c max(q_c low_c,
 // q_c high_c), so that the sum over the G query heads of a unit, sum_c high_c up_c + low_c down_c with up_c = sum_g max(q_gc, 0) and
-// down_c = sum_g min(q_gc, 0), ranks pages without reading their keys.  It is summed in 64 bits and rounded to 32 once: the order of the
-// pages then does not depend on the order of the sum.
+// down_c = sum_g min(q_gc, 0), ranks pages without reading their keys.  It is summed in 64 bits and rounded to 32 once: another
+// order of summation changes a sum by some 2^-53 of its terms, and the score only where that crosses the middle between two values of 32 bits.
 //
 // A few bytes and operations a page: bound by chains of loads and by the search for the smallest key that is taken.  From 64 units on a workgroup has a
 // unit, scores and choice: 112 units of 512 pages 15 us (scores 9.7), 896 of 102 pages 16 (12.2); as two kernels 9.0 + 5.2 and 15.6 + 6.5.  Fewer units'
@@ -133,11 +133,11 @@ __device__ __forceinline__ double add_lanes_16(double v) { // the sum over each 
   return v + moved(v, std::integral_constant<int, 0x140>{});
 }
 
-// A lane's 16 bytes of what a unit's queries make of each column: up = (sum + sum of magnitudes) / 2, down = (sum - sum of magnitudes) / 2.  A thread sums
-// up a column, all find theirs in LDS; the caller has a barrier between both.
+// What a unit's queries make of each column, up and down.  A thread sums up a column, all find theirs in LDS; the caller has a barrier between both.
+// (Each query to its own sum: differences of sums over all would lose a small one of the other sign.  One that is not a number goes to both.)
 template <typename T, int D> __device__ __forceinline__ void sum_queries(const T* q, int G, double (*sums)[D], int thread) {
   if (thread >= D) return;
-  double sum = 0.0, size = 0.0;
+  double up = 0.0, down = 0.0;
   for (int g0 = 0; g0 < G; g0 += kQueriesAtOnce) {
     T v[kQueriesAtOnce];
 #pragma unroll
@@ -148,13 +148,13 @@ template <typename T, int D> __device__ __forceinline__ void sum_queries(const T
       if constexpr (sizeof(T) == 2) x = bf16_to_f32(v[j]);
       else x = v[j];
       if (g0 + j < G) {
-        sum += (double)x;
-        size += fabs((double)x);
+        up += (double)(x < 0.f ? 0.f : x);
+        down += (double)(x > 0.f ? 0.f : x);
       }
     }
   }
-  sums[0][thread] = 0.5 * (sum + size);
-  sums[1][thread] = 0.5 * (sum - size);
+  sums[0][thread] = up;
+  sums[1][thread] = down;
 }
 
 // Keys of pages first, first + stride, ... (a wave's; kAbreast side by side, kPagesAtOnce of a lane group under way together), of a unit's `blocks`.

@@ -127,3 +127,17 @@ def test_a_nan_behind_a_units_rows_changes_nothing():
     got = fc.decode_attention_chosen(Q, co.kv, chosen, 0.125)
     assert _check(got, Q, 0.125, G, lambda b, l, h: co.unit(b, 0, 0, ([1], [0, 1], [1, 0], [])[b])) == (0, 0)
     assert bool((got[3] == 0).all())
+
+
+def test_choice_between_queries_of_very_different_sizes():
+    """A column's queries of either sign, 2^60 apart: the small one's product counts where the large one's is 0."""
+    fc = _fc()
+    rng = np.random.default_rng(9)
+    c = Cache(rng, [[4 * 60]], 1, 64, 4, "f32")
+    bounds = fc.page_bounds(c.kv)
+    bounds[:, 1] = 0                                                # max(2^60 low, 0) = 0, max(-q low, 0) = -q low
+    bounds[:, 0] = -bounds[:, 0].abs() - 1
+    Q = torch.zeros((1, 1, 2, 64), device="cuda")
+    Q[0, 0, 0], Q[0, 0, 1] = 2.0 ** 60, -0.75
+    got = fc.choose_pages(Q, c.kv, bounds, 7, first=0, last=0)
+    assert np.array_equal(got.cpu().numpy(), pr.choose_pages(_f64(Q), _f64(bounds), c.rows_np, c.table_np, 4, 7, 0, 0))
