@@ -437,7 +437,7 @@ fc_status flashcache_page_bounds(const fc_paged_kv* kv, void* bounds, void* hip_
 
 /* The pages of each unit that its q_heads / kv_heads = G queries can score highest in: `count` places in its table, rising, -1 behind the last.  A page's
  * score is the sum over the G queries of the largest dot product that a key within its bounds can have, sum_g sum_c max(q_gc low_c, q_gc high_c), in 64
- * bits, rounded to 32.  The first `first` and the last `last` of the pages that hold a unit's rows are taken whatever their scores (first + last <=
+ * bits, rounded to 32 (0 times infinity is 0).  The first `first` and the last `last` of the pages that hold a unit's rows are taken whatever their scores (first + last <=
  * count), then those of largest score, the earlier one of two alike; pages that are not there never, those whose score is not a number last.
  *   Q       device in, [B][L][q_heads][d] in the cache's dtype, of kv's batch, layers and head_dim;  bounds  as above;  kv's K and V are not read
  *   chosen  device out, int32 [B][L][kv_heads][count]

@@ -45,6 +45,16 @@ def append_bounds(bounds, K_pages, slots, page_size):
     return out
 
 
+def page_score(q, low, high):
+    """sum_g sum_c of the largest product of q_gc and a key from low_c to high_c, rounded to float32, of q [G, d]: q_gc high_c, of a negative query
+    q_gc low_c, where 0 times infinity is 0.  Columns without numbers (+infinity, -infinity) reach from -infinity to +infinity."""
+    none = (low == np.inf) & (high == -np.inf)
+    bound = np.where(q < 0, np.where(none, -np.inf, low), np.where(none, np.inf, high))
+    with np.errstate(invalid="ignore"):
+        product = q * bound
+        return float(np.float32(np.where(np.isnan(product) & ~np.isnan(q) & ~np.isnan(bound), 0.0, product).sum()))
+
+
 def choose_pages(Q, bounds, rows, table, page_size, count, first, last):
     """Q float64 [B, L, Hq, d], bounds float64 [num_pages, 2, d]: places [B, L, H, count]."""
     B, L, H, most = table.shape
@@ -60,9 +70,7 @@ def choose_pages(Q, bounds, rows, table, page_size, count, first, last):
                     page = int(table[b, l, h, i])
                     if not 0 <= page < bounds.shape[0]:
                         continue
-                    with np.errstate(invalid="ignore"):
-                        up, down = np.where(q < 0, 0.0, q).sum(0), np.where(q > 0, 0.0, q).sum(0)
-                        score = float(np.float32((bounds[page, 1] * up + bounds[page, 0] * down).sum()))
+                    score = page_score(q, bounds[page, 0], bounds[page, 1])
                     forced = i < first or i >= blocks - last
                     ranked.append((0 if forced else 2 if math.isnan(score) else 1, 0.0 if forced or math.isnan(score) else -score, i))
                 taken = sorted(i for _, _, i in sorted(ranked)[:count])

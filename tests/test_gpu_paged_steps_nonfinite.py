@@ -129,6 +129,60 @@ def test_a_nan_behind_a_units_rows_changes_nothing():
     assert bool((got[3] == 0).all())
 
 
+# ---- choice ---------------------------------------------------------------------------------------
+# (one workgroup for scores and choice of a unit; scores shared out; columns of both widths, lane groups of 8, 16 and 32 lanes)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,H,G,d", [([[4 * 90, 4 * 61]], 2, 3, 64), ([[4 * 300]], 2, 7, 128), ([[4 * 700]], 1, 1, 64)])
+def test_choice_where_bounds_are_infinite(dtype, rows, H, G, d):
+    """Pages with keys of either infinity, and with columns of NaNs alone, whose bounds are +infinity and -infinity: the score is what the keys' largest
+    products make it, however many queries have one sign."""
+    fc = _fc()
+    rng = np.random.default_rng(d + G)
+    c = Cache(rng, rows, H, d, 4, dtype)
+    B, L = np.array(rows).shape
+    Q = _rand(rng, (B, L, G * H, d), _dt(dtype)).abs()              # every column's queries of one sign ...
+    Q[..., 1::4] *= -1
+    Q[..., 2::4] *= torch.from_numpy(rng.choice([-1.0, 1.0], Q[..., 2::4].shape)).to(Q)      # ... or of both
+    Q[..., 3] = 0
+    for l in range(L):
+        for h in range(H):
+            at = rng.permutation(rows[0][l])[:40]
+            for i, row in enumerate(at):
+                _plant(c, "K", 0, l, h, row, i % 4 if i < 20 else rng.integers(d), (math.inf, -math.inf)[i // 4 % 2])
+            for row in range(8, 12):
+                _plant(c, "K", 0, l, h, row, 5)                     # place 2
+            for row in range(20, 24):
+                _plant(c, "K", 0, l, h, row, 3)                     # place 5: where the queries are 0
+    bounds = fc.page_bounds(c.kv)
+    found = _f64(bounds)
+    assert np.isposinf(found[:, 0]).any() and np.isposinf(found[:, 1]).any() and np.isneginf(found[:, 0]).any() and np.isneginf(found[:, 1]).any()
+    scores = [pr.page_score(_f64(Q)[0, 0, :G], *found[p]) for p in c.table_np[0, 0, 0][:rows[0][0] // 4]]
+    assert sum(map(math.isinf, scores)) > 5 and sum(map(math.isfinite, scores)) > 20
+    for count, first, last in ((1, 0, 0), (12, 0, 0), (33, 1, 2)):
+        got = fc.choose_pages(Q, c.kv, bounds, count, first=first, last=last)
+        assert np.array_equal(got.cpu().numpy(), pr.choose_pages(_f64(Q), found, c.rows_np, c.table_np, 4, count, first, last)), count
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_choice_where_queries_are_infinite_or_nan(dtype):
+    fc = _fc()
+    rng = np.random.default_rng(7)
+    H, G, d = 3, 2, 64
+    c = Cache(rng, [[4 * 200]], H, d, 4, dtype)
+    bounds = fc.page_bounds(c.kv)
+    bounds[c.table[0, 0, :, 30].long(), 1, 9] = 0
+    Q = _rand(rng, (1, 1, G * H, d), _dt(dtype))
+    # a query of +infinity: pages that it can score +infinity in, then those of other scores, then -infinity
+    Q[0, 0, 0, 9], Q[0, 0, 2, 9], Q[0, 0, 4, 9] = math.inf, -math.inf, math.nan
+    found = _f64(bounds)
+    kinds = {(h, "nan" if math.isnan(s) else "inf" if s == math.inf else "-inf" if s == -math.inf else "")
+             for h in range(H) for s in (pr.page_score(_f64(Q)[0, 0, h * G:(h + 1) * G], *found[p]) for p in c.table_np[0, 0, h])}
+    assert kinds >= {(0, "inf"), (0, "-inf"), (1, "inf"), (1, "-inf"), (2, "nan")}, kinds
+    for count in (1, 50, 150, 199):
+        got = fc.choose_pages(Q, c.kv, bounds, count, first=0, last=1)
+        assert np.array_equal(got.cpu().numpy(), pr.choose_pages(_f64(Q), found, c.rows_np, c.table_np, 4, count, 0, 1)), count
+
+
 def test_choice_between_queries_of_very_different_sizes():
     """A column's queries of either sign, 2^60 apart: the small one's product counts where the large one's is 0."""
     fc = _fc()
