@@ -129,6 +129,59 @@ def test_a_nan_behind_a_units_rows_changes_nothing():
     assert bool((got[3] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("common,own,G,H,d", [(90, [1, 40], 7, 1, 128), (200, [5] * 9, 4, 1, 64), (129, [3] * 19, 7, 1, 128), (0, [300, 20], 2, 2, 64)])
+def test_infinite_keys_and_values(dtype, common, own, G, H, d):
+    """Keys whose scores are -infinity have no weight; where there are no others the result is zeros.  An infinite value shows in its column alone."""
+    fc = _fc()
+    rng = np.random.default_rng(d + len(own))
+    B, ps, scale = len(own), 16, 1.0 / math.sqrt(d)
+    cc, co = Cache(rng, [[common]], H, d, ps, dtype), Cache(rng, [[n] for n in own], H, d, ps, dtype)
+    Q = _rand(rng, (B, 1, G * H, d), _dt(dtype))
+    Q[..., 4] = Q[..., 4].abs() + 1
+    for row in range(0, common, 3):
+        _plant(cc, "K", 0, 0, H - 1, row, 4, -math.inf)
+    for b in range(B):
+        for row in range(1, own[b], 2):
+            _plant(co, "K", b, 0, 0, row, 4, -math.inf)
+
+    def rows_for(b, l, h):
+        K, V = (np.concatenate(x) for x in zip(cc.unit(0, 0, h), co.unit(b, 0, h)))
+        there = np.isfinite(K).all(1)
+        return K[there], V[there]
+
+    def shared():
+        return fc.decode_attention_shared(Q, cc.kv, _int([0, B]), co.kv, scale)
+    assert _check(shared(), Q, scale, G, rows_for) == (0, 0)
+    every = _int(np.broadcast_to(np.arange(co.most), (B, 1, H, co.most)))
+
+    def own_rows(b, l, h):
+        K, V = co.unit(b, 0, h)
+        there = np.isfinite(K).all(1)
+        return K[there], V[there]
+    assert _check(fc.decode_attention_chosen(Q, co.kv, every, scale), Q, scale, G, own_rows) == (0, 0)
+    # a value of infinity, of the first sequence's first row of head 0
+    _plant(co, "V", 0, 0, 0, 0, 6, math.inf)
+    for got, clean in ((shared(), rows_for), (fc.decode_attention_chosen(Q, co.kv, every, scale), own_rows)):
+        assert not bool(torch.isfinite(got[0, 0, :G, 6]).any())
+        got[0, 0, :G, 6] = 0
+        co.V64 = np.where(np.isinf(co.V64), 0.0, co.V64)
+        for b in range(B):
+            for g in range(G * H):
+                K, V = clean(b, 0, g // G)
+                if b == 0 and g < G:
+                    V = V.copy()
+                    V[:, 6] = 0
+                want, size, logit, terms = pr.attend(_f64(Q)[b, 0, g:g + 1], K, V, scale)
+                slip = 2 * (d * U * terms + 4 * U * (logit + 1)) + (K.shape[0] / 16 + 64) * U
+                assert np.max(np.abs(_f64(got)[b, 0, g] - want[0]) - slip * size[0]) <= 0, (b, g)
+    # no other scores
+    co.K[..., 4] = torch.where(torch.isnan(co.K[..., 4]), co.K[..., 4], -math.inf)
+    cc.K[..., 4] = torch.where(torch.isnan(cc.K[..., 4]), cc.K[..., 4], -math.inf)
+    co.V.copy_(torch.where(torch.isinf(co.V), torch.zeros_like(co.V), co.V))
+    assert bool((shared() == 0).all()) and bool((fc.decode_attention_chosen(Q, co.kv, every, scale) == 0).all())
+
+
 # ---- choice ---------------------------------------------------------------------------------------
 # (one workgroup for scores and choice of a unit; scores shared out; columns of both widths, lane groups of 8, 16 and 32 lanes)
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
