@@ -7,7 +7,8 @@
 // fewer waves, 114).  With bounds a workgroup has a stretch of one KV head's tokens: it stores their keys and keeps the least and largest of what it stores
 // (rounded values: rounding keeps the order) until the page changes, so that no page has two writers and no row is read back.  2 x 1003 tokens of 32, 8
 // and 8 heads (0.05 GB) 16 us, of which keys and the rest would take 12 each by themselves, both little more than their chains of loads (a wave a stretch in
-// place of a workgroup 30).  Of a single token a wave has a key: eight sequences' step with bounds 5.4 us.
+// place of a workgroup 30); the kernel has the arguments of both kinds, and keeps up to 106 scalar registers in lanes of vector ones.  Of a single token a wave
+// has a key: eight sequences' step with bounds 5.4 us.
 #include <algorithm>
 #include <type_traits>
 #include <math.h>

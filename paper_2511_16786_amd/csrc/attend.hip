@@ -15,7 +15,8 @@
 // merged.  Bound by memory: 64 pages of 64 bf16 rows of 112 units (0.24 GB) 43 us, and as long without the arithmetic; some 8 us of it are the chain of
 // list, table and first rows and the end, the rest is read at 6.7 TB/s.
 // Where more do, the workgroup has up to 128 queries, two tiles of 16 a wave, and reads the rows once for all of them, through LDS.  16 answers of 7 heads to
-// 28 layers of 4 heads, 6554 rows, and 128 rows of their own in the mean (0.50 GB, 43 GFLOP): 137 us (each 16 queries reading the rows for themselves 482).
+// 28 layers of 4 heads, 6554 rows, and 128 rows of their own in the mean (0.50 GB, 43 GFLOP): 137 us (each 16 queries reading the rows for themselves 482), in the
+// long run, when the clock has risen, 118.
 // The prompts' rows by themselves take 76 us without the arithmetic, the arithmetic some 100 without them: matrix instructions keep a SIMD busy for a third
 // of the time, others for two fifths, and two waves a SIMD, as many as 256 registers allow, overlap them in part only.  With two terms of probabilities 126.
 #include <math.h>
@@ -955,8 +956,8 @@ struct SharedSizes {
 SharedSizes shared_sizes(int P, int B, int L, int H, int G, int d, int dtype) {
   SharedSizes z;
   const int64_t units = (int64_t)B * L * H;
-  // pieces of prompts: nearly as many workgroups as are resident together (two on a compute unit, three of 64 columns; 16 answers to 28 layers: 512 of
-  // them 148 us, 480 138, 448 150); of sequences: parts for four times as many waves, 16 of a unit at most
+  // pieces of prompts: some less than as many workgroups as are resident together (two on a compute unit, three of 64 columns); how many less goes by one
+  // measured case (16 answers to 28 layers: 512 of them 148 us, 480 138, 448 150); of sequences: parts for four times as many waves, 16 of a unit at most
   z.groups = d == 64 ? 720 : 480;
   z.own_parts = (int)std::max<int64_t>(1, std::min<int64_t>(16, 8192 / units));
   const int64_t tiles = (int64_t)L * H * most_tiles(P, B, G);

@@ -7,8 +7,8 @@
 //
 // A few bytes and operations a page: bound by chains of loads and by the search for the smallest key that is taken.  From 64 units on a workgroup has a
 // unit, scores and choice: 112 units of 512 pages 15 us (scores 9.7), 896 of 102 pages 16 (12.2); as two kernels 9.0 + 5.2 and 15.6 + 6.5.  Fewer units'
-// scores are shared out over more workgroups: 4 units of 512 pages 4.3 + 5.1, unless a unit's bounds are no more than a workgroup has under way at once: 1 to 63 units
-// of 64 pages of 128 bf16 columns one after another 4.2 to 5.0 in place of 5.7 to 6.5.  64-bit arithmetic is not what takes the time (products left out: the same).
+// scores are shared out over more workgroups: 4 units of 512 pages 4.3 + 5.1, unless a unit's bounds are at most half of what sixteen
+// waves have under way at once (64 KB): 1 to 63 units of 64 pages of 128 bf16 columns one after another 4.2 to 5.0 in place of 5.7 to 6.5.  64-bit arithmetic is not what takes the time (products left out: the same).
 #include <algorithm>
 #include <type_traits>
 
